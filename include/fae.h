@@ -27,6 +27,7 @@
  *   - Types: row ids, hot slots, sample ids and CSR offsets are int32; access
  *     counts are uint32 (precondition: fewer than 2^32 accesses per row);
  *     weights, pooled outputs and gradients are fp32, row-major.
+ *     (Layer norm and dropout also take bf16 and fp16 rows.)
  *   - Limits: n_tables <= FAE_MAX_TABLES; dim >= 1 (dim % 4 == 0 takes the
  *     16-byte vector path); lookups per table per call < 2^31; rows per table < 2^31.
  */
@@ -145,7 +146,10 @@ int32_t fae_set_option(fae_ctx *ctx, const char *name, int64_t value);
 #define FAE_K_ESTIMATE 16    /* chunk counts of the sampled logger                */
 #define FAE_K_READ_PROBE 17  /* plain streaming read (read-only bandwidth ceiling)      */
 #define FAE_K_FILL_PROBE 18  /* plain streaming fill (write-only bandwidth ceiling)     */
-#define FAE_K_COUNT 19
+#define FAE_K_NORM 19        /* layer norm, forward and the rows' gradient       */
+#define FAE_K_NORM_WEIGHTS 20 /* layer norm: its weights' gradient from partial sums */
+#define FAE_K_DROPOUT 21     /* dropout, both directions                         */
+#define FAE_K_COUNT 22
 int32_t fae_timing_enable(fae_ctx *ctx, int32_t on);
 int32_t fae_timing_reset(fae_ctx *ctx);
 int32_t fae_timing_read(fae_ctx *ctx, int32_t kernel_class, double *h_total_ms, int64_t *h_launches);
@@ -314,6 +318,77 @@ int32_t fae_embbag_fwd_opts(fae_ctx *ctx, const fae_tables *hot_tables, const fl
 int32_t fae_embbag_bwd_opts(fae_ctx *ctx, const fae_tables *hot_tables, float *const *h_hotW,
                             const fae_batch *hot_batch, const float *gout, int64_t gout_row_stride,
                             const fae_step_opts *opts, const fae_bwd_debug *dbg, void *ws, size_t ws_bytes);
+
+/* ---- layer norm and dropout of the pooled rows ----------------------------------
+ * What stands between the pooled forward and the dense layers, and on the way back between
+ * their gradient and the embedding's backward.  Both work on rows of any origin:
+ * n_rows samples of n_parts rows of `width` values each, value c of part p of sample r at
+ * [r*row_stride + p*width + c]: the pooled output with one row per table (n_parts tables of
+ * dim `width`, each with its own weights), or any matrix (n_parts = 1).  A row stride is in
+ * values and >= n_parts*width.  Values between the samples are neither read nor written.
+ * Types: FAE_F32, FAE_BF16, FAE_F16 (two bytes each); x and y have the same type, or one of
+ * them is FAE_F32 where a call says so.  Every sum, mean and product is fp32 whatever the types; a result is rounded
+ * to its type once, to nearest even.  Buffers need the alignment of their values, nothing more
+ * (widths, strides and addresses on 16 bytes are fastest).  An output may be the
+ * input it has the shape of (same address, stride and type); every other overlap of a call's buffers is not
+ * allowed, and refused with FAE_EINVAL where rows of input and output share bytes. */
+#define FAE_F32 0
+#define FAE_BF16 1
+#define FAE_F16 2
+
+/* Dropout.  The generator is Philox4x32-10 (Salmon, Moraes, Dror, Shaw: "Parallel random
+ * numbers: as easy as 1, 2, 3", 2011): the mask is made where it is needed and never stored, forward and
+ * backward make the same one from the same seed and offset, and no value depends on how a kernel shares out the
+ * work.  With R = r*n_parts + p and O = offset + (d_offset ? *d_offset : 0) modulo 2^64,
+ *   counter = (c >> 3, R, O low word, O high word), key = (seed low word, seed high word),
+ * and the four words of the result are eight 16-bit numbers, the low half of a word first; number c & 7
+ * belongs to value c.  With T = p * 65536 rounded to the nearest integer (ties to even), a value whose number is below T is
+ * dropped (0, whatever it was), and every other is multiplied by 65536 / (65536 - T).  So p is kept to 2^-17:
+ * 0 and 1 are taken (p = 1 drops everything), other p that would round to them are refused.  A caller
+ * uses another offset for every call (or adds to *d_offset on the device between replays
+ * of a captured step). */
+typedef struct {
+    double p; /* share that is dropped, 0 <= p <= 1 */
+    uint64_t seed;
+    uint64_t offset;
+    const uint64_t *d_offset; /* device, may be NULL; read when the kernel runs */
+} fae_drop;
+
+/* Layer norm over the rows:
+ *   h = (x - mean(x)) / sqrt(var(x) + eps) with the mean and the (biased) variance of the row's width values,
+ *   y = gamma[p][c] * h + beta[p][c], then dropout if asked for.
+ * A row of equal values (the zeros of an empty bag) has h = 0. */
+typedef struct {
+    int64_t n_rows;
+    int32_t n_parts; /* 1 .. FAE_MAX_TABLES; n_rows * n_parts < 2^31 */
+    int32_t width;   /* 1 .. FAE_NORM_MAX_WIDTH */
+    int32_t x_type;  /* of x and gx */
+    int32_t y_type;  /* of y and gy: x_type, or FAE_BF16 / FAE_F16 with x_type FAE_F32 */
+    float eps;       /* > 0, finite */
+    const float *gamma; /* device fp32[n_parts*width], or NULL: ones  */
+    const float *beta;  /* device fp32[n_parts*width], or NULL: zeros */
+} fae_norm;
+#define FAE_NORM_MAX_WIDTH 16384
+/* y from x; drop may be NULL.  Nothing is kept for the backward but x.  Asynchronous. */
+int32_t fae_layer_norm_fwd(fae_ctx *ctx, const fae_norm *norm, const void *x, int64_t x_row_stride, void *y,
+                           int64_t y_row_stride, const fae_drop *drop);
+/* The gradients of fae_layer_norm_fwd (beta is not read).  With g = gy through the same dropout (the same drop as in the forward):
+ *   gx = (a - mean(a) - h * mean(a * h)) / sqrt(var(x) + eps) with a = gamma * g, means over the row,
+ *   dgamma[p][c] = sum over r of g * h,  dbeta[p][c] = sum over r of g.
+ * dgamma and dbeta (device fp32[n_parts*width]) are overwritten (zeros if n_rows is 0); either may be NULL.  gx may be gy (same
+ * address, stride and type) or x.  The sums are taken in an order that depends on the sizes alone, so a call's results are
+ * the same every time.  Two calls that may overlap (two streams, two captured graphs) need a
+ * workspace each.  Asynchronous. */
+size_t fae_layer_norm_bwd_workspace_bytes(const fae_norm *norm);
+int32_t fae_layer_norm_bwd(fae_ctx *ctx, const fae_norm *norm, const void *x, int64_t x_row_stride, const void *gy,
+                           int64_t gy_row_stride, void *gx, int64_t gx_row_stride, float *dgamma, float *dbeta,
+                           const fae_drop *drop, void *ws, size_t ws_bytes);
+/* y = x through dropout, and its gradient gx = gy through the same dropout.  n_rows * n_parts < 2^32; n_parts * width <
+ * 2^31; x and y have the same type or one of them is FAE_F32.  Asynchronous. */
+int32_t fae_dropout_fwd(fae_ctx *ctx, const fae_drop *drop, int64_t n_rows, int32_t n_parts, int32_t width, const void *x,
+                        int32_t x_type, int64_t x_row_stride, void *y, int32_t y_type, int64_t y_row_stride);
+int32_t fae_dropout_bwd(fae_ctx *ctx, const fae_drop *drop, int64_t n_rows, int32_t n_parts, int32_t width, const void *gy,
+                        int32_t y_type, int64_t gy_row_stride, void *gx, int32_t x_type, int64_t gx_row_stride);
 
 /* ---- embedding synchronisation between the hot tables and the full tables ----
  * (Sec. 3 (4); Sec. 6.2, "Embedding Synchronization") */

@@ -21,6 +21,8 @@ FAE_SRC_DEVICE, FAE_SRC_PROCEDURAL = 0, 1
 FAE_SYNC_HOT_TO_FULL, FAE_SYNC_FULL_TO_HOT = 0, 1
 FAE_POOL_SUM, FAE_POOL_MEAN = 0, 1
 FAE_OPT_SGD, FAE_OPT_ROWWISE_ADAGRAD = 0, 1
+FAE_F32, FAE_BF16, FAE_F16 = 0, 1, 2
+FAE_NORM_MAX_WIDTH = 16384
 
 EXPORTS = [
     "fae_create", "fae_destroy", "fae_last_error", "fae_version", "fae_sync", "fae_set_option",
@@ -33,6 +35,8 @@ EXPORTS = [
     "fae_sync_hot_rows", "fae_estimate_workspace_bytes", "fae_estimate_hot", "fae_choose_cutoff_sampled",
     "fae_t_quantile", "fae_sched_init", "fae_sched_report", "fae_sched_segment",
     "fae_embbag_fwd_opts", "fae_embbag_bwd_opts",
+    "fae_layer_norm_fwd", "fae_layer_norm_bwd_workspace_bytes", "fae_layer_norm_bwd",
+    "fae_dropout_fwd", "fae_dropout_bwd",
 ]
 
 
@@ -70,6 +74,15 @@ class _StepOpts(C.Structure):
                 ("h_state", C.POINTER(C.c_void_p))]
 
 
+class _Drop(C.Structure):
+    _fields_ = [("p", C.c_double), ("seed", C.c_uint64), ("offset", C.c_uint64), ("d_offset", C.c_void_p)]
+
+
+class _Norm(C.Structure):
+    _fields_ = [("n_rows", C.c_int64), ("n_parts", C.c_int32), ("width", C.c_int32), ("x_type", C.c_int32),
+                ("y_type", C.c_int32), ("eps", C.c_float), ("gamma", C.c_void_p), ("beta", C.c_void_p)]
+
+
 class _Sched(C.Structure):
     _fields_ = [("rate", C.c_double), ("prev", C.c_double), ("u", C.c_int32), ("falls", C.c_int32),
                 ("reports", C.c_int32)]
@@ -94,7 +107,7 @@ def load():
     lib.fae_version.restype = C.c_char_p
     for name in ("fae_choose_cutoff_workspace_bytes", "fae_build_workspace_bytes",
                  "fae_partition_workspace_bytes", "fae_bwd_workspace_bytes", "fae_estimate_workspace_bytes",
-                 "fae_bwd_static_workspace_bytes"):
+                 "fae_bwd_static_workspace_bytes", "fae_layer_norm_bwd_workspace_bytes"):
         getattr(lib, name).restype = C.c_size_t
     lib.fae_destroy.restype = None
     lib.fae_kernel_name.restype = C.c_char_p
@@ -147,6 +160,81 @@ class Batch:
             b._keep = (idx, off, nl)
             self._c = b
         return self._c
+
+
+@dataclass
+class Drop:
+    """Dropout of a share p; forward and backward of one call take the same seed and offset.  d_offset: a device
+    tensor of one int64 that is added to offset when the kernel runs (steps captured into a graph)."""
+    p: float
+    seed: int
+    offset: int = 0
+    d_offset: Optional[torch.Tensor] = None
+
+    def c(self, device: int):
+        at = None
+        if self.d_offset is not None:
+            if self.d_offset.numel() != 1:
+                raise TypeError("d_offset: need one int64")
+            at = _ptr_on(self.d_offset, torch.int64, device)
+        d = _Drop(float(self.p), self.seed & ((1 << 64) - 1), self.offset & ((1 << 64) - 1), at)
+        d._keep = self.d_offset
+        return d
+
+
+@dataclass
+class Norm:
+    """Layer norm of n_rows samples of n_parts rows of width values; x_dtype: of x and its gradient, y_dtype:
+    of y and its gradient.  gamma and beta: device fp32[n_parts, width] or None."""
+    n_rows: int
+    n_parts: int
+    width: int
+    gamma: Optional[torch.Tensor] = None
+    beta: Optional[torch.Tensor] = None
+    eps: float = 1e-5
+    x_dtype: torch.dtype = torch.float32
+    y_dtype: torch.dtype = torch.float32
+
+    def c(self, device: int):
+        for name, t in (("gamma", self.gamma), ("beta", self.beta)):
+            if t is not None and t.numel() != self.n_parts * self.width:
+                raise ValueError(f"{name}: need {self.n_parts} x {self.width} values, got {tuple(t.shape)}")
+        n = _Norm(int(self.n_rows), int(self.n_parts), int(self.width), _type(self.x_dtype), _type(self.y_dtype), float(self.eps),
+                  _ptr_on(self.gamma, torch.float32, device), _ptr_on(self.beta, torch.float32, device))
+        n._keep = (self.gamma, self.beta)
+        return n
+
+
+_TYPES = {torch.float32: FAE_F32, torch.bfloat16: FAE_BF16, torch.float16: FAE_F16}
+
+
+def _type(dtype: torch.dtype) -> int:
+    if dtype not in _TYPES:
+        raise TypeError(f"need float32, bfloat16 or float16, got {dtype}")
+    return _TYPES[dtype]
+
+
+def _ptr_on(t: Optional[torch.Tensor], dtype, device: int):
+    """_ptr for a tensor that has to be on the context's own device."""
+    if t is not None and t.is_cuda and t.device.index != device:
+        raise ValueError(f"need a tensor on device {device}, got {t.device}")
+    return _ptr(t, dtype)
+
+
+def _rows(t: torch.Tensor, n_parts: int, width: int, dtype, device: int):
+    """Pointer and row stride of [n_rows, n_parts, width] or [n_rows, n_parts * width], whose rows may lie apart."""
+    if t.dtype != dtype or not t.is_cuda:
+        raise TypeError(f"need a device tensor of {dtype}, got {t.dtype} on {t.device}")
+    if t.device.index != device:
+        raise ValueError(f"need a tensor on device {device}, got {t.device}")
+    if tuple(t.shape[1:]) not in ((n_parts, width), (n_parts * width,)):
+        raise ValueError(f"need [rows, {n_parts}, {width}] or [rows, {n_parts * width}], got {tuple(t.shape)}")
+    want = 1
+    for n, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+        if n > 1 and stride != want:
+            raise ValueError(f"need the values of a sample side by side, got strides {t.stride()}")
+        want *= n
+    return C.c_void_p(t.data_ptr()), C.c_int64(t.stride(0) if t.shape[0] > 1 else n_parts * width)
 
 
 def _ptrs(tensors: Sequence[Optional[torch.Tensor]], dtype):
@@ -215,7 +303,7 @@ def fae_set_option(ctx: Context, name: str, value: int):
     ctx.check(load().fae_set_option(ctx._h, name.encode(), C.c_int64(value)))
 
 
-FAE_K_COUNT = 19
+FAE_K_COUNT = 22
 
 
 def fae_kernel_name(kernel_class: int) -> str:
@@ -416,6 +504,93 @@ def fae_embbag_bwd_opts(ctx: Context, hot_tables: Tables, hotW: List[torch.Tenso
     ctx.check(load().fae_embbag_bwd_opts(ctx._h, C.byref(t), _ptrs(hotW, torch.float32), C.byref(b),
                                          _ptr(gout, torch.float32), C.c_int64(gout_row_stride), C.byref(o),
                                          dbg, _ptr(ws, torch.uint8), C.c_size_t(ws.numel())))
+
+
+def _norm_args(ctx: Context, norm: Norm, drop: Optional[Drop], *tensors):
+    n = norm.c(ctx.device)
+    d = drop.c(ctx.device) if drop is not None else None
+    at = []
+    for t, dtype in tensors:
+        if t.shape[0] != norm.n_rows:
+            raise ValueError(f"need {norm.n_rows} rows, got {tuple(t.shape)}")
+        at += _rows(t, norm.n_parts, norm.width, dtype, ctx.device)
+    return n, d, at
+
+
+def _prepare(ctx: Context, fn, args, keep):
+    """A call with everything marshalled, for loops: raises what the library reports."""
+    def call():
+        rc = fn(*args)
+        if rc != FAE_OK:
+            ctx.check(rc)
+    call._keep = keep
+    return call
+
+
+def prepare_layer_norm_fwd(ctx: Context, norm: Norm, x: torch.Tensor, y: torch.Tensor, drop: Optional[Drop] = None):
+    """fae_layer_norm_fwd of these tensors, marshalled once: a zero-argument callable."""
+    n, d, at = _norm_args(ctx, norm, drop, (x, norm.x_dtype), (y, norm.y_dtype))
+    return _prepare(ctx, load().fae_layer_norm_fwd, (ctx._h, C.byref(n), *at, C.byref(d) if d is not None else None),
+                    (ctx, n, d, x, y))
+
+
+def fae_layer_norm_fwd(ctx: Context, norm: Norm, x: torch.Tensor, y: torch.Tensor, drop: Optional[Drop] = None):
+    prepare_layer_norm_fwd(ctx, norm, x, y, drop)()
+
+
+def fae_layer_norm_bwd_workspace_bytes(norm: Norm) -> int:
+    n = _Norm(int(norm.n_rows), int(norm.n_parts), int(norm.width), _type(norm.x_dtype), _type(norm.y_dtype), float(norm.eps), None, None)
+    return int(load().fae_layer_norm_bwd_workspace_bytes(C.byref(n)))
+
+
+def prepare_layer_norm_bwd(ctx: Context, norm: Norm, x: torch.Tensor, gy: torch.Tensor, gx: torch.Tensor,
+                           dgamma: Optional[torch.Tensor], dbeta: Optional[torch.Tensor], ws: torch.Tensor,
+                           drop: Optional[Drop] = None):
+    """fae_layer_norm_bwd of these tensors, marshalled once: a zero-argument callable."""
+    n, d, at = _norm_args(ctx, norm, drop, (x, norm.x_dtype), (gy, norm.y_dtype), (gx, norm.x_dtype))
+    for name, t in (("dgamma", dgamma), ("dbeta", dbeta)):
+        if t is not None and t.numel() != norm.n_parts * norm.width:
+            raise ValueError(f"{name}: need {norm.n_parts} x {norm.width} values, got {tuple(t.shape)}")
+    return _prepare(ctx, load().fae_layer_norm_bwd,
+                    (ctx._h, C.byref(n), *at, _ptr_on(dgamma, torch.float32, ctx.device), _ptr_on(dbeta, torch.float32, ctx.device),
+                     C.byref(d) if d is not None else None, _ptr_on(ws, torch.uint8, ctx.device), C.c_size_t(ws.numel())),
+                    (ctx, n, d, x, gy, gx, dgamma, dbeta, ws))
+
+
+def fae_layer_norm_bwd(ctx: Context, norm: Norm, x: torch.Tensor, gy: torch.Tensor, gx: torch.Tensor,
+                       dgamma: Optional[torch.Tensor], dbeta: Optional[torch.Tensor], ws: torch.Tensor,
+                       drop: Optional[Drop] = None):
+    prepare_layer_norm_bwd(ctx, norm, x, gy, gx, dgamma, dbeta, ws, drop)()
+
+
+def _prepare_dropout(ctx: Context, fn, drop: Drop, src: torch.Tensor, dst: torch.Tensor):
+    """src and dst: [rows, width] or [rows, parts, width], of the same shape."""
+    if src.shape != dst.shape or src.dim() not in (2, 3):
+        raise ValueError(f"need [rows, width] or [rows, parts, width] twice, got {tuple(src.shape)} and {tuple(dst.shape)}")
+    n_parts, width = (src.shape[1] if src.dim() == 3 else 1), src.shape[-1]
+    s = _rows(src, n_parts, width, src.dtype, ctx.device)
+    o = _rows(dst, n_parts, width, dst.dtype, ctx.device)
+    d = drop.c(ctx.device)
+    return _prepare(ctx, fn, (ctx._h, C.byref(d), C.c_int64(src.shape[0]), C.c_int32(n_parts), C.c_int32(width),
+                              s[0], C.c_int32(_type(src.dtype)), s[1], o[0], C.c_int32(_type(dst.dtype)), o[1]), (ctx, d, src, dst))
+
+
+def prepare_dropout_fwd(ctx: Context, drop: Drop, x: torch.Tensor, y: torch.Tensor):
+    """fae_dropout_fwd of these tensors, marshalled once: a zero-argument callable."""
+    return _prepare_dropout(ctx, load().fae_dropout_fwd, drop, x, y)
+
+
+def fae_dropout_fwd(ctx: Context, drop: Drop, x: torch.Tensor, y: torch.Tensor):
+    prepare_dropout_fwd(ctx, drop, x, y)()
+
+
+def prepare_dropout_bwd(ctx: Context, drop: Drop, gy: torch.Tensor, gx: torch.Tensor):
+    """fae_dropout_bwd of these tensors, marshalled once: a zero-argument callable."""
+    return _prepare_dropout(ctx, load().fae_dropout_bwd, drop, gy, gx)
+
+
+def fae_dropout_bwd(ctx: Context, drop: Drop, gy: torch.Tensor, gx: torch.Tensor):
+    prepare_dropout_bwd(ctx, drop, gy, gx)()
 
 
 def fae_sync_hot_rows(ctx: Context, tables: Tables, n_hot: Sequence[int], hot_ids: List[torch.Tensor],

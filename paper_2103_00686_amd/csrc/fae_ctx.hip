@@ -240,7 +240,7 @@ extern "C" const char *fae_kernel_name(int32_t k)
                                              "bwd_reduce", "bwd_fixup", "lds_sort",  "fill",         "profile",
                                              "partition",  "build",     "other",     "copy_probe",
                                              "fwd_sort",   "sync_rows", "estimate",  "read_probe",
-                                             "fill_probe"};
+                                             "fill_probe", "norm",      "norm_weights", "dropout"};
     return (k >= 0 && k < FAE_K_COUNT) ? names[k] : "?";
 }
 

@@ -1,0 +1,76 @@
+// What layer norm and dropout share: rows of fp32, bf16 or fp16 values in parts, their host checks, and the
+// generator of the dropout mask (gfx950).
+#pragma once
+
+#include "fae_internal.h"
+
+typedef __bf16 fae_bf16;
+typedef _Float16 fae_f16;
+
+// ---------------------------------------------------------------------------------
+// host checks
+// ---------------------------------------------------------------------------------
+static inline int fae_type_size(int32_t type) { return type == FAE_F32 ? 4 : 2; }
+
+// one side of a call: n_rows samples of `row` values, `stride` values apart
+struct fae_rows {
+    const void *p;
+    int32_t type;
+    int64_t stride;
+};
+
+// the checks of one buffer (n_rows > 0): there, aligned to its values, no row over the next, addressable
+int32_t fae_check_rows(fae_ctx *ctx, const char *who, const char *what, const fae_rows &b, int64_t n_rows, int64_t row);
+// an output beside an input of the same shape: the same rows or none in common
+int32_t fae_check_overlap(fae_ctx *ctx, const char *who, const fae_rows &out, const fae_rows &in, int64_t n_rows, int64_t row);
+
+// the dropout of a launch, as the kernels take it
+struct fae_drop_args {
+    uint32_t below;  // numbers below this one are dropped (0 .. 65536); 0: no dropout at all
+    float scale;     // what the others are multiplied by
+    uint32_t key[2];
+    uint64_t offset;
+    const uint64_t *d_offset;
+};
+int32_t fae_check_drop(fae_ctx *ctx, const char *who, const fae_drop *drop, fae_drop_args *out);
+
+#ifdef __HIPCC__
+
+// ---------------------------------------------------------------------------------
+// Philox4x32-10 (Salmon, Moraes, Dror, Shaw 2011).  Its ten rounds are 20 products of 32 by 32 bits and 60 exclusive
+// ors and additions, for eight values: 16 bits each decide as well as 32 would (a share of dropped values is kept to
+// 2^-17), and half the generator's work is left out.
+// ---------------------------------------------------------------------------------
+struct fae_mask8 {
+    uint32_t w[4]; // number j of the eight: half j & 1 of word j >> 1
+    __device__ __forceinline__ uint32_t number(int j) const { return j & 1 ? w[j >> 1] >> 16 : w[j >> 1] & 0xffffu; }
+};
+
+__device__ __forceinline__ uint64_t fae_drop_offset(const fae_drop_args &d) { return d.offset + (d.d_offset ? *d.d_offset : 0); }
+
+__device__ __forceinline__ fae_mask8 fae_philox(uint32_t group, uint32_t row, uint64_t offset, uint32_t k0, uint32_t k1)
+{
+    uint32_t c0 = group, c1 = row, c2 = (uint32_t)offset, c3 = (uint32_t)(offset >> 32);
+#pragma unroll
+    for (int r = 0; r < 10; ++r) {
+        const uint64_t a = (uint64_t)c0 * 0xD2511F53u, b = (uint64_t)c2 * 0xCD9E8D57u;
+        c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
+        c1 = (uint32_t)b;
+        c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+        c3 = (uint32_t)a;
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+    return fae_mask8{{c0, c1, c2, c3}};
+}
+
+// A dropped value is zero whatever it was: a choice, not a product.  The product is rounded to fp32 also where fp16 is
+// stored: the compiler would multiply and round to fp16 in one instruction, and a result would depend on where it does.
+__device__ __forceinline__ float fae_drop1(float v, uint32_t number, uint32_t below, float scale)
+{
+    float kept = v * scale;
+    asm("" : "+v"(kept));
+    return number < below ? 0.0f : kept;
+}
+
+#endif // __HIPCC__

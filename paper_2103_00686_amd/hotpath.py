@@ -311,5 +311,66 @@ class HotPath:
         ts = tstart.cpu().tolist()
         return ([uniq[ts[z]:ts[z + 1]] for z in range(self.nt)], [runlen[ts[z]:ts[z + 1]] for z in range(self.nt)])
 
+    # -- layer norm and dropout between the pooled rows and the dense layers -----------
+    @staticmethod
+    def _norm_of(x: torch.Tensor, gamma, beta, eps: float, y_dtype) -> B.Norm:
+        if x.dim() not in (2, 3):
+            raise ValueError(f"need [rows, width] or [rows, parts, width], got {tuple(x.shape)}")
+        parts = x.shape[1] if x.dim() == 3 else 1
+        return B.Norm(x.shape[0], parts, x.shape[-1], gamma, beta, eps, x.dtype, y_dtype)
+
+    def layer_norm(self, x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None,
+                   eps: float = 1e-5, drop: Optional[B.Drop] = None, out_dtype: Optional[torch.dtype] = None,
+                   out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Layer norm of every row of x, [rows, width] or [rows, parts, width] with weights for each part (the
+        pooled output with a norm per table), then dropout."""
+        if out is None:
+            out = torch.empty(x.shape, dtype=out_dtype or x.dtype, device=self.dev)
+        B.fae_layer_norm_fwd(self.ctx, self._norm_of(x, gamma, beta, eps, out.dtype), x, out, drop)
+        return out
+
+    def layer_norm_backward(self, x: torch.Tensor, gy: torch.Tensor, gamma: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                            drop: Optional[B.Drop] = None, out: Optional[torch.Tensor] = None):
+        """(gx, dgamma, dbeta) of ``layer_norm`` from its input and its output's gradient; drop as in the forward."""
+        if out is None:
+            out = torch.empty(x.shape, dtype=x.dtype, device=self.dev)
+        norm = self._norm_of(x, gamma, None, eps, gy.dtype)
+        dgamma, dbeta = (torch.empty((norm.n_parts, norm.width) if x.dim() == 3 else (norm.width,), dtype=torch.float32, device=self.dev)
+                         for _ in range(2))
+        ws = self._workspace("norm", B.fae_layer_norm_bwd_workspace_bytes(norm))
+        B.fae_layer_norm_bwd(self.ctx, norm, x, gy, out, dgamma, dbeta, ws, drop)
+        return out, dgamma, dbeta
+
+    def dropout(self, x: torch.Tensor, drop: B.Drop, out_dtype: Optional[torch.dtype] = None,
+                out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        if out is None:
+            out = torch.empty(x.shape, dtype=out_dtype or x.dtype, device=self.dev)
+        B.fae_dropout_fwd(self.ctx, drop, x, out)
+        return out
+
+    def dropout_backward(self, gy: torch.Tensor, drop: B.Drop, out_dtype: Optional[torch.dtype] = None,
+                         out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        if out is None:
+            out = torch.empty(gy.shape, dtype=out_dtype or gy.dtype, device=self.dev)
+        B.fae_dropout_bwd(self.ctx, drop, gy, out)
+        return out
+
+    # pre-marshalled forms of the four, for tight loops: zero-argument callables
+    def prepare_layer_norm(self, norm: B.Norm, x: torch.Tensor, y: torch.Tensor, drop: Optional[B.Drop] = None):
+        return B.prepare_layer_norm_fwd(self.ctx, norm, x, y, drop)
+
+    def prepare_layer_norm_backward(self, norm: B.Norm, x: torch.Tensor, gy: torch.Tensor, gx: torch.Tensor,
+                                    dgamma: Optional[torch.Tensor] = None, dbeta: Optional[torch.Tensor] = None,
+                                    drop: Optional[B.Drop] = None):
+        """With a workspace of its own, so that captured steps share none."""
+        ws = torch.empty(max(B.fae_layer_norm_bwd_workspace_bytes(norm), 256), dtype=torch.uint8, device=self.dev)
+        return B.prepare_layer_norm_bwd(self.ctx, norm, x, gy, gx, dgamma, dbeta, ws, drop)
+
+    def prepare_dropout(self, drop: B.Drop, x: torch.Tensor, y: torch.Tensor):
+        return B.prepare_dropout_fwd(self.ctx, drop, x, y)
+
+    def prepare_dropout_backward(self, drop: B.Drop, gy: torch.Tensor, gx: torch.Tensor):
+        return B.prepare_dropout_bwd(self.ctx, drop, gy, gx)
+
     def sync(self):
         B.fae_sync(self.ctx)

@@ -1,0 +1,310 @@
+"""Layer norm and its backward against their definition in 64 bits (rows_ref.py has the bounds)."""
+import numpy as np
+import pytest
+import torch
+
+import rows_ref as R
+from paper_2103_00686_amd import binding as B
+from paper_2103_00686_amd.hotpath import HotPath
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+TYPES = [(F32, F32), (F32, BF16), (F32, F16), (BF16, BF16), (F16, F16)]
+EPS = 1e-5
+
+
+@pytest.fixture(scope="module")
+def hp():
+    return HotPath([1], 4)
+
+
+def _buf(n, parts, width, dtype, pad, lead, fill=float("nan")):
+    """[n, parts, width] with `pad` values behind every sample and `lead` in front of the first."""
+    flat = torch.full((lead + n * (parts * width + pad),), fill, dtype=dtype, device="cuda")
+    return flat, flat[lead:].view(n, parts * width + pad)[:, :parts * width].unflatten(1, (parts, width))
+
+
+def _make(seed, n, parts, width, tx, ty, affine=True, pad=0, lead=0, mean=0.0, std=1.0):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    _, x = _buf(n, parts, width, tx, pad, lead)
+    x.copy_(torch.randn((n, parts, width), device="cuda", generator=gen) * std + mean)
+    _, gy = _buf(n, parts, width, ty, pad, lead)
+    gy.copy_(torch.randn((n, parts, width), device="cuda", generator=gen))
+    gamma = torch.randn((parts, width), device="cuda", generator=gen) if affine else None
+    beta = torch.randn((parts, width), device="cuda", generator=gen) if affine else None
+    return x, gy, gamma, beta
+
+
+def _check(hp, x, gy, gamma, beta, ty, p=0.0, pad=0, lead=0, eps=EPS, counter=None):
+    n, parts, width = x.shape
+    drop, keep, scale = None, None, 1.0
+    if p > 0:
+        drop = B.Drop(p, 0x1234567890ABCDEF, (1 << 40) + 7, counter)
+        keep, scale = R.keep_and_scale(n * parts, width, p, drop.seed, drop.offset + (int(counter) if counter is not None else 0))
+        keep = keep.reshape(x.shape).cuda()
+    ref = R.NormRef(x, gamma, beta, eps, keep, scale)
+    yflat, y = _buf(n, parts, width, ty, pad, lead)
+    xflat, gx = _buf(n, parts, width, x.dtype, pad, lead)
+    x0, gy0 = x.clone(), gy.clone()
+    hp.layer_norm(x, gamma, beta, eps, drop, out=y)
+    _, dgamma, dbeta = hp.layer_norm_backward(x, gy, gamma, eps, drop, out=gx)
+    hp.sync()
+    assert torch.equal(x, x0) and torch.equal(gy, gy0)
+    R.assert_within(y, *ref.forward(ty), "y")
+    (rx, rg, rb), (tx, tg, tb) = ref.backward(gy, x.dtype)
+    R.assert_within(gx, rx, tx, "gx")
+    R.assert_within(dgamma.reshape(parts, width), rg, tg, "dgamma")
+    R.assert_within(dbeta.reshape(parts, width), rb, tb, "dbeta")
+    # what lies in front of, behind and between the rows was left as it was
+    for flat, t in ((yflat, y), (xflat, gx)):
+        assert int(torch.isnan(flat).sum()) == flat.numel() - t.numel()
+
+
+WIDTHS = [1, 2, 3, 4, 5, 7, 8, 9, 12, 16, 17, 20, 31, 32, 33, 50, 63, 64, 65, 100, 127, 128, 129, 255, 256, 257, 260, 300, 511, 512, 513,
+          768, 1000, 1023, 1024, 1025, 1500, 1664, 2047, 2048, 2049, 2500, 4095, 4096, 4097, 6000, 8191, 8192, 8193, 12288, 16383, 16384]
+
+
+@pytest.mark.parametrize("tx,ty", TYPES)
+@pytest.mark.parametrize("width", WIDTHS)
+def test_widths(hp, width, tx, ty):
+    n = 37 if width <= 2048 else 5
+    x, gy, gamma, beta = _make(width, n, 1, width, tx, ty)
+    _check(hp, x, gy, gamma, beta, ty)
+
+
+@pytest.mark.parametrize("tx,ty", TYPES)
+@pytest.mark.parametrize("width", [3, 8, 50, 64, 100, 200, 516, 1030, 1664, 4100, 9000])
+def test_widths_with_dropout_and_gaps(hp, width, tx, ty):
+    """Rows that start anywhere (one value past 16 bytes, odd strides), dropout on top, no weights in half of them."""
+    n = 29 if width <= 1100 else 4
+    affine = width % 3 != 0
+    x, gy, gamma, beta = _make(width, n, 2, width, tx, ty, affine, pad=5, lead=3)
+    _check(hp, x, gy, gamma, beta, ty, p=0.3, pad=5, lead=3)
+
+
+@pytest.mark.parametrize("parts", [1, 2, 3, 5, 7, 13, 16, 26, 33, 64])
+@pytest.mark.parametrize("width", [1, 6, 16, 64, 100, 256, 600])
+def test_parts(hp, parts, width):
+    """Weights and their gradients belong to the part; counts of rows and parts that share no factor with anything."""
+    n = {1: 333, 6: 211}.get(width, 67)
+    x, gy, gamma, beta = _make(parts, n, parts, width, F32, F32)
+    _check(hp, x, gy, gamma, beta, F32, p=0.25)
+
+
+@pytest.mark.parametrize("n", [1, 2, 3, 15, 64, 65, 1023, 5000])
+@pytest.mark.parametrize("parts,width", [(1, 16), (26, 64), (1, 256), (1, 1024), (3, 100)])
+def test_rows(hp, n, parts, width):
+    x, gy, gamma, beta = _make(n, n, parts, width, F32, BF16)
+    _check(hp, x, gy, gamma, beta, BF16)
+
+
+@pytest.mark.parametrize("width", [16, 50, 256, 1000, 4096])
+def test_no_rows(hp, width):
+    x = torch.empty((0, 2, width), device="cuda")
+    gamma = torch.ones((2, width), device="cuda")
+    assert hp.layer_norm(x, gamma, gamma).shape == x.shape
+    norm = B.Norm(0, 2, width, gamma, gamma)
+    dg, db = torch.full((2, 2, width), 3.0, device="cuda")
+    hp.prepare_layer_norm_backward(norm, x, x, x, dg, db)()
+    hp.sync()
+    assert not bool(dg.any()) and not bool(db.any())
+
+
+@pytest.mark.parametrize("width", [1, 5, 64, 100, 256, 1024, 4096, 16384])
+def test_rows_of_equal_values(hp, width):
+    """Empty bags: the variance is zero (exactly: the values and their count times them are numbers of fp32)."""
+    x, gy, gamma, beta = _make(1, 9, 1, width, F32, F32)
+    x[::2] = torch.tensor([0.0, 1.0, -2.0, 4.0, 0.5], device="cuda")[:, None, None]
+    y = hp.layer_norm(x, gamma, beta, EPS)
+    hp.sync()
+    assert torch.equal(y[::2], beta.expand_as(y[::2]))
+    _check(hp, x, gy, gamma, beta, F32)
+
+
+@pytest.mark.parametrize("width", [7, 64, 300, 1024, 5000, 16384])
+@pytest.mark.parametrize("mean,std", [(1e4, 1.0), (-300.0, 1e-2), (0.0, 1e12), (0.0, 1e-12), (1e6, 1e3)])
+def test_far_means_and_scales(hp, width, mean, std):
+    """A mean far above the spread: the bound is that of centred values, not of the mean's own rounding."""
+    x, gy, gamma, beta = _make(3, 17, 1, width, F32, F32, mean=mean, std=std)
+    _check(hp, x, gy, gamma, beta, F32)
+
+
+@pytest.mark.parametrize("eps", [1e-30, 1e-12, 0.5])
+def test_eps(hp, eps):
+    x, gy, gamma, beta = _make(3, 17, 2, 100, F32, F32)
+    _check(hp, x, gy, gamma, beta, F32, eps=eps)
+
+
+@pytest.mark.parametrize("parts,width", [(1, 16), (1, 24), (3, 64), (26, 32), (1, 512), (1, 2000), (1, 8192)])
+@pytest.mark.parametrize("n", [1, 17, 1000, 20011])
+def test_weight_gradients_of_whole_numbers(hp, n, parts, width):
+    """h is +1 or -1 exactly (x = +-4096 in equal numbers: the variance is 2^24, eps is below its last place) and gy holds small
+    whole numbers, so both gradients are sums of whole numbers below 2^24: equal bit for bit in any order."""
+    if n * parts * width > 40_000_000:
+        n = 40_000_000 // (parts * width)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(n)
+    order = torch.rand((n, parts, width), device="cuda", generator=gen).argsort(-1)
+    sign = torch.where(order < width // 2, 1.0, -1.0)
+    gy = torch.randint(-8, 9, (n, parts, width), device="cuda", generator=gen).float()
+    _, dgamma, dbeta = hp.layer_norm_backward(sign * 4096, gy)
+    hp.sync()
+    assert torch.equal(dbeta.reshape(parts, width), gy.sum(0, dtype=torch.float64).float())
+    assert torch.equal(dgamma.reshape(parts, width), (gy * sign).sum(0, dtype=torch.float64).float())
+
+
+@pytest.mark.parametrize("width", [16, 100, 256, 1024, 3000, 16384])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_a_bad_row_stays_its_own(hp, width, bad):
+    """A row with an infinity or a NaN spoils itself and the weights' gradients, no other row."""
+    x, gy, gamma, beta = _make(5, 21, 1, width, F32, F32)
+    want_y = hp.layer_norm(x, gamma, beta)
+    want, _, _ = hp.layer_norm_backward(x, gy, gamma)
+    x[7, 0, width - 1] = bad
+    gy[12, 0, 0] = bad
+    y = hp.layer_norm(x, gamma, beta)
+    gx, _, _ = hp.layer_norm_backward(x, gy, gamma)
+    hp.sync()
+    rows = torch.arange(21, device="cuda")
+    assert torch.equal(y[rows != 7], want_y[rows != 7]) and bool(torch.isnan(y[7]).any())
+    good = (rows != 7) & (rows != 12)
+    assert torch.equal(gx[good], want[good]) and bool(torch.isnan(gx[7]).any() & torch.isnan(gx[12]).any())
+
+
+@pytest.mark.parametrize("width", [24, 64, 600, 2048])
+def test_bad_gradients_that_are_dropped(hp, width):
+    """An infinity or a NaN where dropout drops is as if it were not there."""
+    x, gy, gamma, _ = _make(6, 31, 2, width, F32, BF16)
+    drop = B.Drop(0.5, 99, 3)
+    keep = R.keep_and_scale(62, width, 0.5, 99, 3)[0].reshape(31, 2, width).cuda()
+    want = hp.layer_norm_backward(x, gy, gamma, EPS, drop)
+    spoiled = torch.where(keep, gy, torch.where(x > 0, float("nan"), float("inf")).to(BF16))
+    got = hp.layer_norm_backward(x, spoiled, gamma, EPS, drop)
+    hp.sync()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("width", [40, 256, 1500, 9000])
+def test_in_place(hp, width):
+    x, gy, gamma, beta = _make(8, 33, 1, width, BF16, BF16)
+    y = hp.layer_norm(x, gamma, beta)
+    gx, dg, db = hp.layer_norm_backward(x, gy, gamma)
+    x1, g1, x2, g2 = x.clone(), gy.clone(), x.clone(), gy.clone()
+    hp.layer_norm(x1, gamma, beta, out=x1)
+    _, dg1, db1 = hp.layer_norm_backward(x, g1, gamma, out=g1)
+    _, dg2, db2 = hp.layer_norm_backward(x2, gy, gamma, out=x2)
+    hp.sync()
+    assert torch.equal(x1, y) and torch.equal(g1, gx) and torch.equal(x2, gx)
+    assert torch.equal(dg, dg1) and torch.equal(db, db1) and torch.equal(dg, dg2) and torch.equal(db, db2)
+
+
+def test_side_by_side_in_one_buffer(hp):
+    """Input and output as columns of one matrix: their rows interleave in memory and share no bytes."""
+    buf = torch.randn((50, 160), device="cuda")
+    x, y = buf[:, :64], buf[:, 80:144]
+    want = hp.layer_norm(x.contiguous())
+    before = buf.clone()
+    hp.layer_norm(x, out=y)
+    hp.sync()
+    assert torch.equal(y, want) and torch.equal(buf[:, :80], before[:, :80]) and torch.equal(buf[:, 144:], before[:, 144:])
+
+
+@pytest.mark.parametrize("parts,width", [(1, 12), (2, 40), (1, 300)])
+def test_gradients_against_differences(hp, parts, width):
+    """Central differences of the 64-bit forward: their own error is below 1e-7 of the sums at a step of 1e-4 (third derivatives
+    of order one times the step squared) and 1e-10 of rounding."""
+    n = 6
+    x, gy, gamma, beta = _make(11, n, parts, width, F32, F32)
+    gx, dgamma, dbeta = hp.layer_norm_backward(x, gy, gamma)
+    hp.sync()
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(5)
+    eps = float(np.float32(EPS))
+
+    def loss(xx, gg, bb):
+        d = xx - xx.mean(-1, keepdim=True)
+        return float((((d / ((d * d).mean(-1, keepdim=True) + eps).sqrt()) * gg + bb) * gy.double()).sum())
+    at = [x.double(), gamma.double(), beta.double()]
+    _, (tx, tg, tb) = R.NormRef(x, gamma, beta, EPS).backward(gy, F32)
+    for i, (grad, tol) in enumerate(((gx, tx), (dgamma.reshape(parts, width), tg), (dbeta.reshape(parts, width), tb))):
+        for _ in range(4):
+            v = torch.randn(at[i].shape, dtype=torch.float64, device="cuda", generator=gen)
+            h = 1e-4
+            up, down = list(at), list(at)
+            up[i], down[i] = at[i] + h * v, at[i] - h * v
+            diff = (loss(*up) - loss(*down)) / (2 * h)
+            size = float((grad.double() * v).abs().sum())
+            assert abs(float((grad.double() * v).sum()) - diff) <= float((tol * v.abs()).sum()) + 1e-6 * size + 1e-6
+
+
+def test_only_one_of_the_weight_gradients(hp):
+    x, gy, gamma, _ = _make(4, 70, 3, 48, F32, F32)
+    want = hp.layer_norm_backward(x, gy, gamma)
+    norm = B.Norm(70, 3, 48, gamma, None)
+    for which in ([1], [2], []):
+        out = [torch.full_like(x, 7.0), torch.full((3, 48), 7.0, device="cuda"), torch.full((3, 48), 7.0, device="cuda")]
+        hp.prepare_layer_norm_backward(norm, x, gy, out[0], out[1] if 1 in which else None, out[2] if 2 in which else None)()
+        hp.sync()
+        for i in range(3):
+            assert torch.equal(out[i], want[i]) if i == 0 or i in which else bool((out[i] == 7.0).all())
+
+
+@pytest.mark.parametrize("width", [16, 64, 300, 1664, 8192])
+def test_the_same_result_every_time(hp, width):
+    x, gy, gamma, beta = _make(2, 700, 1, width, F32, F32)
+    first = hp.layer_norm_backward(x, gy, gamma)
+    for _ in range(3):
+        for a, b in zip(first, hp.layer_norm_backward(x, gy, gamma)):
+            assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("parts,width,p", [(26, 64, 0.1), (1, 1000, 0.0), (1, 5000, 0.2)])
+def test_captured_and_replayed(hp, parts, width, p):
+    """Forward and backward in one graph, replayed on other inputs and with the offset moved on the device."""
+    st = torch.cuda.Stream()
+    hp = HotPath([1], 4, stream=st.cuda_stream)
+    n = 90
+    x, gy, gamma, beta = _make(1, n, parts, width, F32, F32)
+    counter = torch.zeros(1, dtype=torch.int64, device="cuda")
+    drop = B.Drop(p, 42, 1000, counter) if p > 0 else None
+    norm = B.Norm(n, parts, width, gamma, beta)
+    y, gx = torch.empty_like(x), torch.empty_like(x)
+    dg, db = torch.empty_like(gamma), torch.empty_like(gamma)
+    fwd, bwd = hp.prepare_layer_norm(norm, x, y, drop), hp.prepare_layer_norm_backward(norm, x, gy, gx, dg, db, drop)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=st):
+        fwd()
+        bwd()
+    for i in range(4):
+        x.copy_(torch.randn_like(x))
+        gy.copy_(torch.randn_like(x))
+        counter.fill_(i * 3)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (y, gx, dg, db)]
+        for t in (y, gx, dg, db):
+            t.fill_(float("nan"))
+        torch.cuda.synchronize()
+        eager = B.Drop(p, 42, 1000 + i * 3) if p > 0 else None
+        want = [hp.layer_norm(x, gamma, beta, EPS, eager), *hp.layer_norm_backward(x, gy, gamma, EPS, eager)]
+        hp.sync()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b.reshape(a.shape))
+
+
+def test_many_rows_past_32_bits(hp):
+    """Offsets in values and bytes that pass 32 bits: rows of 16 values, 2^16 + 3 of them, 2^16 + 40 values apart in x."""
+    n, stride = 65539, 65576
+    x = torch.empty(n * stride, dtype=BF16, device="cuda")[:n * stride].view(n, stride)[:, 5:21]
+    x.copy_(torch.randn((n, 16), device="cuda"))
+    y = hp.layer_norm(x)
+    want = hp.layer_norm(x.contiguous())
+    gx, dg, db = hp.layer_norm_backward(x, want)
+    gx2, dg2, db2 = hp.layer_norm_backward(x.contiguous(), want)
+    hp.sync()
+    assert torch.equal(y, want) and torch.equal(gx, gx2) and torch.equal(dg, dg2) and torch.equal(db, db2)
