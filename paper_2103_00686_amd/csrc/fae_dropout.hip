@@ -61,30 +61,57 @@ struct DropArgs {
     const void *x;
     void *y;
     int64_t x_stride, y_stride;
-    int64_t n_groups; // groups of eight values in all rows
-    uint32_t per_row; // of them in a row
+    int64_t n_groups;  // groups of eight values in all rows
+    uint32_t per_row;  // of them in a row
+    uint32_t per_row_inv; // 2^21 / per_row, rounded up (for rows of fewer than DROP_TILE groups)
     uint32_t n_parts, width;
     fae_drop_args drop;
 };
 
-// A thread makes the eight numbers of a group and takes its values one after the other.
+#define DROP_UNROLL 4
+#define DROP_TILE (256 * DROP_UNROLL)
+static_assert(DROP_TILE <= 1024, "the division by rows of fewer groups is exact up to 2^11");
+
+// A workgroup takes DROP_TILE consecutive groups of eight values, a thread DROP_UNROLL of them, 256 apart, whose loads are all in
+// flight before the first number is made.  One division per workgroup finds its first row; a group's row is a small number of rows
+// on: none or one where rows are as long as the tile, else a product with per_row's inverse, exact as q < 2^11 times
+// the inverse's excess, below per_row < 2^10, stays under 2^21.
 template <typename TX, typename TY> __global__ __launch_bounds__(256) void dropout_kernel(DropArgs a)
 {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= a.n_groups)
-        return;
-    const int64_t row = i / a.per_row;
-    const uint32_t group = (uint32_t)(i - row * a.per_row);
-    const int64_t r = row / a.n_parts;
-    const int64_t at = (row - r * a.n_parts) * a.width + (int64_t)group * 8;
-    const TX *x = (const TX *)a.x + r * a.x_stride + at;
-    TY *y = (TY *)a.y + r * a.y_stride + at;
-    const fae_mask8 m = fae_philox(group, (uint32_t)row, fae_drop_offset(a.drop), a.drop.key[0], a.drop.key[1]);
-    const uint32_t left = a.width - group * 8;
+    const int64_t base = (int64_t)blockIdx.x * DROP_TILE;
+    const int64_t row0 = fae_div_small(base, a.per_row);
+    const uint32_t g0 = (uint32_t)(base - row0 * a.per_row);
+    const uint64_t offset = fae_drop_offset(a.drop);
+    uint32_t row[DROP_UNROLL], group[DROP_UNROLL];
+    int there[DROP_UNROLL];
+    TY *y[DROP_UNROLL];
+    typename fae_vec<TX, 8>::type v[DROP_UNROLL];
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-        if ((uint32_t)j < left)
-            y[j] = (TY)fae_drop1((float)x[j], m.number(j), a.drop.below, a.drop.scale);
+    for (int u = 0; u < DROP_UNROLL; ++u) {
+        const uint32_t i = u * 256 + threadIdx.x, q = g0 + i;
+        const uint32_t on = a.per_row >= DROP_TILE ? (q >= a.per_row ? 1 : 0) : (q * a.per_row_inv) >> 21;
+        group[u] = q - on * a.per_row;
+        row[u] = (uint32_t)row0 + on;
+        const int left = (int)(a.width - group[u] * 8);
+        there[u] = base + i < a.n_groups ? (left < 8 ? left : 8) : 0;
+        uint32_t r = row[u], part = 0;
+        if (a.n_parts > 1) {
+            r = row[u] / a.n_parts;
+            part = row[u] - r * a.n_parts;
+        }
+        const int64_t at = (int64_t)part * a.width + group[u] * 8;
+        y[u] = (TY *)a.y + r * a.y_stride + at;
+        v[u] = fae_load<TX, 8>((const TX *)a.x + r * a.x_stride + at, there[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < DROP_UNROLL; ++u) {
+        float o[8];
+        const fae_mask8 m = fae_philox(group[u], row[u], offset, a.drop.key[0], a.drop.key[1]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            o[j] = fae_drop1((float)v[u][j], m.number(j), a.drop.below, a.drop.scale);
+        fae_store<TY, 8>(y[u], o, there[u]);
+    }
 }
 
 static int32_t dropout_impl(fae_ctx *ctx, const char *who, const fae_drop *drop, int64_t n_rows, int32_t n_parts, int32_t width,
@@ -120,10 +147,15 @@ static int32_t dropout_impl(fae_ctx *ctx, const char *who, const fae_drop *drop,
     a.x_stride = x.stride;
     a.y_stride = y.stride;
     a.per_row = ((uint32_t)width + 7) / 8;
+    a.per_row_inv = ((1u << 21) + a.per_row - 1) / a.per_row;
     a.n_groups = n_rows * n_parts * (int64_t)a.per_row;
     a.n_parts = n_parts;
     a.width = width;
-    const int64_t blocks = (a.n_groups + 255) / 256;
+    if (x.stride == row && y.stride == row) { // the parts are rows
+        a.n_parts = 1;
+        a.x_stride = a.y_stride = width;
+    }
+    const int64_t blocks = (a.n_groups + DROP_TILE - 1) / DROP_TILE;
     if (blocks > 2147483647LL)
         return fae_fail(ctx, FAE_EINVAL, "%s: too many values for one launch", who);
     FAE_HIP(ctx, hipSetDevice(ctx->device));

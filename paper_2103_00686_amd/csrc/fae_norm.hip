@@ -27,43 +27,6 @@ struct NormArgs {
 };
 
 // ---------------------------------------------------------------------------------
-// chunks: E values, loaded and stored at once where all are there (the vector unit's accesses take any alignment of the values)
-// ---------------------------------------------------------------------------------
-template <typename T, int E> struct norm_vec {
-    typedef T type __attribute__((ext_vector_type(E)));
-    typedef type loose __attribute__((aligned(sizeof(T))));
-};
-
-template <typename T, int E> __device__ __forceinline__ typename norm_vec<T, E>::type norm_load(const T *p, int there)
-{
-    typename norm_vec<T, E>::type v;
-    if (there == E) {
-        v = *(const typename norm_vec<T, E>::loose *)p;
-    } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-            v[e] = e < there ? p[e] : (T)0.f;
-    }
-    return v;
-}
-
-template <typename T, int E> __device__ __forceinline__ void norm_store(T *p, const float (&v)[E], int there)
-{
-    typename norm_vec<T, E>::type o;
-#pragma unroll
-    for (int e = 0; e < E; ++e)
-        o[e] = (T)v[e];
-    if (there == E) {
-        *(typename norm_vec<T, E>::loose *)p = o;
-    } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (e < there)
-                p[e] = o[e];
-    }
-}
-
-// ---------------------------------------------------------------------------------
 // sums over a team, the same bits in every lane
 // ---------------------------------------------------------------------------------
 template <int CTRL> __device__ __forceinline__ float norm_dpp_add(float v)
@@ -215,8 +178,8 @@ __global__ __launch_bounds__(WAVES ? 1024 : 256) void norm_fwd_kernel(NormArgs a
     float gamma[NV][E], beta[NV][E];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-        const auto g = a.gamma ? norm_load<float, E>(a.gamma + part * a.width + at.col[j], at.there[j]) : typename norm_vec<float, E>::type(1.f);
-        const auto b = a.beta ? norm_load<float, E>(a.beta + part * a.width + at.col[j], at.there[j]) : typename norm_vec<float, E>::type(0.f);
+        const auto g = a.gamma ? fae_load<float, E>(a.gamma + part * a.width + at.col[j], at.there[j]) : typename fae_vec<float, E>::type(1.f);
+        const auto b = a.beta ? fae_load<float, E>(a.beta + part * a.width + at.col[j], at.there[j]) : typename fae_vec<float, E>::type(0.f);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             gamma[j][e] = g[e];
@@ -227,7 +190,7 @@ __global__ __launch_bounds__(WAVES ? 1024 : 256) void norm_fwd_kernel(NormArgs a
         float v[NV][E];
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const auto raw = norm_load<TX, E>(x + at.col[j], at.there[j]);
+            const auto raw = fae_load<TX, E>(x + at.col[j], at.there[j]);
 #pragma unroll
             for (int e = 0; e < E; ++e)
                 v[j][e] = (float)raw[e];
@@ -240,7 +203,7 @@ __global__ __launch_bounds__(WAVES ? 1024 : 256) void norm_fwd_kernel(NormArgs a
                 v[j][e] = v[j][e] * rstd * gamma[j][e] + beta[j][e];
             if (a.drop.below)
                 norm_drop<E>(v[j], at.col[j], (uint32_t)row, offset, a.drop);
-            norm_store<TY, E>(y + at.col[j], v[j], at.there[j]);
+            fae_store<TY, E>(y + at.col[j], v[j], at.there[j]);
         }
     }
 }
@@ -261,7 +224,7 @@ __global__ __launch_bounds__(WAVES ? 1024 : 256) void norm_bwd_kernel(NormArgs a
     float gamma[NV][E], dgamma[NV][E], dbeta[NV][E];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-        const auto g = a.gamma && at.q < a.step ? norm_load<float, E>(a.gamma + part * a.width + at.col[j], at.there[j]) : typename norm_vec<float, E>::type(1.f);
+        const auto g = a.gamma && at.q < a.step ? fae_load<float, E>(a.gamma + part * a.width + at.col[j], at.there[j]) : typename fae_vec<float, E>::type(1.f);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             gamma[j][e] = g[e];
@@ -272,8 +235,8 @@ __global__ __launch_bounds__(WAVES ? 1024 : 256) void norm_bwd_kernel(NormArgs a
         float v[NV][E], g[NV][E];
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const auto rx = norm_load<TX, E>(x + at.col[j], at.there[j]);
-            const auto rg = norm_load<TY, E>(gy + at.col[j], at.there[j]);
+            const auto rx = fae_load<TX, E>(x + at.col[j], at.there[j]);
+            const auto rg = fae_load<TY, E>(gy + at.col[j], at.there[j]);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 v[j][e] = (float)rx[e];
@@ -304,7 +267,7 @@ __global__ __launch_bounds__(WAVES ? 1024 : 256) void norm_bwd_kernel(NormArgs a
 #pragma unroll
             for (int e = 0; e < E; ++e)
                 g[j][e] = rstd * (g[j][e] - c1 - v[j][e] * c2);
-            norm_store<TX, E>(gx + at.col[j], g[j], at.there[j]);
+            fae_store<TX, E>(gx + at.col[j], g[j], at.there[j]);
         }
     }
     if (!a.pgamma && !a.pbeta)
@@ -318,9 +281,9 @@ __global__ __launch_bounds__(WAVES ? 1024 : 256) void norm_bwd_kernel(NormArgs a
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             if (a.pgamma)
-                norm_store<float, E>(a.pgamma + (int64_t)r * a.pitch + at.col[j], dgamma[j], at.there[j]);
+                fae_store<float, E>(a.pgamma + (int64_t)r * a.pitch + at.col[j], dgamma[j], at.there[j]);
             if (a.pbeta)
-                norm_store<float, E>(a.pbeta + (int64_t)r * a.pitch + at.col[j], dbeta[j], at.there[j]);
+                fae_store<float, E>(a.pbeta + (int64_t)r * a.pitch + at.col[j], dbeta[j], at.there[j]);
         }
         return;
     }

@@ -37,6 +37,43 @@ int32_t fae_check_drop(fae_ctx *ctx, const char *who, const fae_drop *drop, fae_
 #ifdef __HIPCC__
 
 // ---------------------------------------------------------------------------------
+// chunks: E values, loaded and stored at once where all are there (the vector unit's accesses take any alignment of the values)
+// ---------------------------------------------------------------------------------
+template <typename T, int E> struct fae_vec {
+    typedef T type __attribute__((ext_vector_type(E)));
+    typedef type loose __attribute__((aligned(sizeof(T))));
+};
+
+template <typename T, int E> __device__ __forceinline__ typename fae_vec<T, E>::type fae_load(const T *p, int there)
+{
+    typename fae_vec<T, E>::type v;
+    if (there == E) {
+        v = *(const typename fae_vec<T, E>::loose *)p;
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            v[e] = e < there ? p[e] : (T)0.f;
+    }
+    return v;
+}
+
+template <typename T, int E> __device__ __forceinline__ void fae_store(T *p, const float (&v)[E], int there)
+{
+    typename fae_vec<T, E>::type o;
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+        o[e] = (T)v[e];
+    if (there == E) {
+        *(typename fae_vec<T, E>::loose *)p = o;
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (e < there)
+                p[e] = o[e];
+    }
+}
+
+// ---------------------------------------------------------------------------------
 // Philox4x32-10 (Salmon, Moraes, Dror, Shaw 2011).  Its ten rounds are 20 products of 32 by 32 bits and 60 exclusive
 // ors and additions, for eight values: 16 bits each decide as well as 32 would (a share of dropped values is kept to
 // 2^-17), and half the generator's work is left out.
