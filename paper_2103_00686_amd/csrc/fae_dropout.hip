@@ -65,10 +65,13 @@ struct DropArgs {
     uint32_t per_row;  // of them in a row
     uint32_t per_row_inv; // 2^21 / per_row, rounded up (for rows of fewer than DROP_TILE groups)
     uint32_t n_parts, width;
+    int32_t ends; // how the rows end, in chunks of 16 bytes of x
     fae_drop_args drop;
 };
 
+#ifndef DROP_UNROLL
 #define DROP_UNROLL 4
+#endif
 #define DROP_TILE (256 * DROP_UNROLL)
 static_assert(DROP_TILE <= 1024, "the division by rows of fewer groups is exact up to 2^11");
 
@@ -78,39 +81,50 @@ static_assert(DROP_TILE <= 1024, "the division by rows of fewer groups is exact 
 // the inverse's excess, below per_row < 2^10, stays under 2^21.
 template <typename TX, typename TY> __global__ __launch_bounds__(256) void dropout_kernel(DropArgs a)
 {
+    constexpr int E = sizeof(TX) == 2 ? 8 : 4; // values in 16 bytes
     const int64_t base = (int64_t)blockIdx.x * DROP_TILE;
     const int64_t row0 = fae_div_small(base, a.per_row);
     const uint32_t g0 = (uint32_t)(base - row0 * a.per_row);
     const uint64_t offset = fae_drop_offset(a.drop);
     uint32_t row[DROP_UNROLL], group[DROP_UNROLL];
-    int there[DROP_UNROLL];
+    bool in[DROP_UNROLL];
     TY *y[DROP_UNROLL];
-    typename fae_vec<TX, 8>::type v[DROP_UNROLL];
+    fae_place<E> at[DROP_UNROLL][8 / E];
+    typename fae_vec<TX, E>::type v[DROP_UNROLL][8 / E];
 #pragma unroll
     for (int u = 0; u < DROP_UNROLL; ++u) {
-        const uint32_t i = u * 256 + threadIdx.x, q = g0 + i;
+        const uint32_t i = u * 256 + threadIdx.x;
+        in[u] = base + i < a.n_groups;
+        const uint32_t q = in[u] ? g0 + i : g0; // the tile's first group again past the last one
         const uint32_t on = a.per_row >= DROP_TILE ? (q >= a.per_row ? 1 : 0) : (q * a.per_row_inv) >> 21;
         group[u] = q - on * a.per_row;
         row[u] = (uint32_t)row0 + on;
-        const int left = (int)(a.width - group[u] * 8);
-        there[u] = base + i < a.n_groups ? (left < 8 ? left : 8) : 0;
         uint32_t r = row[u], part = 0;
         if (a.n_parts > 1) {
             r = row[u] / a.n_parts;
             part = row[u] - r * a.n_parts;
         }
-        const int64_t at = (int64_t)part * a.width + group[u] * 8;
-        y[u] = (TY *)a.y + r * a.y_stride + at;
-        v[u] = fae_load<TX, 8>((const TX *)a.x + r * a.x_stride + at, there[u]);
+        y[u] = (TY *)a.y + r * a.y_stride + (int64_t)part * a.width;
+        const TX *x = (const TX *)a.x + r * a.x_stride + (int64_t)part * a.width;
+#pragma unroll
+        for (int h = 0; h < 8 / E; ++h) {
+            at[u][h].set(group[u] * 8 + h * E, a.width);
+            v[u][h] = fae_load<TX, E>(x, at[u][h], a.ends);
+        }
     }
 #pragma unroll
     for (int u = 0; u < DROP_UNROLL; ++u) {
-        float o[8];
         const fae_mask8 m = fae_philox(group[u], row[u], offset, a.drop.key[0], a.drop.key[1]);
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            o[j] = fae_drop1((float)v[u][j], m.number(j), a.drop.below, a.drop.scale);
-        fae_store<TY, 8>(y[u], o, there[u]);
+        for (int h = 0; h < 8 / E; ++h) {
+            float o[E];
+            fae_settle<TX, E>(v[u][h], at[u][h], a.ends, o);
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                o[e] = fae_drop1(o[e], m.number(h * E + e), a.drop.below, a.drop.scale);
+            if (in[u])
+                fae_store<TY, E>(y[u], o, at[u][h], a.ends);
+        }
     }
 }
 
@@ -151,6 +165,7 @@ static int32_t dropout_impl(fae_ctx *ctx, const char *who, const fae_drop *drop,
     a.n_groups = n_rows * n_parts * (int64_t)a.per_row;
     a.n_parts = n_parts;
     a.width = width;
+    a.ends = fae_row_end(width, 16 / fae_type_size(x.type), a.per_row * 8LL);
     if (x.stride == row && y.stride == row) { // the parts are rows
         a.n_parts = 1;
         a.x_stride = a.y_stride = width;

@@ -1,0 +1,481 @@
+// Layer norm over rows in parts, forward and backward, with dropout as its epilogue: kernels (gfx950).
+#pragma once
+
+#include "fae_rows.h"
+
+// A row is held by a team: LANES lanes of a wave (several teams to a wave) or whole waves, each lane with NV chunks of E
+// values in registers, so that x (and gy) are read once whatever the statistics need.  `step` teams are a gang, which takes a stretch
+// of consecutive rows, its team j the rows j, j + step, j + 2 step, ... of it; step is a multiple of the parts, so a team stays with
+// one part, holds its weights in registers, and can add up their gradient over all its rows.
+struct NormArgs {
+    const void *x, *gy;
+    void *y; // forward: y, backward: gx
+    int64_t x_stride, gy_stride, y_stride;
+    int64_t x_step, gy_step, y_step; // from one of a team's rows to its next
+    const float *gamma, *beta;
+    float *pgamma, *pbeta; // backward: sums of the launch's workgroups, or the gradients themselves
+    int64_t n_rows;        // rows of all parts
+    int64_t stretch;       // of them that a gang takes, a multiple of step
+    uint32_t step;         // teams of a gang
+    int64_t gang_samples;  // samples of a stretch
+    uint32_t n_parts, width;
+    uint32_t pitch;   // of a row of sums
+    uint32_t part_rows; // rows of sums that a workgroup leaves: its teams, or the parts if these are fewer
+    int32_t direct;   // the sums are the gradients
+    int32_t ends;     // how the rows end: FAE_WHOLE ..
+    int32_t in_regs;  // a team's sums go out as they are
+    float eps, inv_width;
+    fae_drop_args drop;
+};
+
+// ---------------------------------------------------------------------------------
+// sums over a team, the same bits in every lane
+// ---------------------------------------------------------------------------------
+template <int CTRL> __device__ __forceinline__ float norm_dpp_add(float v)
+{
+    return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+template <int LANES> __device__ __forceinline__ float norm_lane_sum(float v)
+{
+    if constexpr (LANES >= 2)
+        v = norm_dpp_add<0xB1>(v); // the neighbour
+    if constexpr (LANES >= 4)
+        v = norm_dpp_add<0x4E>(v); // the other pair of four lanes
+    if constexpr (LANES >= 8)
+        v = norm_dpp_add<0x141>(v); // eight lanes mirrored: the other four
+    if constexpr (LANES >= 16)
+        v = norm_dpp_add<0x140>(v); // sixteen lanes mirrored: the other eight
+    if constexpr (LANES >= 32) {
+        const uint32_t b = __builtin_bit_cast(uint32_t, v);
+        auto r = __builtin_amdgcn_permlane16_swap(b, b, false, false); // rows 0, 0, 2, 2 and 1, 1, 3, 3 of sixteen lanes
+        const uint32_t lo = r[0], hi = r[1];
+        v = __builtin_bit_cast(float, lo) + __builtin_bit_cast(float, hi);
+    }
+    if constexpr (LANES >= 64) {
+        const uint32_t b = __builtin_bit_cast(uint32_t, v);
+        auto r = __builtin_amdgcn_permlane32_swap(b, b, false, false); // the lower half twice and the upper half twice
+        const uint32_t lo = r[0], hi = r[1];
+        v = __builtin_bit_cast(float, lo) + __builtin_bit_cast(float, hi);
+    }
+    return v;
+}
+
+// Two sums at once.  Teams of several waves (a workgroup of their own) join them in LDS, in two buffers taken in turn: one barrier per
+// call, as whoever writes a buffer again has passed the barrier behind everyone's reads of it.
+template <int LANES, bool WAVES> struct norm_team {
+    float2 (*red)[16];
+    int turn = 0;
+    __device__ __forceinline__ void sum2(float &a, float &b)
+    {
+        a = norm_lane_sum<LANES>(a);
+        b = norm_lane_sum<LANES>(b);
+        if constexpr (WAVES) {
+            const int lane = fae_lane(), w = threadIdx.x / FAE_WAVE, n = blockDim.x / FAE_WAVE;
+            if (lane == 0)
+                red[turn][w] = make_float2(a, b);
+            __syncthreads();
+            const float2 t = (lane & 15) < n ? red[turn][lane & 15] : make_float2(0.f, 0.f);
+            a = norm_lane_sum<16>(t.x);
+            b = norm_lane_sum<16>(t.y);
+            turn ^= 1;
+        }
+    }
+};
+
+// dropout of a chunk that starts at column c
+template <int E> __device__ __forceinline__ void norm_drop(float (&v)[E], uint32_t c, uint32_t row, uint64_t offset, const fae_drop_args &d)
+{
+    static_assert(E == 4 || E == 8, "half a group of eight or a whole one");
+    const fae_mask8 m = fae_philox(c >> 3, row, offset, d.key[0], d.key[1]);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const uint32_t w = E == 8 ? m.w[e >> 1] : (c & 4 ? m.w[2 + (e >> 1)] : m.w[e >> 1]);
+        v[e] = fae_drop1(v[e], e & 1 ? w >> 16 : w & 0xffffu, d.below, d.scale);
+    }
+}
+
+template <typename TX> constexpr int norm_chunk() { return sizeof(TX) == 2 ? 8 : 4; } // values in 16 bytes of x
+
+// where a thread stands
+template <int LANES, bool WAVES, int NV, int E> struct norm_place {
+    uint32_t q;      // team of the launch
+    int l;           // lane of the team
+    int lanes;       // lanes of the team
+    fae_place<E> at[NV];
+    __device__ __forceinline__ norm_place(uint32_t width)
+    {
+        if constexpr (WAVES) {
+            q = blockIdx.x;
+            l = threadIdx.x;
+            lanes = blockDim.x;
+        } else {
+            q = blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+            l = threadIdx.x % LANES;
+            lanes = LANES;
+        }
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            at[j].set((uint32_t)(j * lanes + l) * E, width);
+    }
+};
+
+// Deviations from the mean in v's place and 1 / sqrt(variance + eps).  They are taken from a first mean, whose own rounding error
+// is then their mean and goes off them too: with one number for the mean, a row far from zero beside its spread
+// would keep that error.  Columns that do not exist add nothing to
+// either sum (a choice, as the first mean may be rounded in one place and not in another).
+template <bool WHOLE, int LANES, bool WAVES, int NV, int E>
+__device__ __forceinline__ float norm_center(float (&v)[NV][E], const fae_place<E> (&at)[NV], const NormArgs &a, norm_team<LANES, WAVES> &team)
+{
+    float s = 0.f, none = 0.f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            s += v[j][e];
+    team.sum2(s, none);
+    const float m = s * a.inv_width;
+    float d1 = 0.f, d2 = 0.f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            v[j][e] = WHOLE || e < at[j].there ? v[j][e] - m : 0.f;
+            d1 += v[j][e];
+            d2 += v[j][e] * v[j][e];
+        }
+    team.sum2(d1, d2);
+    const float rest = d1 * a.inv_width;
+    const float var = d2 * a.inv_width - rest * rest;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            v[j][e] -= rest;
+    return 1.0f / sqrtf(fmaxf(var, 0.f) + a.eps);
+}
+
+// a team's first row, the end of its gang's stretch, the first row's sample; returns the part
+__device__ __forceinline__ uint32_t norm_rows_of(uint32_t q, const NormArgs &a, int64_t *row, int64_t *end, int64_t *sample)
+{
+    const uint32_t gang = q / a.step, j = q - gang * a.step, s = j / a.n_parts;
+    *row = gang * a.stretch + j;
+    *end = (gang + 1) * a.stretch < a.n_rows ? (gang + 1) * a.stretch : a.n_rows;
+    *sample = gang * a.gang_samples + s;
+    return j - s * a.n_parts;
+}
+
+// a part's gamma or beta, ones or zeros if there are none
+template <bool WHOLE, int E, int NV>
+__device__ __forceinline__ void norm_weights(const float *w, float none, const NormArgs &a, uint32_t part, const fae_place<E> (&at)[NV],
+                                             float (&out)[NV][E])
+{
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        if (!w) {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                out[j][e] = none;
+        } else if (WHOLE || a.ends == FAE_CHUNKS) {
+            const auto v = fae_load<float, E>(w + part * a.width, at[j], WHOLE ? FAE_WHOLE : FAE_CHUNKS);
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                out[j][e] = v[e];
+        } else { // columns that do not exist get the last one's
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                out[j][e] = w[part * a.width + (at[j].col + e < a.width ? at[j].col + e : a.width - 1)];
+        }
+    }
+}
+
+// A batch of U rows of a team, asked for together; rows past the end are the first one again
+template <typename T, int E, int NV, int U, bool WHOLE> struct norm_batch {
+    typename fae_vec<T, E>::type raw[U][NV];
+    __device__ __forceinline__ void load(const T *p, int64_t step, int64_t row, int64_t end, const NormArgs &a, const fae_place<E> (&at)[NV])
+    {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const T *r = U == 1 || row + (int64_t)u * a.step < end ? p + u * step : p;
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+                raw[u][j] = fae_load<T, E>(r, at[j], WHOLE ? FAE_WHOLE : a.ends);
+        }
+    }
+    __device__ __forceinline__ void get(int u, const NormArgs &a, const fae_place<E> (&at)[NV], float (&v)[NV][E]) const
+    {
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            fae_settle<T, E>(raw[u][j], at[j], WHOLE ? FAE_WHOLE : a.ends, v[j]);
+    }
+};
+
+template <typename TX, typename TY, int LANES, int THREADS, int NV, int U, bool WHOLE, bool DROP>
+__global__ __launch_bounds__(THREADS) void norm_fwd_kernel(NormArgs a)
+{
+    constexpr int E = norm_chunk<TX>();
+    constexpr bool WAVES = THREADS > 256;
+    __shared__ float2 red[2][16];
+    norm_team<LANES, WAVES> team{red};
+    const norm_place<LANES, WAVES, NV, E> at(a.width);
+    int64_t row, end, s0;
+    const uint32_t part = norm_rows_of(at.q, a, &row, &end, &s0);
+    if (row >= end)
+        return;
+    const TX *x = (const TX *)a.x + s0 * a.x_stride + part * a.width;
+    TY *y = (TY *)a.y + s0 * a.y_stride + part * a.width;
+    norm_batch<TX, E, NV, U, WHOLE> in;
+    in.load(x, a.x_step, row, end, a, at.at);
+    const uint64_t offset = DROP ? fae_drop_offset(a.drop) : 0;
+    float gamma[NV][E], beta[NV][E];
+    norm_weights<WHOLE, E, NV>(a.gamma, 1.f, a, part, at.at, gamma);
+    norm_weights<WHOLE, E, NV>(a.beta, 0.f, a, part, at.at, beta);
+    while (row < end) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (U > 1 && row + (int64_t)u * a.step >= end)
+                break;
+            float v[NV][E];
+            in.get(u, a, at.at, v);
+            const float rstd = norm_center<WHOLE, LANES, WAVES, NV, E>(v, at.at, a, team);
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    v[j][e] = v[j][e] * rstd * gamma[j][e] + beta[j][e];
+                if constexpr (DROP)
+                    norm_drop<E>(v[j], at.at[j].col, (uint32_t)(row + (int64_t)u * a.step), offset, a.drop);
+                fae_store<TY, E>(y + u * a.y_step, v[j], at.at[j], WHOLE ? FAE_WHOLE : a.ends);
+            }
+        }
+        row += (int64_t)U * a.step;
+        x += U * a.x_step;
+        y += U * a.y_step;
+        if (row < end)
+            in.load(x, a.x_step, row, end, a, at.at);
+    }
+}
+
+// The rows' gradient, and the team's sums of the weights' gradients in registers over all its rows.  The next batch's loads go out
+// before the present one's sums are taken.
+template <typename TX, typename TY, int LANES, int THREADS, int NV, int U, bool PRE, bool WHOLE, bool DROP>
+__global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
+{
+    constexpr int E = norm_chunk<TX>();
+    constexpr bool WAVES = THREADS > 256;
+    __shared__ float2 red[2][16];
+    norm_team<LANES, WAVES> team{red};
+    const norm_place<LANES, WAVES, NV, E> at(a.width);
+    int64_t row, end, s0;
+    const uint32_t part = norm_rows_of(at.q, a, &row, &end, &s0);
+    const TX *x = (const TX *)a.x + s0 * a.x_stride + part * a.width;
+    const TY *gy = (const TY *)a.gy + s0 * a.gy_stride + part * a.width;
+    TX *gx = (TX *)a.y + s0 * a.y_stride + part * a.width;
+    const int64_t row0 = row;
+    norm_batch<TX, E, NV, U, WHOLE> inx;
+    norm_batch<TY, E, NV, U, WHOLE> ing;
+    if (row < end) {
+        inx.load(x, a.x_step, row, end, a, at.at);
+        ing.load(gy, a.gy_step, row, end, a, at.at);
+    }
+    const uint64_t offset = DROP ? fae_drop_offset(a.drop) : 0;
+    float gamma[NV][E], dgamma[NV][E], dbeta[NV][E];
+    norm_weights<WHOLE, E, NV>(a.gamma, 1.f, a, part, at.at, gamma);
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            dgamma[j][e] = dbeta[j][e] = 0.f;
+    while (row < end) {
+        const int64_t next = row + (int64_t)U * a.step;
+        norm_batch<TX, E, NV, U, WHOLE> nextx;
+        norm_batch<TY, E, NV, U, WHOLE> nextg;
+        if (PRE && next < end) {
+            nextx.load(x + U * a.x_step, a.x_step, next, end, a, at.at);
+            nextg.load(gy + U * a.gy_step, a.gy_step, next, end, a, at.at);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (U > 1 && row + (int64_t)u * a.step >= end)
+                break;
+            float v[NV][E], g[NV][E];
+            inx.get(u, a, at.at, v);
+            ing.get(u, a, at.at, g);
+            const float rstd = norm_center<WHOLE, LANES, WAVES, NV, E>(v, at.at, a, team);
+            float c1 = 0.f, c2 = 0.f;
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                if constexpr (DROP)
+                    norm_drop<E>(g[j], at.at[j].col, (uint32_t)(row + (int64_t)u * a.step), offset, a.drop);
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    v[j][e] *= rstd; // h
+                    dbeta[j][e] += g[j][e];
+                    dgamma[j][e] += g[j][e] * v[j][e];
+                    g[j][e] *= gamma[j][e]; // a
+                    c1 += g[j][e];
+                    c2 += g[j][e] * v[j][e];
+                }
+            }
+            team.sum2(c1, c2);
+            c1 *= a.inv_width;
+            c2 *= a.inv_width;
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    g[j][e] = rstd * (g[j][e] - c1 - v[j][e] * c2);
+                fae_store<TX, E>(gx + u * a.y_step, g[j], at.at[j], WHOLE ? FAE_WHOLE : a.ends);
+            }
+        }
+        row = next;
+        x += U * a.x_step;
+        gy += U * a.gy_step;
+        gx += U * a.y_step;
+        if constexpr (PRE) {
+            inx = nextx;
+            ing = nextg;
+        } else if (row < end) {
+            inx.load(x, a.x_step, row, end, a, at.at);
+            ing.load(gy, a.gy_step, row, end, a, at.at);
+        }
+    }
+    if (!a.pgamma && !a.pbeta)
+        return;
+    // The sums go out a row per team, or where a workgroup has more teams than there are parts a row per part, the teams of a part
+    // added up in LDS.
+    if (a.in_regs) {
+        const uint32_t r = a.direct ? part : at.q;
+        if (a.direct && row0 >= end)
+            return;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            if (a.pgamma)
+                fae_store<float, E>(a.pgamma + (int64_t)r * a.pitch, dgamma[j], at.at[j], WHOLE ? FAE_WHOLE : a.ends);
+            if (a.pbeta)
+                fae_store<float, E>(a.pbeta + (int64_t)r * a.pitch, dbeta[j], at.at[j], WHOLE ? FAE_WHOLE : a.ends);
+        }
+        return;
+    }
+    if constexpr (!WAVES) {
+        constexpr int TEAMS = 256 / LANES, ROW = LANES * NV * E;
+        __shared__ float sums[TEAMS * ROW];
+        for (int which = 0; which < 2; ++which) {
+            float *out = which ? a.pbeta : a.pgamma;
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    sums[threadIdx.x / LANES * ROW + at.at[j].col + e] = which ? dbeta[j][e] : dgamma[j][e];
+            __syncthreads();
+            if (!out)
+                continue;
+            const uint32_t n = a.part_rows * a.width;
+            for (uint32_t i = threadIdx.x; i < n; i += 256) {
+                const uint32_t k = i / a.width, c = i - k * a.width;
+                float s = 0.f;
+                for (uint32_t t = k; t < TEAMS; t += a.n_parts)
+                    s += sums[t * ROW + c];
+                out[(int64_t)(blockIdx.x * a.part_rows + k) * a.pitch + c] = s;
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------------
+// rows that a lane has in flight: about 64 bytes of x
+#ifndef FWD_U
+#define FWD_U(NV) (NV == 1 ? 4 : NV == 2 ? 2 : 1)
+#endif
+#ifndef BWD_U
+#define BWD_U(NV) (NV == 1 ? 2 : 1)
+#endif
+#ifndef BWD_PRE
+#define BWD_PRE(NV, THREADS) (THREADS == 256)
+#endif
+#ifndef PER_LANE
+#define PER_LANE 16
+#endif
+constexpr int norm_per_lane(bool bwd) { return bwd ? PER_LANE : 16; } // values per lane at most
+#ifndef GANG
+#define GANG 1
+#endif
+#ifndef PER_TEAM
+#define PER_TEAM 8
+#endif
+#ifndef MOST_THREADS
+#define MOST_THREADS (256 * 1024)
+#endif
+// how a launch shares out the rows
+struct NormShape {
+    int chunk;      // values per chunk
+    int lanes;      // per team: 1 .. 64, or 64 times the waves
+    int nv;         // chunks per lane
+    uint32_t teams; // per workgroup
+    uint32_t threads;
+    uint32_t blocks, step;
+    int64_t iters;      // rows of a team
+    bool direct;        // backward: the only rows of sums are the gradients
+    uint32_t part_rows; // backward: rows of sums per workgroup
+    uint32_t n_sums;    // backward: rows of sums per part
+    uint32_t pitch;
+};
+
+template <bool BWD, typename TX, typename TY, int LANES, int THREADS, int NV, bool WHOLE, bool DROP>
+static void norm_launch(fae_ctx *ctx, const NormShape &s, const NormArgs &a)
+{
+    if constexpr (BWD)
+        FAE_LAUNCH(ctx, (norm_bwd_kernel<TX, TY, LANES, THREADS, NV, BWD_U(NV), BWD_PRE(NV, THREADS), WHOLE, DROP>), dim3(s.blocks), dim3(s.threads), 0,
+                   ctx->stream, a);
+    else
+        FAE_LAUNCH(ctx, (norm_fwd_kernel<TX, TY, LANES, THREADS, NV, FWD_U(NV), WHOLE, DROP>), dim3(s.blocks), dim3(s.threads), 0, ctx->stream, a);
+}
+
+template <bool BWD, typename TX, typename TY, int LANES, int THREADS, int NV> static void norm_run(fae_ctx *ctx, const NormShape &s, const NormArgs &a)
+{
+    if (a.ends == FAE_WHOLE && a.drop.below)
+        norm_launch<BWD, TX, TY, LANES, THREADS, NV, true, true>(ctx, s, a);
+    else if (a.ends == FAE_WHOLE)
+        norm_launch<BWD, TX, TY, LANES, THREADS, NV, true, false>(ctx, s, a);
+    else if (a.drop.below)
+        norm_launch<BWD, TX, TY, LANES, THREADS, NV, false, true>(ctx, s, a);
+    else
+        norm_launch<BWD, TX, TY, LANES, THREADS, NV, false, false>(ctx, s, a);
+}
+
+template <bool BWD, typename TX, typename TY> static void norm_by_width(fae_ctx *ctx, const NormShape &s, const NormArgs &a)
+{
+    constexpr int MOST = norm_per_lane(BWD) / norm_chunk<TX>();
+    switch (s.lanes) {
+    case 2: norm_run<BWD, TX, TY, 2, 256, 1>(ctx, s, a); return;
+    case 4: norm_run<BWD, TX, TY, 4, 256, 1>(ctx, s, a); return;
+    case 8: norm_run<BWD, TX, TY, 8, 256, 1>(ctx, s, a); return;
+    case 16: norm_run<BWD, TX, TY, 16, 256, 1>(ctx, s, a); return;
+    case 32: norm_run<BWD, TX, TY, 32, 256, 1>(ctx, s, a); return;
+    case 64: break;
+    default:
+        if (s.lanes <= 512)
+            norm_run<BWD, TX, TY, 64, 512, MOST>(ctx, s, a);
+        else
+            norm_run<BWD, TX, TY, 64, 1024, MOST>(ctx, s, a);
+        return;
+    }
+    if (s.nv == 1) {
+        norm_run<BWD, TX, TY, 64, 256, 1>(ctx, s, a);
+        return;
+    }
+    if constexpr (MOST >= 2)
+        if (s.nv == 2)
+            norm_run<BWD, TX, TY, 64, 256, 2>(ctx, s, a);
+    if constexpr (MOST >= 4)
+        if (s.nv == 4)
+            norm_run<BWD, TX, TY, 64, 256, 4>(ctx, s, a);
+}
+
+// fae_norm_fwd.hip, fae_norm_bwd.hip
+void norm_fwd_by_type(fae_ctx *ctx, const fae_norm *n, const NormShape &s, const NormArgs &a);
+void norm_bwd_by_type(fae_ctx *ctx, const fae_norm *n, const NormShape &s, const NormArgs &a);
+void norm_bwd16_by_type(fae_ctx *ctx, const fae_norm *n, const NormShape &s, const NormArgs &a);
+void norm_fwd16_by_type(fae_ctx *ctx, const fae_norm *n, const NormShape &s, const NormArgs &a);

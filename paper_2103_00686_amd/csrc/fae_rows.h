@@ -44,31 +44,90 @@ template <typename T, int E> struct fae_vec {
     typedef type loose __attribute__((aligned(sizeof(T))));
 };
 
-template <typename T, int E> __device__ __forceinline__ typename fae_vec<T, E>::type fae_load(const T *p, int there)
+template <typename T, int E> __device__ __forceinline__ typename fae_vec<T, E>::type fae_load(const T *p)
 {
-    typename fae_vec<T, E>::type v;
-    if (there == E) {
-        v = *(const typename fae_vec<T, E>::loose *)p;
-    } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-            v[e] = e < there ? p[e] : (T)0.f;
-    }
-    return v;
+    return *(const typename fae_vec<T, E>::loose *)p;
 }
 
-template <typename T, int E> __device__ __forceinline__ void fae_store(T *p, const float (&v)[E], int there)
+// Where a lane's chunk of E values lies in a row of `width`.  Loads have no branch per lane or value (a load behind one waits for the
+// loads in front of it): a chunk that the row's end cuts is loaded as the E values that end with the row and moved down when they
+// are there, and lanes behind the row load that chunk too.  Rows shorter than a chunk are the exception.
+template <int E> struct fae_place {
+    uint32_t col;  // the chunk's first column
+    uint32_t from; // the first column that is loaded
+    int there;     // values of the chunk that exist, 0 .. E
+    __device__ __forceinline__ void set(uint32_t c, uint32_t width)
+    {
+        col = c;
+        there = c >= width ? 0 : (width - c < (uint32_t)E ? (int)(width - c) : E);
+        const uint32_t last = width < (uint32_t)E ? 0 : width - E;
+        from = c < last ? c : last;
+    }
+};
+// how a launch's rows end
+enum { FAE_WHOLE, FAE_CHUNKS, FAE_CROOKED, FAE_SHORT }; // every lane's chunk whole; some absent; one cut; no whole chunk at all
+static inline int32_t fae_row_end(int64_t width, int chunk, int64_t lanes_width)
 {
+    return width == lanes_width ? FAE_WHOLE : (width < chunk ? FAE_SHORT : (width % chunk ? FAE_CROOKED : FAE_CHUNKS));
+}
+template <typename T, int E> __device__ __forceinline__ typename fae_vec<T, E>::type fae_load(const T *row, const fae_place<E> &at, int ends)
+{
+    if (ends == FAE_SHORT) {
+        typename fae_vec<T, E>::type v;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            v[e] = e < at.there ? row[e] : (T)0.f;
+        return v;
+    }
+    const T *p = row + (ends == FAE_WHOLE ? at.col : at.from);
+#ifdef NTL
+    return __builtin_nontemporal_load((const typename fae_vec<T, E>::loose *)p);
+#else
+    return *(const typename fae_vec<T, E>::loose *)p;
+#endif
+}
+// what fae_load brought, as it belongs: zeros where the row has no values
+template <typename T, int E>
+__device__ __forceinline__ void fae_settle(typename fae_vec<T, E>::type v, const fae_place<E> &at, int ends, float (&out)[E])
+{
+    if (ends == FAE_CROOKED && at.there > 0) {
+        const uint32_t sh = (at.col - at.from) * 8 * sizeof(T);
+        if constexpr (sizeof(v) == 8) {
+            v = __builtin_bit_cast(typename fae_vec<T, E>::type, __builtin_bit_cast(uint64_t, v) >> sh);
+        } else {
+            static_assert(sizeof(v) == 16, "8 or 16 bytes");
+            typedef uint64_t pair __attribute__((ext_vector_type(2)));
+            pair w = __builtin_bit_cast(pair, v);
+            const uint64_t lo = w[0], hi = w[1];
+            const uint32_t s = sh & 63;
+            const uint64_t h = hi >> s, l = (lo >> s) | ((hi << 1) << (63 - s));
+            w[0] = sh < 64 ? l : h;
+            w[1] = sh < 64 ? h : 0;
+            v = __builtin_bit_cast(typename fae_vec<T, E>::type, w);
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+        out[e] = ends == FAE_WHOLE || e < at.there ? (float)v[e] : 0.f;
+}
+
+template <typename T, int E> __device__ __forceinline__ void fae_store(T *row, const float (&v)[E], const fae_place<E> &at, int ends)
+{
+    T *p = row + at.col;
     typename fae_vec<T, E>::type o;
 #pragma unroll
     for (int e = 0; e < E; ++e)
         o[e] = (T)v[e];
-    if (there == E) {
+    if (ends == FAE_WHOLE || at.there == E) {
+#ifdef NTS
+        __builtin_nontemporal_store(o, (typename fae_vec<T, E>::loose *)p);
+#else
         *(typename fae_vec<T, E>::loose *)p = o;
+#endif
     } else {
 #pragma unroll
         for (int e = 0; e < E; ++e)
-            if (e < there)
+            if (e < at.there)
                 p[e] = o[e];
     }
 }
