@@ -82,16 +82,50 @@ template <int LANES, bool WAVES> struct norm_team {
     }
 };
 
-// dropout of a chunk that starts at column c
-template <int E> __device__ __forceinline__ void norm_drop(float (&v)[E], uint32_t c, uint32_t row, uint64_t offset, const fae_drop_args &d)
-{
-    static_assert(E == 4 || E == 8, "half a group of eight or a whole one");
-    const fae_mask8 m = fae_philox(c >> 3, row, offset, d.key[0], d.key[1]);
+// The numbers of a chunk's E values, two to a word
+template <int E> struct norm_mask {
+    uint32_t w[E / 2];
+    __device__ __forceinline__ void drop(float (&v)[E], const fae_drop_args &d) const
+    {
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-        const uint32_t w = E == 8 ? m.w[e >> 1] : (c & 4 ? m.w[2 + (e >> 1)] : m.w[e >> 1]);
-        v[e] = fae_drop1(v[e], e & 1 ? w >> 16 : w & 0xffffu, d.below, d.scale);
+        for (int e = 0; e < E; ++e)
+            v[e] = fae_drop1(v[e], e & 1 ? w[e >> 1] >> 16 : w[e >> 1] & 0xffffu, d.below, d.scale);
     }
+};
+// Two chunks' numbers (chunks of four or eight that start at columns ca and cb).  A chunk of four is half a group of eight, whose
+// other half a neighbouring lane has: each of the two makes one of the two groups whole and hands over what it does
+// not need itself.
+template <int E>
+__device__ __forceinline__ void norm_masks(norm_mask<E> &a, norm_mask<E> &b, uint32_t ca, uint32_t ra, uint32_t cb, uint32_t rb, uint64_t offset,
+                                           const fae_drop_args &d)
+{
+    if constexpr (E == 8) {
+        const fae_mask8 ma = fae_philox(ca >> 3, ra, offset, d.key[0], d.key[1]), mb = fae_philox(cb >> 3, rb, offset, d.key[0], d.key[1]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            a.w[i] = ma.w[i];
+            b.w[i] = mb.w[i];
+        }
+    } else {
+        static_assert(E == 4, "half a group of eight or a whole one");
+        const bool odd = threadIdx.x & 1; // a team's lanes are even in number: the neighbour is of the same team
+        const fae_mask8 m = fae_philox((odd ? cb : ca) >> 3, odd ? rb : ra, offset, d.key[0], d.key[1]);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t give = odd ? m.w[i] : m.w[2 + i];
+            const uint32_t got = __builtin_amdgcn_update_dpp(0, give, 0xB1, 0xf, 0xf, true);
+            a.w[i] = odd ? got : m.w[i];
+            b.w[i] = odd ? m.w[2 + i] : got;
+        }
+    }
+}
+// all chunks of a row where a lane has two and more
+template <int E, int NV>
+__device__ __forceinline__ void norm_row_masks(norm_mask<E> (&m)[NV], const fae_place<E> (&at)[NV], uint32_t row, uint64_t offset, const fae_drop_args &d)
+{
+#pragma unroll
+    for (int j = 0; j + 1 < NV; j += 2)
+        norm_masks<E>(m[j], m[j + 1], at[j].col, row, at[j + 1].col, row, offset, d);
 }
 
 template <typename TX> constexpr int norm_chunk() { return sizeof(TX) == 2 ? 8 : 4; } // values in 16 bytes of x
@@ -229,11 +263,19 @@ __global__ __launch_bounds__(THREADS) void norm_fwd_kernel(NormArgs a)
     float gamma[NV][E], beta[NV][E];
     norm_weights<WHOLE, E, NV>(a.gamma, 1.f, a, part, at.at, gamma);
     norm_weights<WHOLE, E, NV>(a.beta, 0.f, a, part, at.at, beta);
+    norm_mask<E> mask[2][NV]; // of two rows where a lane has one chunk
     while (row < end) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (U > 1 && row + (int64_t)u * a.step >= end)
                 break;
+            if constexpr (DROP) {
+                const uint32_t r = (uint32_t)(row + (int64_t)u * a.step);
+                if constexpr (NV > 1)
+                    norm_row_masks<E, NV>(mask[u & 1], at.at, r, offset, a.drop);
+                else if (u % 2 == 0)
+                    norm_masks<E>(mask[0][0], mask[1][0], at.at[0].col, r, at.at[0].col, r + a.step, offset, a.drop);
+            }
             float v[NV][E];
             in.get(u, a, at.at, v);
             const float rstd = norm_center<WHOLE, LANES, WAVES, NV, E>(v, at.at, a, team);
@@ -243,7 +285,7 @@ __global__ __launch_bounds__(THREADS) void norm_fwd_kernel(NormArgs a)
                 for (int e = 0; e < E; ++e)
                     v[j][e] = v[j][e] * rstd * gamma[j][e] + beta[j][e];
                 if constexpr (DROP)
-                    norm_drop<E>(v[j], at.at[j].col, (uint32_t)(row + (int64_t)u * a.step), offset, a.drop);
+                    mask[u & 1][j].drop(v[j], a.drop);
                 fae_store<TY, E>(y + u * a.y_step, v[j], at.at[j], WHOLE ? FAE_WHOLE : a.ends);
             }
         }
@@ -255,9 +297,10 @@ __global__ __launch_bounds__(THREADS) void norm_fwd_kernel(NormArgs a)
     }
 }
 
-// The rows' gradient, and the team's sums of the weights' gradients in registers over all its rows.  The next batch's loads go out
-// before the present one's sums are taken.
-template <typename TX, typename TY, int LANES, int THREADS, int NV, int U, bool PRE, bool WHOLE, bool DROP>
+// The rows' gradient, and the team's sums of the weights' gradients in registers over all its rows.  DEPTH rows of a team are held:
+// the loads of the next DEPTH - 1 go out before the present one's sums are taken (into registers of their own, with no
+// copies between them, which would wait for the loads).
+template <typename TX, typename TY, int LANES, int THREADS, int NV, int DEPTH, bool WHOLE, bool DROP>
 __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
 {
     constexpr int E = norm_chunk<TX>();
@@ -271,11 +314,18 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
     const TY *gy = (const TY *)a.gy + s0 * a.gy_stride + part * a.width;
     TX *gx = (TX *)a.y + s0 * a.y_stride + part * a.width;
     const int64_t row0 = row;
-    norm_batch<TX, E, NV, U, WHOLE> inx;
-    norm_batch<TY, E, NV, U, WHOLE> ing;
+    norm_batch<TX, E, NV, 1, WHOLE> inx[DEPTH];
+    norm_batch<TY, E, NV, 1, WHOLE> ing[DEPTH];
+    // row `ahead` from the present one, or that one again if the team has no such row
+    auto load = [&](int k, int ahead) {
+        const int64_t n = row + (int64_t)ahead * a.step < end ? ahead : 0;
+        inx[k].load(x + n * a.x_step, 0, row, end, a, at.at);
+        ing[k].load(gy + n * a.gy_step, 0, row, end, a, at.at);
+    };
     if (row < end) {
-        inx.load(x, a.x_step, row, end, a, at.at);
-        ing.load(gy, a.gy_step, row, end, a, at.at);
+#pragma unroll
+        for (int k = 0; k < DEPTH - 1; ++k)
+            load(k, k);
     }
     const uint64_t offset = DROP ? fae_drop_offset(a.drop) : 0;
     float gamma[NV][E], dgamma[NV][E], dbeta[NV][E];
@@ -285,27 +335,27 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
 #pragma unroll
         for (int e = 0; e < E; ++e)
             dgamma[j][e] = dbeta[j][e] = 0.f;
+    static_assert(DEPTH % 2 == 0, "rows whose masks are made together");
+    norm_mask<E> mask[2][NV]; // of two rows where a lane has one chunk
     while (row < end) {
-        const int64_t next = row + (int64_t)U * a.step;
-        norm_batch<TX, E, NV, U, WHOLE> nextx;
-        norm_batch<TY, E, NV, U, WHOLE> nextg;
-        if (PRE && next < end) {
-            nextx.load(x + U * a.x_step, a.x_step, next, end, a, at.at);
-            nextg.load(gy + U * a.gy_step, a.gy_step, next, end, a, at.at);
-        }
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (U > 1 && row + (int64_t)u * a.step >= end)
-                break;
+        for (int k = 0; k < DEPTH; ++k) {
+            load((k + DEPTH - 1) % DEPTH, DEPTH - 1);
+            if constexpr (DROP) {
+                if constexpr (NV > 1)
+                    norm_row_masks<E, NV>(mask[k & 1], at.at, (uint32_t)row, offset, a.drop);
+                else if (k % 2 == 0)
+                    norm_masks<E>(mask[0][0], mask[1][0], at.at[0].col, (uint32_t)row, at.at[0].col, (uint32_t)row + a.step, offset, a.drop);
+            }
             float v[NV][E], g[NV][E];
-            inx.get(u, a, at.at, v);
-            ing.get(u, a, at.at, g);
+            inx[k].get(0, a, at.at, v);
+            ing[k].get(0, a, at.at, g);
             const float rstd = norm_center<WHOLE, LANES, WAVES, NV, E>(v, at.at, a, team);
             float c1 = 0.f, c2 = 0.f;
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
                 if constexpr (DROP)
-                    norm_drop<E>(g[j], at.at[j].col, (uint32_t)(row + (int64_t)u * a.step), offset, a.drop);
+                    mask[k & 1][j].drop(g[j], a.drop);
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
                     v[j][e] *= rstd; // h
@@ -324,19 +374,14 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
 #pragma unroll
                 for (int e = 0; e < E; ++e)
                     g[j][e] = rstd * (g[j][e] - c1 - v[j][e] * c2);
-                fae_store<TX, E>(gx + u * a.y_step, g[j], at.at[j], WHOLE ? FAE_WHOLE : a.ends);
+                fae_store<TX, E>(gx, g[j], at.at[j], WHOLE ? FAE_WHOLE : a.ends);
             }
-        }
-        row = next;
-        x += U * a.x_step;
-        gy += U * a.gy_step;
-        gx += U * a.y_step;
-        if constexpr (PRE) {
-            inx = nextx;
-            ing = nextg;
-        } else if (row < end) {
-            inx.load(x, a.x_step, row, end, a, at.at);
-            ing.load(gy, a.gy_step, row, end, a, at.at);
+            row += a.step;
+            if (row >= end)
+                break;
+            x += a.x_step;
+            gy += a.gy_step;
+            gx += a.y_step;
         }
     }
     if (!a.pgamma && !a.pbeta)
@@ -389,11 +434,8 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
 #ifndef FWD_U
 #define FWD_U(NV) (NV == 1 ? 4 : NV == 2 ? 2 : 1)
 #endif
-#ifndef BWD_U
-#define BWD_U(NV) (NV == 1 ? 2 : 1)
-#endif
-#ifndef BWD_PRE
-#define BWD_PRE(NV, THREADS) (THREADS == 256)
+#ifndef BWD_DEPTH
+#define BWD_DEPTH(NV, THREADS) 2
 #endif
 #ifndef PER_LANE
 #define PER_LANE 16
@@ -427,7 +469,7 @@ template <bool BWD, typename TX, typename TY, int LANES, int THREADS, int NV, bo
 static void norm_launch(fae_ctx *ctx, const NormShape &s, const NormArgs &a)
 {
     if constexpr (BWD)
-        FAE_LAUNCH(ctx, (norm_bwd_kernel<TX, TY, LANES, THREADS, NV, BWD_U(NV), BWD_PRE(NV, THREADS), WHOLE, DROP>), dim3(s.blocks), dim3(s.threads), 0,
+        FAE_LAUNCH(ctx, (norm_bwd_kernel<TX, TY, LANES, THREADS, NV, BWD_DEPTH(NV, THREADS), WHOLE, DROP>), dim3(s.blocks), dim3(s.threads), 0,
                    ctx->stream, a);
     else
         FAE_LAUNCH(ctx, (norm_fwd_kernel<TX, TY, LANES, THREADS, NV, FWD_U(NV), WHOLE, DROP>), dim3(s.blocks), dim3(s.threads), 0, ctx->stream, a);

@@ -144,15 +144,17 @@ struct fae_mask8 {
 
 __device__ __forceinline__ uint64_t fae_drop_offset(const fae_drop_args &d) { return d.offset + (d.d_offset ? *d.d_offset : 0); }
 
+__device__ __forceinline__ uint32_t fae_xor3(uint32_t a, uint32_t b, uint32_t c) { return __builtin_amdgcn_bitop3_b32(a, b, c, 0x96); }
+
 __device__ __forceinline__ fae_mask8 fae_philox(uint32_t group, uint32_t row, uint64_t offset, uint32_t k0, uint32_t k1)
 {
     uint32_t c0 = group, c1 = row, c2 = (uint32_t)offset, c3 = (uint32_t)(offset >> 32);
 #pragma unroll
     for (int r = 0; r < 10; ++r) {
         const uint64_t a = (uint64_t)c0 * 0xD2511F53u, b = (uint64_t)c2 * 0xCD9E8D57u;
-        c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
+        c0 = fae_xor3((uint32_t)(b >> 32), c1, k0);
         c1 = (uint32_t)b;
-        c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+        c2 = fae_xor3((uint32_t)(a >> 32), c3, k1);
         c3 = (uint32_t)a;
         k0 += 0x9E3779B9u;
         k1 += 0xBB67AE85u;
