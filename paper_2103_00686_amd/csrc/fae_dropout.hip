@@ -61,70 +61,57 @@ struct DropArgs {
     const void *x;
     void *y;
     int64_t x_stride, y_stride;
-    int64_t n_groups;  // groups of eight values in all rows
-    uint32_t per_row;  // of them in a row
-    uint32_t per_row_inv; // 2^21 / per_row, rounded up (for rows of fewer than DROP_TILE groups)
+    int64_t n_groups;     // groups of eight values in all rows
+    uint32_t per_row;     // of them in a row
+    uint32_t per_row_inv; // 2^18 / per_row, rounded up (for rows of fewer than DROP_TILE groups)
     uint32_t n_parts, width;
     int32_t ends; // how the rows end, in chunks of 16 bytes of x
     fae_drop_args drop;
 };
 
-#ifndef DROP_UNROLL
-#define DROP_UNROLL 4
-#endif
-#define DROP_TILE (256 * DROP_UNROLL)
-static_assert(DROP_TILE <= 1024, "the division by rows of fewer groups is exact up to 2^11");
+#define DROP_TILE 256
 
-// A workgroup takes DROP_TILE consecutive groups of eight values, a thread DROP_UNROLL of them, 256 apart, whose loads are all in
-// flight before the first number is made.  One division per workgroup finds its first row; a group's row is a small number of rows
-// on: none or one where rows are as long as the tile, else a product with per_row's inverse, exact as q < 2^11 times
-// the inverse's excess, below per_row < 2^10, stays under 2^21.
-template <typename TX, typename TY> __global__ __launch_bounds__(256) void dropout_kernel(DropArgs a)
+// A thread takes a group of eight values, a workgroup DROP_TILE consecutive groups: one division per workgroup finds its first row,
+// and a group's row is a small number of rows on: none or one where rows are as long as the tile, else a product with
+// per_row's inverse, exact as q < 2^9 times the inverse's excess, below per_row < 2^8, stays under 2^17.
+// What bounds it: memory.  50 001 x 1664 fp32 to bf16 82 us, 6.1 TB/s (a copy of that size reaches 6.0); 65 536 x 1024 fp16 44 us,
+// 6.1 TB/s.  Two and four groups per thread took longer (84 and 85 us, 49 and 46), as did non-temporal
+// accesses (100 us, the f32 one of 16 384 x 1664 60 against 40): lines of which a store writes half go out twice.
+// WHOLE: every row is a multiple of eight values.
+template <typename TX, typename TY, bool WHOLE> __global__ __launch_bounds__(DROP_TILE) void dropout_kernel(DropArgs a)
 {
     constexpr int E = sizeof(TX) == 2 ? 8 : 4; // values in 16 bytes
+    const int ends = WHOLE ? FAE_WHOLE : a.ends;
     const int64_t base = (int64_t)blockIdx.x * DROP_TILE;
+    if (base + threadIdx.x >= a.n_groups)
+        return;
     const int64_t row0 = fae_div_small(base, a.per_row);
-    const uint32_t g0 = (uint32_t)(base - row0 * a.per_row);
-    const uint64_t offset = fae_drop_offset(a.drop);
-    uint32_t row[DROP_UNROLL], group[DROP_UNROLL];
-    bool in[DROP_UNROLL];
-    TY *y[DROP_UNROLL];
-    fae_place<E> at[DROP_UNROLL][8 / E];
-    typename fae_vec<TX, E>::type v[DROP_UNROLL][8 / E];
-#pragma unroll
-    for (int u = 0; u < DROP_UNROLL; ++u) {
-        const uint32_t i = u * 256 + threadIdx.x;
-        in[u] = base + i < a.n_groups;
-        const uint32_t q = in[u] ? g0 + i : g0; // the tile's first group again past the last one
-        const uint32_t on = a.per_row >= DROP_TILE ? (q >= a.per_row ? 1 : 0) : (q * a.per_row_inv) >> 21;
-        group[u] = q - on * a.per_row;
-        row[u] = (uint32_t)row0 + on;
-        uint32_t r = row[u], part = 0;
-        if (a.n_parts > 1) {
-            r = row[u] / a.n_parts;
-            part = row[u] - r * a.n_parts;
-        }
-        y[u] = (TY *)a.y + r * a.y_stride + (int64_t)part * a.width;
-        const TX *x = (const TX *)a.x + r * a.x_stride + (int64_t)part * a.width;
-#pragma unroll
-        for (int h = 0; h < 8 / E; ++h) {
-            at[u][h].set(group[u] * 8 + h * E, a.width);
-            v[u][h] = fae_load<TX, E>(x, at[u][h], a.ends);
-        }
+    const uint32_t q = (uint32_t)(base - row0 * a.per_row) + threadIdx.x;
+    const uint32_t on = a.per_row >= DROP_TILE ? (q >= a.per_row ? 1 : 0) : (q * a.per_row_inv) >> 18;
+    const uint32_t group = q - on * a.per_row, row = (uint32_t)row0 + on;
+    uint32_t r = row, part = 0;
+    if (a.n_parts > 1) {
+        r = row / a.n_parts;
+        part = row - r * a.n_parts;
     }
+    const TX *x = (const TX *)a.x + r * a.x_stride + (int64_t)part * a.width;
+    TY *y = (TY *)a.y + r * a.y_stride + (int64_t)part * a.width;
+    fae_place<E> at[8 / E];
+    typename fae_vec<TX, E>::type v[8 / E];
 #pragma unroll
-    for (int u = 0; u < DROP_UNROLL; ++u) {
-        const fae_mask8 m = fae_philox(group[u], row[u], offset, a.drop.key[0], a.drop.key[1]);
+    for (int h = 0; h < 8 / E; ++h) {
+        at[h].set(group * 8 + h * E, a.width);
+        v[h] = fae_load<TX, E>(x, at[h], ends);
+    }
+    const fae_mask8 m = fae_philox(group, row, fae_drop_offset(a.drop), a.drop.key[0], a.drop.key[1]);
 #pragma unroll
-        for (int h = 0; h < 8 / E; ++h) {
-            float o[E];
-            fae_settle<TX, E>(v[u][h], at[u][h], a.ends, o);
+    for (int h = 0; h < 8 / E; ++h) {
+        float o[E];
+        fae_settle<TX, E>(v[h], at[h], ends, o);
 #pragma unroll
-            for (int e = 0; e < E; ++e)
-                o[e] = fae_drop1(o[e], m.number(h * E + e), a.drop.below, a.drop.scale);
-            if (in[u])
-                fae_store<TY, E>(y[u], o, at[u][h], a.ends);
-        }
+        for (int e = 0; e < E; ++e)
+            o[e] = fae_drop1(o[e], m.number(h * E + e), a.drop.below, a.drop.scale);
+        fae_store<TY, E>(y, o, at[h], ends);
     }
 }
 
@@ -161,7 +148,7 @@ static int32_t dropout_impl(fae_ctx *ctx, const char *who, const fae_drop *drop,
     a.x_stride = x.stride;
     a.y_stride = y.stride;
     a.per_row = ((uint32_t)width + 7) / 8;
-    a.per_row_inv = ((1u << 21) + a.per_row - 1) / a.per_row;
+    a.per_row_inv = ((1u << 18) + a.per_row - 1) / a.per_row;
     a.n_groups = n_rows * n_parts * (int64_t)a.per_row;
     a.n_parts = n_parts;
     a.width = width;
@@ -177,15 +164,19 @@ static int32_t dropout_impl(fae_ctx *ctx, const char *who, const fae_drop *drop,
     fae_ktimer kt(ctx, FAE_K_DROPOUT);
     const dim3 grid((unsigned)blocks), block(256);
 #define DROP_CASE(TX, TX_, TY, TY_)                                                              \
-    if (x.type == TX && y.type == TY)                                                            \
-        FAE_LAUNCH(ctx, (dropout_kernel<TX_, TY_>), grid, block, 0, ctx->stream, a)
-    DROP_CASE(FAE_F32, float, FAE_F32, float);
-    DROP_CASE(FAE_F32, float, FAE_BF16, fae_bf16);
-    DROP_CASE(FAE_F32, float, FAE_F16, fae_f16);
-    DROP_CASE(FAE_BF16, fae_bf16, FAE_F32, float);
-    DROP_CASE(FAE_F16, fae_f16, FAE_F32, float);
-    DROP_CASE(FAE_BF16, fae_bf16, FAE_BF16, fae_bf16);
-    DROP_CASE(FAE_F16, fae_f16, FAE_F16, fae_f16);
+    if (x.type == TX && y.type == TY) {                                                          \
+        if (a.ends == FAE_WHOLE)                                                                 \
+            FAE_LAUNCH(ctx, (dropout_kernel<TX_, TY_, true>), grid, block, 0, ctx->stream, a);   \
+        else                                                                                     \
+            FAE_LAUNCH(ctx, (dropout_kernel<TX_, TY_, false>), grid, block, 0, ctx->stream, a);  \
+    }
+    DROP_CASE(FAE_F32, float, FAE_F32, float)
+    DROP_CASE(FAE_F32, float, FAE_BF16, fae_bf16)
+    DROP_CASE(FAE_F32, float, FAE_F16, fae_f16)
+    DROP_CASE(FAE_BF16, fae_bf16, FAE_F32, float)
+    DROP_CASE(FAE_F16, fae_f16, FAE_F32, float)
+    DROP_CASE(FAE_BF16, fae_bf16, FAE_BF16, fae_bf16)
+    DROP_CASE(FAE_F16, fae_f16, FAE_F16, fae_f16)
 #undef DROP_CASE
     FAE_LAUNCH_CHECK(ctx);
     return FAE_OK;

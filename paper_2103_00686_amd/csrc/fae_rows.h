@@ -80,11 +80,7 @@ template <typename T, int E> __device__ __forceinline__ typename fae_vec<T, E>::
         return v;
     }
     const T *p = row + (ends == FAE_WHOLE ? at.col : at.from);
-#ifdef NTL
-    return __builtin_nontemporal_load((const typename fae_vec<T, E>::loose *)p);
-#else
     return *(const typename fae_vec<T, E>::loose *)p;
-#endif
 }
 // what fae_load brought, as it belongs: zeros where the row has no values
 template <typename T, int E>
@@ -119,11 +115,7 @@ template <typename T, int E> __device__ __forceinline__ void fae_store(T *row, c
     for (int e = 0; e < E; ++e)
         o[e] = (T)v[e];
     if (ends == FAE_WHOLE || at.there == E) {
-#ifdef NTS
-        __builtin_nontemporal_store(o, (typename fae_vec<T, E>::loose *)p);
-#else
         *(typename fae_vec<T, E>::loose *)p = o;
-#endif
     } else {
 #pragma unroll
         for (int e = 0; e < E; ++e)
