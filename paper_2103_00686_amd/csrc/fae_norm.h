@@ -4,9 +4,9 @@
 #include "fae_rows.h"
 
 // A row is held by a team: LANES lanes of a wave (several teams to a wave) or whole waves, each lane with NV chunks of E
-// values in registers, so that x (and gy) are read once whatever the statistics need.  `step` teams are a gang, which takes a stretch
-// of consecutive rows, its team j the rows j, j + step, j + 2 step, ... of it; step is a multiple of the parts, so a team stays with
-// one part, holds its weights in registers, and can add up their gradient over all its rows.
+// values in registers, so that x (and gy) are read once whatever the statistics need.  Team q of a launch takes the rows q, q + step,
+// q + 2 step, ...; step, the number of teams, is a multiple of the parts, so a team stays with one part, holds its weights in
+// registers, and can add up their gradient over all its rows.
 struct NormArgs {
     const void *x, *gy;
     void *y; // forward: y, backward: gx
@@ -14,10 +14,8 @@ struct NormArgs {
     int64_t x_step, gy_step, y_step; // from one of a team's rows to its next
     const float *gamma, *beta;
     float *pgamma, *pbeta; // backward: sums of the launch's workgroups, or the gradients themselves
-    int64_t n_rows;        // rows of all parts
-    int64_t stretch;       // of them that a gang takes, a multiple of step
-    uint32_t step;         // teams of a gang
-    int64_t gang_samples;  // samples of a stretch
+    int64_t n_rows;   // rows of all parts
+    uint32_t step;    // teams
     uint32_t n_parts, width;
     uint32_t pitch;   // of a row of sums
     uint32_t part_rows; // rows of sums that a workgroup leaves: its teams, or the parts if these are fewer
@@ -188,16 +186,6 @@ __device__ __forceinline__ float norm_center(float (&v)[NV][E], const fae_place<
     return 1.0f / sqrtf(fmaxf(var, 0.f) + a.eps);
 }
 
-// a team's first row, the end of its gang's stretch, the first row's sample; returns the part
-__device__ __forceinline__ uint32_t norm_rows_of(uint32_t q, const NormArgs &a, int64_t *row, int64_t *end, int64_t *sample)
-{
-    const uint32_t gang = q / a.step, j = q - gang * a.step, s = j / a.n_parts;
-    *row = gang * a.stretch + j;
-    *end = (gang + 1) * a.stretch < a.n_rows ? (gang + 1) * a.stretch : a.n_rows;
-    *sample = gang * a.gang_samples + s;
-    return j - s * a.n_parts;
-}
-
 // a part's gamma or beta, ones or zeros if there are none
 template <bool WHOLE, int E, int NV>
 __device__ __forceinline__ void norm_weights(const float *w, float none, const NormArgs &a, uint32_t part, const fae_place<E> (&at)[NV],
@@ -251,10 +239,11 @@ __global__ __launch_bounds__(THREADS) void norm_fwd_kernel(NormArgs a)
     __shared__ float2 red[2][16];
     norm_team<LANES, WAVES> team{red};
     const norm_place<LANES, WAVES, NV, E> at(a.width);
-    int64_t row, end, s0;
-    const uint32_t part = norm_rows_of(at.q, a, &row, &end, &s0);
-    if (row >= end)
+    if (at.q >= a.step || at.q >= a.n_rows)
         return;
+    const uint32_t s0 = at.q / a.n_parts, part = at.q - s0 * a.n_parts;
+    const int64_t end = a.n_rows;
+    int64_t row = at.q;
     const TX *x = (const TX *)a.x + s0 * a.x_stride + part * a.width;
     TY *y = (TY *)a.y + s0 * a.y_stride + part * a.width;
     norm_batch<TX, E, NV, U, WHOLE> in;
@@ -308,12 +297,12 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
     __shared__ float2 red[2][16];
     norm_team<LANES, WAVES> team{red};
     const norm_place<LANES, WAVES, NV, E> at(a.width);
-    int64_t row, end, s0;
-    const uint32_t part = norm_rows_of(at.q, a, &row, &end, &s0);
+    const uint32_t s0 = at.q / a.n_parts, part = at.q - s0 * a.n_parts;
+    const int64_t end = a.n_rows;
+    int64_t row = at.q < a.step ? (int64_t)at.q : end;
     const TX *x = (const TX *)a.x + s0 * a.x_stride + part * a.width;
     const TY *gy = (const TY *)a.gy + s0 * a.gy_stride + part * a.width;
     TX *gx = (TX *)a.y + s0 * a.y_stride + part * a.width;
-    const int64_t row0 = row;
     norm_batch<TX, E, NV, 1, WHOLE> inx[DEPTH];
     norm_batch<TY, E, NV, 1, WHOLE> ing[DEPTH];
     // row `ahead` from the present one, or that one again if the team has no such row
@@ -335,7 +324,7 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
 #pragma unroll
         for (int e = 0; e < E; ++e)
             dgamma[j][e] = dbeta[j][e] = 0.f;
-    static_assert(DEPTH % 2 == 0, "rows whose masks are made together");
+    static_assert(NV > 1 || DEPTH % 2 == 0, "rows whose masks are made together");
     norm_mask<E> mask[2][NV]; // of two rows where a lane has one chunk
     while (row < end) {
 #pragma unroll
@@ -390,7 +379,7 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
     // added up in LDS.
     if (a.in_regs) {
         const uint32_t r = a.direct ? part : at.q;
-        if (a.direct && row0 >= end)
+        if (a.direct && at.q >= a.step)
             return;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
@@ -403,7 +392,7 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
     }
     if constexpr (!WAVES) {
         constexpr int TEAMS = 256 / LANES, ROW = LANES * NV * E;
-        __shared__ float sums[TEAMS * ROW];
+        __shared__ float sums[TEAMS * ROW], pieces[256];
         for (int which = 0; which < 2; ++which) {
             float *out = which ? a.pbeta : a.pgamma;
             __syncthreads();
@@ -415,13 +404,27 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
             __syncthreads();
             if (!out)
                 continue;
-            const uint32_t n = a.part_rows * a.width;
-            for (uint32_t i = threadIdx.x; i < n; i += 256) {
-                const uint32_t k = i / a.width, c = i - k * a.width;
+            // several threads to an output where there are fewer of these than threads
+            const uint32_t n = a.part_rows * a.width, split = n < 256 ? 256 / n : 1;
+            for (uint32_t i = threadIdx.x; i < n * split; i += 256) {
+                const uint32_t piece = i / n, o = i - piece * n, k = o / a.width, c = o - k * a.width;
                 float s = 0.f;
-                for (uint32_t t = k; t < TEAMS; t += a.n_parts)
+                for (uint32_t t = k + piece * a.n_parts; t < TEAMS; t += split * a.n_parts)
                     s += sums[t * ROW + c];
-                out[(int64_t)(blockIdx.x * a.part_rows + k) * a.pitch + c] = s;
+                if (split == 1)
+                    out[(int64_t)(blockIdx.x * a.part_rows + k) * a.pitch + c] = s;
+                else
+                    pieces[i] = s;
+            }
+            if (split == 1)
+                continue;
+            __syncthreads();
+            if (threadIdx.x < n) {
+                float s = pieces[threadIdx.x];
+                for (uint32_t q = 1; q < split; ++q)
+                    s += pieces[threadIdx.x + q * n];
+                const uint32_t k = threadIdx.x / a.width;
+                out[(int64_t)(blockIdx.x * a.part_rows + k) * a.pitch + threadIdx.x - k * a.width] = s;
             }
         }
     }
@@ -430,26 +433,16 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
 // ---------------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------------
-// rows that a lane has in flight: about 64 bytes of x
-#ifndef FWD_U
-#define FWD_U(NV) (NV == 1 ? 4 : NV == 2 ? 2 : 1)
-#endif
-#ifndef BWD_DEPTH
-#define BWD_DEPTH(NV, THREADS) 2
-#endif
-#ifndef PER_LANE
-#define PER_LANE 16
-#endif
-constexpr int norm_per_lane(bool bwd) { return bwd ? PER_LANE : 16; } // values per lane at most
-#ifndef GANG
-#define GANG 1
-#endif
-#ifndef PER_TEAM
-#define PER_TEAM 8
-#endif
-#ifndef MOST_THREADS
-#define MOST_THREADS (256 * 1024)
-#endif
+// rows of a team whose loads go out together
+constexpr int norm_fwd_rows(int nv) { return nv == 1 ? 4 : nv == 2 ? 2 : 1; }
+// rows of a team that are held in the backward: two, four where a lane has little else to do beside the generator, one where a
+// workgroup of 1024 has no registers for more
+constexpr int norm_bwd_depth(int nv, int chunk, int threads, bool drop) { return threads == 1024 && nv * chunk > 8 ? 1 : nv == 1 && drop ? 4 : 2; }
+
+// chunks per lane at most, where a workgroup of 1024 then holds the row: two in the backward, whose sums and weights take six times
+// their registers; 16 values in the forward
+constexpr int norm_chunks(bool bwd, int chunk) { return bwd ? 2 : 16 / chunk; }
+
 // how a launch shares out the rows
 struct NormShape {
     int chunk;      // values per chunk
@@ -458,7 +451,6 @@ struct NormShape {
     uint32_t teams; // per workgroup
     uint32_t threads;
     uint32_t blocks, step;
-    int64_t iters;      // rows of a team
     bool direct;        // backward: the only rows of sums are the gradients
     uint32_t part_rows; // backward: rows of sums per workgroup
     uint32_t n_sums;    // backward: rows of sums per part
@@ -469,10 +461,10 @@ template <bool BWD, typename TX, typename TY, int LANES, int THREADS, int NV, bo
 static void norm_launch(fae_ctx *ctx, const NormShape &s, const NormArgs &a)
 {
     if constexpr (BWD)
-        FAE_LAUNCH(ctx, (norm_bwd_kernel<TX, TY, LANES, THREADS, NV, BWD_DEPTH(NV, THREADS), WHOLE, DROP>), dim3(s.blocks), dim3(s.threads), 0,
+        FAE_LAUNCH(ctx, (norm_bwd_kernel<TX, TY, LANES, THREADS, NV, norm_bwd_depth(NV, norm_chunk<TX>(), THREADS, DROP), WHOLE, DROP>), dim3(s.blocks), dim3(s.threads), 0,
                    ctx->stream, a);
     else
-        FAE_LAUNCH(ctx, (norm_fwd_kernel<TX, TY, LANES, THREADS, NV, FWD_U(NV), WHOLE, DROP>), dim3(s.blocks), dim3(s.threads), 0, ctx->stream, a);
+        FAE_LAUNCH(ctx, (norm_fwd_kernel<TX, TY, LANES, THREADS, NV, norm_fwd_rows(NV), WHOLE, DROP>), dim3(s.blocks), dim3(s.threads), 0, ctx->stream, a);
 }
 
 template <bool BWD, typename TX, typename TY, int LANES, int THREADS, int NV> static void norm_run(fae_ctx *ctx, const NormShape &s, const NormArgs &a)
@@ -489,7 +481,7 @@ template <bool BWD, typename TX, typename TY, int LANES, int THREADS, int NV> st
 
 template <bool BWD, typename TX, typename TY> static void norm_by_width(fae_ctx *ctx, const NormShape &s, const NormArgs &a)
 {
-    constexpr int MOST = norm_per_lane(BWD) / norm_chunk<TX>();
+    constexpr int MOST = norm_chunks(BWD, norm_chunk<TX>()), ALL = FAE_NORM_MAX_WIDTH / norm_chunk<TX>() / 1024; // per lane
     switch (s.lanes) {
     case 2: norm_run<BWD, TX, TY, 2, 256, 1>(ctx, s, a); return;
     case 4: norm_run<BWD, TX, TY, 4, 256, 1>(ctx, s, a); return;
@@ -500,17 +492,18 @@ template <bool BWD, typename TX, typename TY> static void norm_by_width(fae_ctx 
     default:
         if (s.lanes <= 512)
             norm_run<BWD, TX, TY, 64, 512, MOST>(ctx, s, a);
-        else
+        else if (s.nv == MOST)
             norm_run<BWD, TX, TY, 64, 1024, MOST>(ctx, s, a);
+        else if constexpr (ALL > MOST)
+            norm_run<BWD, TX, TY, 64, 1024, ALL>(ctx, s, a);
         return;
     }
     if (s.nv == 1) {
         norm_run<BWD, TX, TY, 64, 256, 1>(ctx, s, a);
         return;
     }
-    if constexpr (MOST >= 2)
-        if (s.nv == 2)
-            norm_run<BWD, TX, TY, 64, 256, 2>(ctx, s, a);
+    if (s.nv == 2)
+        norm_run<BWD, TX, TY, 64, 256, 2>(ctx, s, a);
     if constexpr (MOST >= 4)
         if (s.nv == 4)
             norm_run<BWD, TX, TY, 64, 256, 4>(ctx, s, a);

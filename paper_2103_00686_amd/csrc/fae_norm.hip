@@ -3,7 +3,7 @@
 
 #include "fae_norm.h"
 
-// dgamma (z = 0) and dbeta (z = 1) of a part from its rows of sums: sixteen lanes of four columns, 64 rows at a time.
+// dgamma (z = 0) and dbeta (z = 1) of a part from its rows of sums: L lanes of four columns each, 256 / L rows of sums at a time.
 struct NormWeightArgs {
     const float *sums[2];
     float *out[2];
@@ -11,19 +11,24 @@ struct NormWeightArgs {
     uint32_t n_sums;  // rows of sums of a part
     uint32_t teams;   // of a workgroup if it left a row per part, 0 if it left one per team
 };
-__global__ __launch_bounds__(1024) void norm_weights_kernel(NormWeightArgs a)
+// From this many columns on, workgroups of 64 columns are enough for the chip and read whole lines; below, of 16 (64 and 16 columns,
+// us of a whole backward: 512 x 8192 bf16 16.2 and 17.2, 4096 x 16384 bf16 96.7 and 101, 16384 x 8192 bf16 147 and 150;
+// 6007 x 4 x 100 fp32 16.0 and 15.3, 400 000 x 64 fp32 59.5 and 58.8).
+#define NORM_WIDE_SUMS 4096
+template <int L, int THREADS> __global__ __launch_bounds__(THREADS) void norm_weights_kernel(NormWeightArgs a)
 {
-    __shared__ float4 part_sum[64][16];
+    constexpr int ROWS = THREADS / L;
+    __shared__ float4 part_sum[ROWS][L];
     const float *sums = a.sums[blockIdx.z];
-    const uint32_t p = blockIdx.y, l = threadIdx.x % 16, g = threadIdx.x / 16, c = blockIdx.x * 64 + l * 4;
+    const uint32_t p = blockIdx.y, l = threadIdx.x % L, g = threadIdx.x / L, c = (blockIdx.x * L + l) * 4;
     if (!a.out[blockIdx.z])
         return;
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
     if (c < a.pitch) {
 #pragma unroll 4
-        for (uint32_t t = g; t < a.n_sums; t += 64) {
+        for (uint32_t t = g; t < a.n_sums; t += ROWS) {
             // workgroup t's first team has part t * teams modulo the parts
-            const uint32_t k = a.teams ? (p + a.n_parts - (uint32_t)((uint64_t)t * a.teams % a.n_parts)) % a.n_parts : p;
+            const uint32_t k = a.teams ? (p + a.n_parts - t * a.teams % a.n_parts) % a.n_parts : p;
             const float4 v = *(const float4 *)(sums + ((int64_t)t * a.n_parts + k) * a.pitch + c);
             s.x += v.x;
             s.y += v.y;
@@ -32,7 +37,7 @@ __global__ __launch_bounds__(1024) void norm_weights_kernel(NormWeightArgs a)
         }
     }
     part_sum[g][l] = s;
-    for (int half = 32; half > 0; half >>= 1) {
+    for (int half = ROWS / 2; half > 0; half >>= 1) {
         __syncthreads();
         if ((int)g < half) {
             const float4 v = part_sum[g + half][l];
@@ -59,12 +64,14 @@ static NormShape norm_shape(const fae_norm *n, bool bwd)
     NormShape s;
     memset(&s, 0, sizeof(s));
     s.chunk = fae_type_size(n->x_type) == 2 ? 8 : 4;
-    const int chunks = (n->width + s.chunk - 1) / s.chunk, most = norm_per_lane(bwd) / s.chunk;
+    const int chunks = (n->width + s.chunk - 1) / s.chunk, most = norm_chunks(bwd, s.chunk);
     s.nv = 1;
     s.lanes = 2;
     while (s.lanes < 64 && s.lanes < chunks)
         s.lanes *= 2;
     while (s.nv < most && s.nv * 64 < chunks)
+        s.nv *= 2;
+    if (s.nv * 1024 < chunks)
         s.nv *= 2;
     if (s.nv * 64 < chunks)
         s.lanes = 64 * ((chunks + 64 * s.nv - 1) / (64 * s.nv));
@@ -73,31 +80,26 @@ static NormShape norm_shape(const fae_norm *n, bool bwd)
     const int64_t rows = n->n_rows * n->n_parts;
     const uint32_t parts = n->n_parts, whole = parts / norm_gcd(parts, s.teams); // workgroups whose teams are a multiple of the parts
     s.pitch = (n->width + 3) / 4 * 4;
-    const int64_t per_team = bwd ? PER_TEAM : FWD_U(s.nv);
-    int64_t blocks = (rows + per_team * s.teams - 1) / (per_team * s.teams);
     s.part_rows = s.teams > parts ? parts : s.teams;
-    bool capped = false;
-    if (bwd) {
-        const int64_t most_blocks = MOST_THREADS / s.threads;
-        if (blocks > most_blocks) {
-            blocks = most_blocks;
-            capped = true;
-        }
-        s.direct = blocks * s.teams <= parts || blocks == 1;
-    }
-    if (s.direct) {
+        // Rows of a team at least.  Backward: fewer where a workgroup adds up its teams' sums before it writes them (2 and 4, us: 717 x 16
+    // 6.5 and 7.0; 8 instead of 4 where it does not: 4096 x 1664 bf16 27.9 against 22.3, 512 x 8192 bf16 22.0 against 17.2).
+    const int64_t per_team = bwd ? (s.teams > parts ? 2 : 4) : norm_fwd_rows(s.nv);
+    int64_t blocks = (rows + per_team * s.teams - 1) / (per_team * s.teams);
+    const int64_t most_blocks = bwd ? (s.threads > 512 ? 256 : 128 * 1024 / s.threads) : blocks;
+    if (bwd && (blocks * s.teams <= parts || blocks == 1)) {
+        s.direct = true;
         s.step = parts * (s.teams > parts ? s.teams / parts : 1);
         s.blocks = (s.step + s.teams - 1) / s.teams;
-        s.iters = (rows + s.step - 1) / s.step;
         s.n_sums = 1;
         return s;
     }
-    const uint32_t gang = GANG * whole;
-    const int64_t gangs = capped && blocks >= gang ? blocks / gang : (blocks + gang - 1) / gang;
-    s.step = gang * s.teams;
-    s.iters = (rows + gangs * s.step - 1) / (gangs * s.step);
-    s.blocks = (uint32_t)(gangs * gang);
-    s.n_sums = s.teams > parts ? s.blocks : s.blocks * s.teams / parts;
+    if (blocks > most_blocks)
+        blocks = most_blocks >= whole ? most_blocks / whole * whole : whole;
+    else
+        blocks = (blocks + whole - 1) / whole * whole;
+    s.blocks = (uint32_t)blocks;
+    s.step = s.blocks * s.teams;
+    s.n_sums = s.teams > parts ? s.blocks : s.step / parts;
     return s;
 }
 
@@ -108,8 +110,6 @@ static void norm_place_rows(const NormShape &s, NormArgs *a)
     a->gy_step = samples * a->gy_stride;
     a->y_step = samples * a->y_stride;
     a->step = s.step;
-    a->stretch = s.iters * s.step;
-    a->gang_samples = s.iters * samples;
     a->ends = fae_row_end(a->width, s.chunk, (int64_t)s.lanes * s.nv * s.chunk);
 }
 
@@ -264,7 +264,10 @@ extern "C" int32_t fae_layer_norm_bwd(fae_ctx *ctx, const fae_norm *norm, const 
     }
     if (!s.direct && (dgamma || dbeta)) {
         fae_ktimer kt(ctx, FAE_K_NORM_WEIGHTS);
-        FAE_LAUNCH(ctx, norm_weights_kernel, dim3((s.pitch + 63) / 64, a.n_parts, 2), dim3(1024), 0, ctx->stream, w);
+        if ((int64_t)a.n_parts * s.pitch >= NORM_WIDE_SUMS)
+            FAE_LAUNCH(ctx, (norm_weights_kernel<16, 1024>), dim3((s.pitch + 63) / 64, a.n_parts, 2), dim3(1024), 0, ctx->stream, w);
+        else
+            FAE_LAUNCH(ctx, (norm_weights_kernel<4, 256>), dim3((s.pitch + 15) / 16, a.n_parts, 2), dim3(256), 0, ctx->stream, w);
         FAE_LAUNCH_CHECK(ctx);
     }
     return FAE_OK;
