@@ -355,6 +355,23 @@ class HotPath:
         B.fae_dropout_bwd(self.ctx, drop, gy, out)
         return out
 
+    # -- a step with them: pooled forward -> norm -> dropout, and back to the hot tables ----
+    def forward_norm(self, hb: HotBatch, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None,
+                     eps: float = 1e-5, drop: Optional[B.Drop] = None, out_dtype: torch.dtype = torch.float32,
+                     pooling: int = B.FAE_POOL_SUM):
+        """(pooled, y): the pooled rows of every table and their layer norm, dropped out, as the dense layers read it.
+        gamma and beta: [tables, dim].  ``backward_norm_sgd`` takes pooled."""
+        pooled = self.forward(hb, pooling=pooling)
+        return pooled, self.layer_norm(pooled, gamma, beta, eps, drop, out_dtype)
+
+    def backward_norm_sgd(self, hb: HotBatch, pooled: torch.Tensor, gy: torch.Tensor, lr: float,
+                          gamma: Optional[torch.Tensor] = None, eps: float = 1e-5, drop: Optional[B.Drop] = None):
+        """From y's gradient to the hot tables (sum pooling, SGD), with the forward's gamma, eps and drop; returns
+        (dgamma, dbeta).  pooled is overwritten with its gradient."""
+        _, dgamma, dbeta = self.layer_norm_backward(pooled, gy, gamma, eps, drop, out=pooled)
+        self.backward_sgd(hb, pooled, lr)
+        return dgamma, dbeta
+
     # pre-marshalled forms of the four, for tight loops: zero-argument callables
     def prepare_layer_norm(self, norm: B.Norm, x: torch.Tensor, y: torch.Tensor, drop: Optional[B.Drop] = None):
         return B.prepare_layer_norm_fwd(self.ctx, norm, x, y, drop)
