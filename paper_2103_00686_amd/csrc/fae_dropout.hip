@@ -77,11 +77,10 @@ struct DropArgs {
 // What bounds it: memory.  50 001 x 1664 fp32 to bf16 82 us, 6.1 TB/s (a copy of that size reaches 6.0); 65 536 x 1024 fp16 44 us,
 // 6.1 TB/s.  Two and four groups per thread took longer (84 and 85 us, 49 and 46), as did non-temporal
 // accesses (100 us, the f32 one of 16 384 x 1664 60 against 40): lines of which a store writes half go out twice.
-// WHOLE: every row is a multiple of eight values.
-template <typename TX, typename TY, bool WHOLE> __global__ __launch_bounds__(DROP_TILE) void dropout_kernel(DropArgs a)
+// ENDS: FAE_WHOLE where every row is a multiple of eight values.
+template <typename TX, typename TY, int ENDS> __global__ __launch_bounds__(DROP_TILE) void dropout_kernel(DropArgs a)
 {
     constexpr int E = sizeof(TX) == 2 ? 8 : 4; // values in 16 bytes
-    const int ends = WHOLE ? FAE_WHOLE : a.ends;
     const int64_t base = (int64_t)blockIdx.x * DROP_TILE;
     if (base + threadIdx.x >= a.n_groups)
         return;
@@ -101,17 +100,17 @@ template <typename TX, typename TY, bool WHOLE> __global__ __launch_bounds__(DRO
 #pragma unroll
     for (int h = 0; h < 8 / E; ++h) {
         at[h].set(group * 8 + h * E, a.width);
-        v[h] = fae_load<TX, E>(x, at[h], ends);
+        v[h] = fae_load<TX, E, ENDS>(x, at[h], a.ends);
     }
     const fae_mask8 m = fae_philox(group, row, fae_drop_offset(a.drop), a.drop.key[0], a.drop.key[1]);
 #pragma unroll
     for (int h = 0; h < 8 / E; ++h) {
         float o[E];
-        fae_settle<TX, E>(v[h], at[h], ends, o);
+        fae_settle<TX, E, ENDS>(v[h], at[h], a.ends, o);
 #pragma unroll
         for (int e = 0; e < E; ++e)
             o[e] = fae_drop1(o[e], m.number(h * E + e), a.drop.below, a.drop.scale);
-        fae_store<TY, E>(y, o, at[h], ends);
+        fae_store<TY, E, ENDS>(y, o, at[h]);
     }
 }
 
@@ -166,9 +165,9 @@ static int32_t dropout_impl(fae_ctx *ctx, const char *who, const fae_drop *drop,
 #define DROP_CASE(TX, TX_, TY, TY_)                                                              \
     if (x.type == TX && y.type == TY) {                                                          \
         if (a.ends == FAE_WHOLE)                                                                 \
-            FAE_LAUNCH(ctx, (dropout_kernel<TX_, TY_, true>), grid, block, 0, ctx->stream, a);   \
+            FAE_LAUNCH(ctx, (dropout_kernel<TX_, TY_, FAE_WHOLE>), grid, block, 0, ctx->stream, a);   \
         else                                                                                     \
-            FAE_LAUNCH(ctx, (dropout_kernel<TX_, TY_, false>), grid, block, 0, ctx->stream, a);  \
+            FAE_LAUNCH(ctx, (dropout_kernel<TX_, TY_, FAE_ANY>), grid, block, 0, ctx->stream, a);  \
     }
     DROP_CASE(FAE_F32, float, FAE_F32, float)
     DROP_CASE(FAE_F32, float, FAE_BF16, fae_bf16)

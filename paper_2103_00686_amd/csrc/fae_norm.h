@@ -155,7 +155,7 @@ template <int LANES, bool WAVES, int NV, int E> struct norm_place {
 // is then their mean and goes off them too: with one number for the mean, a row far from zero beside its spread
 // would keep that error.  Columns that do not exist add nothing to
 // either sum (a choice, as the first mean may be rounded in one place and not in another).
-template <bool WHOLE, int LANES, bool WAVES, int NV, int E>
+template <int ENDS, int LANES, bool WAVES, int NV, int E>
 __device__ __forceinline__ float norm_center(float (&v)[NV][E], const fae_place<E> (&at)[NV], const NormArgs &a, norm_team<LANES, WAVES> &team)
 {
     float s = 0.f, none = 0.f;
@@ -171,7 +171,10 @@ __device__ __forceinline__ float norm_center(float (&v)[NV][E], const fae_place<
     for (int j = 0; j < NV; ++j)
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            v[j][e] = WHOLE || e < at[j].there ? v[j][e] - m : 0.f;
+            if constexpr (ENDS == FAE_ANY)
+                v[j][e] = e < at[j].there ? v[j][e] - m : 0.f;
+            else
+                v[j][e] -= ENDS == FAE_WHOLE || at[j].there > 0 ? m : 0.f; // an absent chunk's values are zeros
             d1 += v[j][e];
             d2 += v[j][e] * v[j][e];
         }
@@ -187,7 +190,7 @@ __device__ __forceinline__ float norm_center(float (&v)[NV][E], const fae_place<
 }
 
 // a part's gamma or beta, ones or zeros if there are none
-template <bool WHOLE, int E, int NV>
+template <int ENDS, int E, int NV>
 __device__ __forceinline__ void norm_weights(const float *w, float none, const NormArgs &a, uint32_t part, const fae_place<E> (&at)[NV],
                                              float (&out)[NV][E])
 {
@@ -197,8 +200,8 @@ __device__ __forceinline__ void norm_weights(const float *w, float none, const N
 #pragma unroll
             for (int e = 0; e < E; ++e)
                 out[j][e] = none;
-        } else if (WHOLE || a.ends == FAE_CHUNKS) {
-            const auto v = fae_load<float, E>(w + part * a.width, at[j], WHOLE ? FAE_WHOLE : FAE_CHUNKS);
+        } else if constexpr (ENDS != FAE_ANY) {
+            const auto v = fae_load<float, E, ENDS>(w + part * a.width, at[j], a.ends);
 #pragma unroll
             for (int e = 0; e < E; ++e)
                 out[j][e] = v[e];
@@ -211,7 +214,7 @@ __device__ __forceinline__ void norm_weights(const float *w, float none, const N
 }
 
 // A batch of U rows of a team, asked for together; rows past the end are the first one again
-template <typename T, int E, int NV, int U, bool WHOLE> struct norm_batch {
+template <typename T, int E, int NV, int U, int ENDS, bool MAY_SHORT> struct norm_batch {
     typename fae_vec<T, E>::type raw[U][NV];
     __device__ __forceinline__ void load(const T *p, int64_t step, int64_t row, int64_t end, const NormArgs &a, const fae_place<E> (&at)[NV])
     {
@@ -220,18 +223,18 @@ template <typename T, int E, int NV, int U, bool WHOLE> struct norm_batch {
             const T *r = U == 1 || row + (int64_t)u * a.step < end ? p + u * step : p;
 #pragma unroll
             for (int j = 0; j < NV; ++j)
-                raw[u][j] = fae_load<T, E>(r, at[j], WHOLE ? FAE_WHOLE : a.ends);
+                raw[u][j] = fae_load<T, E, ENDS, MAY_SHORT>(r, at[j], a.ends);
         }
     }
     __device__ __forceinline__ void get(int u, const NormArgs &a, const fae_place<E> (&at)[NV], float (&v)[NV][E]) const
     {
 #pragma unroll
         for (int j = 0; j < NV; ++j)
-            fae_settle<T, E>(raw[u][j], at[j], WHOLE ? FAE_WHOLE : a.ends, v[j]);
+            fae_settle<T, E, ENDS>(raw[u][j], at[j], a.ends, v[j]);
     }
 };
 
-template <typename TX, typename TY, int LANES, int THREADS, int NV, int U, bool WHOLE, bool DROP>
+template <typename TX, typename TY, int LANES, int THREADS, int NV, int U, int ENDS, bool DROP>
 __global__ __launch_bounds__(THREADS) void norm_fwd_kernel(NormArgs a)
 {
     constexpr int E = norm_chunk<TX>();
@@ -246,12 +249,12 @@ __global__ __launch_bounds__(THREADS) void norm_fwd_kernel(NormArgs a)
     int64_t row = at.q;
     const TX *x = (const TX *)a.x + s0 * a.x_stride + part * a.width;
     TY *y = (TY *)a.y + s0 * a.y_stride + part * a.width;
-    norm_batch<TX, E, NV, U, WHOLE> in;
+    norm_batch<TX, E, NV, U, ENDS, LANES == 2> in;
     in.load(x, a.x_step, row, end, a, at.at);
     const uint64_t offset = DROP ? fae_drop_offset(a.drop) : 0;
     float gamma[NV][E], beta[NV][E];
-    norm_weights<WHOLE, E, NV>(a.gamma, 1.f, a, part, at.at, gamma);
-    norm_weights<WHOLE, E, NV>(a.beta, 0.f, a, part, at.at, beta);
+    norm_weights<ENDS, E, NV>(a.gamma, 1.f, a, part, at.at, gamma);
+    norm_weights<ENDS, E, NV>(a.beta, 0.f, a, part, at.at, beta);
     norm_mask<E> mask[2][NV]; // of two rows where a lane has one chunk
     while (row < end) {
 #pragma unroll
@@ -267,7 +270,7 @@ __global__ __launch_bounds__(THREADS) void norm_fwd_kernel(NormArgs a)
             }
             float v[NV][E];
             in.get(u, a, at.at, v);
-            const float rstd = norm_center<WHOLE, LANES, WAVES, NV, E>(v, at.at, a, team);
+            const float rstd = norm_center<ENDS, LANES, WAVES, NV, E>(v, at.at, a, team);
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
 #pragma unroll
@@ -275,7 +278,7 @@ __global__ __launch_bounds__(THREADS) void norm_fwd_kernel(NormArgs a)
                     v[j][e] = v[j][e] * rstd * gamma[j][e] + beta[j][e];
                 if constexpr (DROP)
                     mask[u & 1][j].drop(v[j], a.drop);
-                fae_store<TY, E>(y + u * a.y_step, v[j], at.at[j], WHOLE ? FAE_WHOLE : a.ends);
+                fae_store<TY, E, ENDS>(y + u * a.y_step, v[j], at.at[j]);
             }
         }
         row += (int64_t)U * a.step;
@@ -289,7 +292,7 @@ __global__ __launch_bounds__(THREADS) void norm_fwd_kernel(NormArgs a)
 // The rows' gradient, and the team's sums of the weights' gradients in registers over all its rows.  DEPTH rows of a team are held:
 // the loads of the next DEPTH - 1 go out before the present one's sums are taken (into registers of their own, with no
 // copies between them, which would wait for the loads).
-template <typename TX, typename TY, int LANES, int THREADS, int NV, int DEPTH, bool WHOLE, bool DROP>
+template <typename TX, typename TY, int LANES, int THREADS, int NV, int DEPTH, int ENDS, bool DROP>
 __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
 {
     constexpr int E = norm_chunk<TX>();
@@ -303,8 +306,8 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
     const TX *x = (const TX *)a.x + s0 * a.x_stride + part * a.width;
     const TY *gy = (const TY *)a.gy + s0 * a.gy_stride + part * a.width;
     TX *gx = (TX *)a.y + s0 * a.y_stride + part * a.width;
-    norm_batch<TX, E, NV, 1, WHOLE> inx[DEPTH];
-    norm_batch<TY, E, NV, 1, WHOLE> ing[DEPTH];
+    norm_batch<TX, E, NV, 1, ENDS, LANES == 2> inx[DEPTH];
+    norm_batch<TY, E, NV, 1, ENDS, LANES == 2> ing[DEPTH];
     // row `ahead` from the present one, or that one again if the team has no such row
     auto load = [&](int k, int ahead) {
         const int64_t n = row + (int64_t)ahead * a.step < end ? ahead : 0;
@@ -318,7 +321,7 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
     }
     const uint64_t offset = DROP ? fae_drop_offset(a.drop) : 0;
     float gamma[NV][E], dgamma[NV][E], dbeta[NV][E];
-    norm_weights<WHOLE, E, NV>(a.gamma, 1.f, a, part, at.at, gamma);
+    norm_weights<ENDS, E, NV>(a.gamma, 1.f, a, part, at.at, gamma);
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
@@ -339,7 +342,7 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
             float v[NV][E], g[NV][E];
             inx[k].get(0, a, at.at, v);
             ing[k].get(0, a, at.at, g);
-            const float rstd = norm_center<WHOLE, LANES, WAVES, NV, E>(v, at.at, a, team);
+            const float rstd = norm_center<ENDS, LANES, WAVES, NV, E>(v, at.at, a, team);
             float c1 = 0.f, c2 = 0.f;
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
@@ -363,7 +366,7 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
 #pragma unroll
                 for (int e = 0; e < E; ++e)
                     g[j][e] = rstd * (g[j][e] - c1 - v[j][e] * c2);
-                fae_store<TX, E>(gx, g[j], at.at[j], WHOLE ? FAE_WHOLE : a.ends);
+                fae_store<TX, E, ENDS>(gx, g[j], at.at[j]);
             }
             row += a.step;
             if (row >= end)
@@ -384,9 +387,9 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             if (a.pgamma)
-                fae_store<float, E>(a.pgamma + (int64_t)r * a.pitch, dgamma[j], at.at[j], WHOLE ? FAE_WHOLE : a.ends);
+                fae_store<float, E, ENDS>(a.pgamma + (int64_t)r * a.pitch, dgamma[j], at.at[j]);
             if (a.pbeta)
-                fae_store<float, E>(a.pbeta + (int64_t)r * a.pitch, dbeta[j], at.at[j], WHOLE ? FAE_WHOLE : a.ends);
+                fae_store<float, E, ENDS>(a.pbeta + (int64_t)r * a.pitch, dbeta[j], at.at[j]);
         }
         return;
     }
@@ -457,26 +460,33 @@ struct NormShape {
     uint32_t pitch;
 };
 
-template <bool BWD, typename TX, typename TY, int LANES, int THREADS, int NV, bool WHOLE, bool DROP>
+template <bool BWD, typename TX, typename TY, int LANES, int THREADS, int NV, int ENDS, bool DROP>
 static void norm_launch(fae_ctx *ctx, const NormShape &s, const NormArgs &a)
 {
     if constexpr (BWD)
-        FAE_LAUNCH(ctx, (norm_bwd_kernel<TX, TY, LANES, THREADS, NV, norm_bwd_depth(NV, norm_chunk<TX>(), THREADS, DROP), WHOLE, DROP>), dim3(s.blocks), dim3(s.threads), 0,
+        FAE_LAUNCH(ctx, (norm_bwd_kernel<TX, TY, LANES, THREADS, NV, norm_bwd_depth(NV, norm_chunk<TX>(), THREADS, DROP), ENDS, DROP>), dim3(s.blocks), dim3(s.threads), 0,
                    ctx->stream, a);
     else
-        FAE_LAUNCH(ctx, (norm_fwd_kernel<TX, TY, LANES, THREADS, NV, norm_fwd_rows(NV), WHOLE, DROP>), dim3(s.blocks), dim3(s.threads), 0, ctx->stream, a);
+        FAE_LAUNCH(ctx, (norm_fwd_kernel<TX, TY, LANES, THREADS, NV, norm_fwd_rows(NV), ENDS, DROP>), dim3(s.blocks), dim3(s.threads), 0, ctx->stream, a);
+}
+
+template <bool BWD, typename TX, typename TY, int LANES, int THREADS, int NV, bool DROP>
+static void norm_by_end(fae_ctx *ctx, const NormShape &s, const NormArgs &a)
+{
+    if (a.ends == FAE_WHOLE)
+        norm_launch<BWD, TX, TY, LANES, THREADS, NV, FAE_WHOLE, DROP>(ctx, s, a);
+    else if (a.ends == FAE_CHUNKS)
+        norm_launch<BWD, TX, TY, LANES, THREADS, NV, FAE_CHUNKS, DROP>(ctx, s, a);
+    else
+        norm_launch<BWD, TX, TY, LANES, THREADS, NV, FAE_ANY, DROP>(ctx, s, a);
 }
 
 template <bool BWD, typename TX, typename TY, int LANES, int THREADS, int NV> static void norm_run(fae_ctx *ctx, const NormShape &s, const NormArgs &a)
 {
-    if (a.ends == FAE_WHOLE && a.drop.below)
-        norm_launch<BWD, TX, TY, LANES, THREADS, NV, true, true>(ctx, s, a);
-    else if (a.ends == FAE_WHOLE)
-        norm_launch<BWD, TX, TY, LANES, THREADS, NV, true, false>(ctx, s, a);
-    else if (a.drop.below)
-        norm_launch<BWD, TX, TY, LANES, THREADS, NV, false, true>(ctx, s, a);
+    if (a.drop.below)
+        norm_by_end<BWD, TX, TY, LANES, THREADS, NV, true>(ctx, s, a);
     else
-        norm_launch<BWD, TX, TY, LANES, THREADS, NV, false, false>(ctx, s, a);
+        norm_by_end<BWD, TX, TY, LANES, THREADS, NV, false>(ctx, s, a);
 }
 
 template <bool BWD, typename TX, typename TY> static void norm_by_width(fae_ctx *ctx, const NormShape &s, const NormArgs &a)

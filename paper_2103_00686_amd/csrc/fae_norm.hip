@@ -71,7 +71,7 @@ static NormShape norm_shape(const fae_norm *n, bool bwd)
         s.lanes *= 2;
     while (s.nv < most && s.nv * 64 < chunks)
         s.nv *= 2;
-    if (s.nv * 1024 < chunks)
+    if (s.nv * 1024 < chunks) // a workgroup of 1024 holds the row
         s.nv *= 2;
     if (s.nv * 64 < chunks)
         s.lanes = 64 * ((chunks + 64 * s.nv - 1) / (64 * s.nv));

@@ -64,34 +64,45 @@ template <int E> struct fae_place {
         from = c < last ? c : last;
     }
 };
-// how a launch's rows end
-enum { FAE_WHOLE, FAE_CHUNKS, FAE_CROOKED, FAE_SHORT }; // every lane's chunk whole; some absent; one cut; no whole chunk at all
+// How a launch's rows end: every lane's chunk whole; whole or absent; one cut by the end; no whole chunk at all.  Kernels are built for
+// the first two, and for the others together (FAE_ANY).
+enum { FAE_WHOLE, FAE_CHUNKS, FAE_CROOKED, FAE_SHORT };
+#define FAE_ANY FAE_CROOKED
 static inline int32_t fae_row_end(int64_t width, int chunk, int64_t lanes_width)
 {
     return width == lanes_width ? FAE_WHOLE : (width < chunk ? FAE_SHORT : (width % chunk ? FAE_CROOKED : FAE_CHUNKS));
 }
-template <typename T, int E> __device__ __forceinline__ typename fae_vec<T, E>::type fae_load(const T *row, const fae_place<E> &at, int ends)
+// ENDS: FAE_WHOLE, FAE_CHUNKS or FAE_ANY.  MAY_SHORT: a row may be shorter than a chunk (never where it has two)
+template <typename T, int E, int ENDS, bool MAY_SHORT = true>
+__device__ __forceinline__ typename fae_vec<T, E>::type fae_load(const T *row, const fae_place<E> &at, int ends)
 {
-    if (ends == FAE_SHORT) {
+    if (ENDS == FAE_ANY && MAY_SHORT && ends == FAE_SHORT) {
         typename fae_vec<T, E>::type v;
 #pragma unroll
         for (int e = 0; e < E; ++e)
             v[e] = e < at.there ? row[e] : (T)0.f;
         return v;
     }
-    const T *p = row + (ends == FAE_WHOLE ? at.col : at.from);
-    return *(const typename fae_vec<T, E>::loose *)p;
+    return *(const typename fae_vec<T, E>::loose *)(row + (ENDS == FAE_WHOLE ? at.col : at.from));
 }
 // what fae_load brought, as it belongs: zeros where the row has no values
-template <typename T, int E>
+template <typename T, int E, int ENDS>
 __device__ __forceinline__ void fae_settle(typename fae_vec<T, E>::type v, const fae_place<E> &at, int ends, float (&out)[E])
 {
-    if (ends == FAE_CROOKED && at.there > 0) {
+    static_assert(sizeof(v) == 8 || sizeof(v) == 16, "8 or 16 bytes");
+    if constexpr (ENDS == FAE_CHUNKS) {
+        typedef uint32_t words __attribute__((ext_vector_type(sizeof(v) / 4)));
+        words w = __builtin_bit_cast(words, v);
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(v) / 4; ++i)
+            w[i] = at.there > 0 ? w[i] : 0u;
+        v = __builtin_bit_cast(typename fae_vec<T, E>::type, w);
+    }
+    if (ENDS == FAE_ANY && ends == FAE_CROOKED && at.there > 0) {
         const uint32_t sh = (at.col - at.from) * 8 * sizeof(T);
         if constexpr (sizeof(v) == 8) {
             v = __builtin_bit_cast(typename fae_vec<T, E>::type, __builtin_bit_cast(uint64_t, v) >> sh);
         } else {
-            static_assert(sizeof(v) == 16, "8 or 16 bytes");
             typedef uint64_t pair __attribute__((ext_vector_type(2)));
             pair w = __builtin_bit_cast(pair, v);
             const uint64_t lo = w[0], hi = w[1];
@@ -104,19 +115,19 @@ __device__ __forceinline__ void fae_settle(typename fae_vec<T, E>::type v, const
     }
 #pragma unroll
     for (int e = 0; e < E; ++e)
-        out[e] = ends == FAE_WHOLE || e < at.there ? (float)v[e] : 0.f;
+        out[e] = ENDS != FAE_ANY || e < at.there ? (float)v[e] : 0.f;
 }
 
-template <typename T, int E> __device__ __forceinline__ void fae_store(T *row, const float (&v)[E], const fae_place<E> &at, int ends)
+template <typename T, int E, int ENDS> __device__ __forceinline__ void fae_store(T *row, const float (&v)[E], const fae_place<E> &at)
 {
     T *p = row + at.col;
     typename fae_vec<T, E>::type o;
 #pragma unroll
     for (int e = 0; e < E; ++e)
         o[e] = (T)v[e];
-    if (ends == FAE_WHOLE || at.there == E) {
+    if (ENDS == FAE_WHOLE || at.there == E) {
         *(typename fae_vec<T, E>::loose *)p = o;
-    } else {
+    } else if (ENDS == FAE_ANY) {
 #pragma unroll
         for (int e = 0; e < E; ++e)
             if (e < at.there)
