@@ -357,7 +357,9 @@ typedef struct {
 /* Layer norm over the rows:
  *   h = (x - mean(x)) / sqrt(var(x) + eps) with the mean and the (biased) variance of the row's width values,
  *   y = gamma[p][c] * h + beta[p][c], then dropout if asked for.
- * A row of equal values (the zeros of an empty bag) has h = 0. */
+ * A row of zeros (an empty bag) has h = 0, one of another value everywhere at most
+ * 2^-45 of that value / sqrt(eps).  The sum of the squared deviations of a row has to be a number of fp32
+ * (deviations below about 1e17). */
 typedef struct {
     int64_t n_rows;
     int32_t n_parts; /* 1 .. FAE_MAX_TABLES; n_rows * n_parts < 2^31 */
