@@ -82,6 +82,7 @@ class HotPath:
         self.remap = self.hot_ids = self.hotW = None
         self.n_hot: List[int] = []
         self._ws = {}
+        self._norm_ws: List[torch.Tensor] = []
 
     # -- plumbing -----------------------------------------------------------------
     def _workspace(self, name: str, nbytes: int) -> torch.Tensor:
@@ -319,6 +320,13 @@ class HotPath:
         parts = x.shape[1] if x.dim() == 3 else 1
         return B.Norm(x.shape[0], parts, x.shape[-1], gamma, beta, eps, x.dtype, y_dtype)
 
+    def _norm_workspace(self, nbytes: int) -> torch.Tensor:
+        """Grows by doubling and keeps the outgrown ones: a captured step, or one still queued, may use them."""
+        if not self._norm_ws or self._norm_ws[-1].numel() < nbytes:
+            least = 2 * self._norm_ws[-1].numel() if self._norm_ws else 1 << 16
+            self._norm_ws.append(torch.empty(max(nbytes, least), dtype=torch.uint8, device=self.dev))
+        return self._norm_ws[-1]
+
     def layer_norm(self, x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None,
                    eps: float = 1e-5, drop: Optional[B.Drop] = None, out_dtype: Optional[torch.dtype] = None,
                    out: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -337,7 +345,7 @@ class HotPath:
         norm = self._norm_of(x, gamma, None, eps, gy.dtype)
         dgamma, dbeta = (torch.empty((norm.n_parts, norm.width) if x.dim() == 3 else (norm.width,), dtype=torch.float32, device=self.dev)
                          for _ in range(2))
-        ws = self._workspace("norm", B.fae_layer_norm_bwd_workspace_bytes(norm))
+        ws = self._norm_workspace(B.fae_layer_norm_bwd_workspace_bytes(norm))
         B.fae_layer_norm_bwd(self.ctx, norm, x, gy, out, dgamma, dbeta, ws, drop)
         return out, dgamma, dbeta
 

@@ -122,3 +122,56 @@ def test_step_in_a_graph(dim, p):
         hp.sync()
         for a, b in zip(seen[i], [yy, gg, bb] + hp.hotW):
             assert torch.equal(a, b)
+
+
+def test_two_at_once():
+    """Two programs' steps on two streams, queued in turn without waiting: each has its own workspace."""
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    hps = [HotPath([1], 4, stream=st.cuda_stream) for st in streams]
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(3)
+    shapes = [(3000, 26, 64), (2000, 1, 1000)]
+    x = [torch.randn(sh, device="cuda", generator=gen) for sh in shapes]
+    gy = [torch.randn(sh, device="cuda", generator=gen) for sh in shapes]
+    gamma = [torch.randn(sh[1:], device="cuda", generator=gen) for sh in shapes]
+    torch.cuda.synchronize()  # the tensors were made on another stream than the calls run on, and the results are read on it
+    want = [hps[i].layer_norm_backward(x[i], gy[i], gamma[i]) for i in range(2)]
+    torch.cuda.synchronize()
+    outs = [[[torch.full_like(t, float("nan")) for t in want[i]] for _ in range(8)] for i in range(2)]
+    torch.cuda.synchronize()
+    calls = [[hps[i].prepare_layer_norm_backward(B.Norm(*shapes[i], gamma[i]), x[i], gy[i], *o) for o in outs[i]] for i in range(2)]
+    for a, b in zip(*calls):
+        a()
+        b()
+    torch.cuda.synchronize()
+    for i in range(2):
+        for o in outs[i]:
+            for a, b in zip(o, want[i]):
+                assert torch.equal(a, b.reshape(a.shape))
+
+
+def test_a_captured_step_outlives_its_workspace():
+    """A larger call behind the capture needs a larger workspace: the graph still has the one it was captured with."""
+    st = torch.cuda.Stream()
+    hp = HotPath([1], 4, stream=st.cuda_stream)
+    x, gy = torch.randn((2, 700, 3, 40), device="cuda")
+    torch.cuda.synchronize()
+    want = hp.layer_norm_backward(x, gy)
+    hp.sync()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=st):
+        got = hp.layer_norm_backward(x, gy)
+    big = torch.randn((20000, 1, 2000), device="cuda")
+    torch.cuda.synchronize()
+    hp.layer_norm_backward(big, big)
+    hp.sync()
+    fill = [torch.full((1 << 20,), float("nan"), device="cuda") for _ in range(64)]
+    for _ in range(3):
+        for t in got:
+            t.fill_(0.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+    assert all(bool(torch.isnan(f).all()) for f in fill)
