@@ -18,7 +18,7 @@ struct NormArgs {
     int64_t x_step, gy_step, y_step; // from one of a team's rows to its next
     const float *gamma, *beta;
     float *pgamma, *pbeta; // backward: sums of the launch's workgroups, or the gradients themselves
-    int64_t n_rows;   // rows of all parts
+    uint32_t n_rows;  // rows of all parts, below 2^31
     uint32_t step;    // teams
     uint32_t n_parts, width;
     uint32_t pitch;   // of a row of sums
@@ -62,11 +62,24 @@ template <int LANES> __device__ __forceinline__ float norm_lane_sum(float v)
     return v;
 }
 
-// Two sums at once.  Teams of several waves (a workgroup of their own) join them in LDS, in two buffers taken in turn: one barrier per
+// Teams of several waves (a workgroup of their own) join their sums in LDS, in two buffers taken in turn: one barrier per
 // call, as whoever writes a buffer again has passed the barrier behind everyone's reads of it.
 template <int LANES, bool WAVES> struct norm_team {
     float2 (*red)[16];
     int turn = 0;
+    __device__ __forceinline__ float sum(float a)
+    {
+        a = norm_lane_sum<LANES>(a);
+        if constexpr (WAVES) {
+            const int lane = fae_lane(), w = threadIdx.x / FAE_WAVE, n = blockDim.x / FAE_WAVE;
+            if (lane == 0)
+                red[turn][w].x = a;
+            __syncthreads();
+            a = norm_lane_sum<16>((lane & 15) < n ? red[turn][lane & 15].x : 0.f);
+            turn ^= 1;
+        }
+        return a;
+    }
     __device__ __forceinline__ void sum2(float &a, float &b)
     {
         a = norm_lane_sum<LANES>(a);
@@ -87,11 +100,12 @@ template <int LANES, bool WAVES> struct norm_team {
 // The numbers of a chunk's E values, two to a word
 template <int E> struct norm_mask {
     uint32_t w[E / 2];
+    // dropped values to zero, whatever they were; what the others are multiplied by is in the weights
     __device__ __forceinline__ void drop(float (&v)[E], const fae_drop_args &d) const
     {
 #pragma unroll
         for (int e = 0; e < E; ++e)
-            v[e] = fae_drop1(v[e], e & 1 ? w[e >> 1] >> 16 : w[e >> 1] & 0xffffu, d.below, d.scale);
+            v[e] = (e & 1 ? w[e >> 1] >> 16 : w[e >> 1] & 0xffffu) < d.below ? 0.f : v[e];
     }
 };
 // Two chunks' numbers (chunks of four or eight that start at columns ca and cb).  A chunk of four is half a group of eight, whose
@@ -161,14 +175,13 @@ template <int LANES, bool WAVES, int NV, int E> struct norm_place {
 template <int ENDS, int LANES, bool WAVES, int NV, int E>
 __device__ __forceinline__ float norm_center(float (&v)[NV][E], const fae_place<E> (&at)[NV], const NormArgs &a, norm_team<LANES, WAVES> &team)
 {
-    float s = 0.f, none = 0.f;
+    float s = 0.f;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
         for (int e = 0; e < E; ++e)
             s += v[j][e];
-    team.sum2(s, none);
-    const float m = s * a.inv_width;
+    const float m = team.sum(s) * a.inv_width;
     float d1 = 0.f, d2 = 0.f;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
@@ -189,11 +202,11 @@ __device__ __forceinline__ float norm_center(float (&v)[NV][E], const fae_place<
 #pragma unroll
         for (int e = 0; e < E; ++e)
             v[j][e] -= rest;
-    return 1.0f / sqrtf(fmaxf(var, 0.f) + a.eps);
+    return rsqrtf(fmaxf(var, 0.f) + a.eps); // to a unit of the last place; a root and a quotient would be a third of a short row's work
 }
 
-// a part's gamma or beta, ones or zeros if there are none
-template <int ENDS, int E, int NV>
+// a part's gamma or beta (ones or zeros if there are none) times dropout's factor
+template <int ENDS, bool DROP, int E, int NV>
 __device__ __forceinline__ void norm_weights(const float *w, float none, const NormArgs &a, uint32_t part, const fae_place<E> (&at)[NV],
                                              float (&out)[NV][E])
 {
@@ -213,6 +226,11 @@ __device__ __forceinline__ void norm_weights(const float *w, float none, const N
             for (int e = 0; e < E; ++e)
                 out[j][e] = w[part * a.width + (at[j].col + e < a.width ? at[j].col + e : a.width - 1)];
         }
+        if constexpr (DROP) {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                out[j][e] *= a.drop.scale;
+        }
     }
 }
 
@@ -220,11 +238,11 @@ __device__ __forceinline__ void norm_weights(const float *w, float none, const N
 // (behind one that some lanes do not take, every load waited for the one before: 6007 x 4 x 100 backward 28 -> 16 us)
 template <typename T, int E, int NV, int U, int ENDS, bool MAY_SHORT> struct norm_batch {
     typename fae_vec<T, E>::type raw[U][NV];
-    __device__ __forceinline__ void load(const T *p, int64_t step, int64_t row, int64_t end, const NormArgs &a, const fae_place<E> (&at)[NV])
+    __device__ __forceinline__ void load(const T *p, int64_t step, uint32_t row, uint32_t end, const NormArgs &a, const fae_place<E> (&at)[NV])
     {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const T *r = U == 1 || row + (int64_t)u * a.step < end ? p + u * step : p;
+            const T *r = U == 1 || row + u * a.step < end ? p + u * step : p;
 #pragma unroll
             for (int j = 0; j < NV; ++j)
                 raw[u][j] = fae_load<T, E, ENDS, MAY_SHORT>(r, at[j], a.ends);
@@ -249,24 +267,24 @@ __global__ __launch_bounds__(THREADS) void norm_fwd_kernel(NormArgs a)
     if (at.q >= a.step || at.q >= a.n_rows)
         return;
     const uint32_t s0 = at.q / a.n_parts, part = at.q - s0 * a.n_parts;
-    const int64_t end = a.n_rows;
-    int64_t row = at.q;
+    const uint32_t end = a.n_rows; // row + U * step stays below 2^32: the teams are no more than the rows need
+    uint32_t row = at.q;
     const TX *x = (const TX *)a.x + s0 * a.x_stride + part * a.width;
     TY *y = (TY *)a.y + s0 * a.y_stride + part * a.width;
     norm_batch<TX, E, NV, U, ENDS, LANES == 2> in;
     in.load(x, a.x_step, row, end, a, at.at);
     const uint64_t offset = DROP ? fae_drop_offset(a.drop) : 0;
     float gamma[NV][E], beta[NV][E];
-    norm_weights<ENDS, E, NV>(a.gamma, 1.f, a, part, at.at, gamma);
-    norm_weights<ENDS, E, NV>(a.beta, 0.f, a, part, at.at, beta);
+    norm_weights<ENDS, DROP, E, NV>(a.gamma, 1.f, a, part, at.at, gamma);
+    norm_weights<ENDS, DROP, E, NV>(a.beta, 0.f, a, part, at.at, beta);
     norm_mask<E> mask[2][NV]; // of two rows where a lane has one chunk
     while (row < end) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (U > 1 && row + (int64_t)u * a.step >= end)
+            if (U > 1 && row + u * a.step >= end)
                 break;
             if constexpr (DROP) {
-                const uint32_t r = (uint32_t)(row + (int64_t)u * a.step);
+                const uint32_t r = row + u * a.step;
                 if constexpr (NV > 1)
                     norm_row_masks<E, NV>(mask[u & 1], at.at, r, offset, a.drop);
                 else if (u % 2 == 0)
@@ -285,7 +303,7 @@ __global__ __launch_bounds__(THREADS) void norm_fwd_kernel(NormArgs a)
                 fae_store<TY, E, ENDS>(y + u * a.y_step, v[j], at.at[j]);
             }
         }
-        row += (int64_t)U * a.step;
+        row += U * a.step;
         x += U * a.x_step;
         y += U * a.y_step;
         if (row < end)
@@ -306,8 +324,8 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
     norm_team<LANES, WAVES> team{red};
     const norm_place<LANES, WAVES, NV, E> at(a.width);
     const uint32_t s0 = at.q / a.n_parts, part = at.q - s0 * a.n_parts;
-    const int64_t end = a.n_rows;
-    int64_t row = at.q < a.step ? (int64_t)at.q : end;
+    const uint32_t end = a.n_rows;
+    uint32_t row = at.q < a.step ? at.q : end;
     const TX *x = (const TX *)a.x + s0 * a.x_stride + part * a.width;
     const TY *gy = (const TY *)a.gy + s0 * a.gy_stride + part * a.width;
     TX *gx = (TX *)a.y + s0 * a.y_stride + part * a.width;
@@ -315,7 +333,7 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
     norm_batch<TY, E, NV, 1, ENDS, LANES == 2> ing[DEPTH];
     // row `ahead` from the present one, or that one again if the team has no such row
     auto load = [&](int k, int ahead) {
-        const int64_t n = row + (int64_t)ahead * a.step < end ? ahead : 0;
+        const int64_t n = row + ahead * a.step < end ? ahead : 0;
         inx[k].load(x + n * a.x_step, 0, row, end, a, at.at);
         ing[k].load(gy + n * a.gy_step, 0, row, end, a, at.at);
     };
@@ -326,7 +344,7 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
     }
     const uint64_t offset = DROP ? fae_drop_offset(a.drop) : 0;
     float gamma[NV][E], dgamma[NV][E], dbeta[NV][E];
-    norm_weights<ENDS, E, NV>(a.gamma, 1.f, a, part, at.at, gamma);
+    norm_weights<ENDS, DROP, E, NV>(a.gamma, 1.f, a, part, at.at, gamma);
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
@@ -340,9 +358,9 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
             load((k + DEPTH - 1) % DEPTH, DEPTH - 1);
             if constexpr (DROP) {
                 if constexpr (NV > 1)
-                    norm_row_masks<E, NV>(mask[k & 1], at.at, (uint32_t)row, offset, a.drop);
+                    norm_row_masks<E, NV>(mask[k & 1], at.at, row, offset, a.drop);
                 else if (k % 2 == 0)
-                    norm_masks<E>(mask[0][0], mask[1][0], at.at[0].col, (uint32_t)row, at.at[0].col, (uint32_t)row + a.step, offset, a.drop);
+                    norm_masks<E>(mask[0][0], mask[1][0], at.at[0].col, row, at.at[0].col, row + a.step, offset, a.drop);
             }
             float v[NV][E], g[NV][E];
             inx[k].get(0, a, at.at, v);
@@ -383,6 +401,15 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
     }
     if (!a.pgamma && !a.pbeta)
         return;
+    if constexpr (DROP) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                dgamma[j][e] *= a.drop.scale;
+                dbeta[j][e] *= a.drop.scale;
+            }
+    }
     // The sums go out a row per team, or where a workgroup has more teams than there are parts a row per part, the teams of a part
     // added up in LDS.
     if (a.in_regs) {

@@ -140,7 +140,7 @@ static int32_t norm_check(fae_ctx *ctx, const char *who, const fae_norm *n, cons
     memset(a, 0, sizeof(*a));
     a->gamma = n->gamma;
     a->beta = n->beta;
-    a->n_rows = n->n_rows * n->n_parts;
+    a->n_rows = (uint32_t)(n->n_rows * n->n_parts);
     a->n_parts = n->n_parts;
     a->width = n->width;
     a->eps = n->eps;
