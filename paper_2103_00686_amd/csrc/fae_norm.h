@@ -9,7 +9,7 @@
 // registers, and can add up their gradient over all its rows.
 //
 // What bounds it: memory where there are many rows (the forward writes 16 384 x 26 x 64 fp32 in 40 us, 5.4 TB/s, as a copy of that size
-// takes; the backward 63 us, 5.2 TB/s, where adding two such buffers up into a third takes 59), the chain of a row's three
+// takes; the backward 61 us, 5.3 TB/s, where adding two such buffers up into a third takes 59), the chain of a row's three
 // reductions where there are few (about half a microsecond a row, one where a team is several waves).
 struct NormArgs {
     const void *x, *gy;
@@ -470,10 +470,9 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
 // ---------------------------------------------------------------------------------
 // rows of a team whose loads go out together: up to 64 bytes of a lane
 constexpr int norm_fwd_rows(int nv) { return nv == 1 ? 4 : nv == 2 ? 2 : 1; }
-// Rows of a team that are held in the backward: two; four where a lane has one chunk and the generator to run beside it (50 001 x 26 x 64
-// with dropout 176 -> 159 us; without it four took longer, 63 -> 65); one where a workgroup of 1024 has no registers for more
-// (4096 x 16 384 bf16 148 -> 97 us).
-constexpr int norm_bwd_depth(int nv, int chunk, int threads, bool drop) { return threads == 1024 && nv * chunk > 8 ? 1 : nv == 1 && drop ? 4 : 2; }
+// Rows of a team that are held in the backward: two (four: 16 384 x 26 x 64 62 -> 65 us, 50 001 x 26 x 64 with dropout 152 -> 160); one where
+// a workgroup of 1024 has no registers for more (4096 x 16 384 bf16 148 -> 97 us).
+constexpr int norm_bwd_depth(int nv, int chunk, int threads) { return threads == 1024 && nv * chunk > 8 ? 1 : 2; }
 
 // Chunks per lane at most, as long as a workgroup of 1024 then holds the row: 16 values in the forward; two in the backward, where a value
 // takes eight registers (16 384 x 4096 fp32 with two and four 147 and 160 us; with one, bf16, 16 384 x 1664 53 instead of 48).
@@ -497,7 +496,7 @@ template <bool BWD, typename TX, typename TY, int LANES, int THREADS, int NV, in
 static void norm_launch(fae_ctx *ctx, const NormShape &s, const NormArgs &a)
 {
     if constexpr (BWD)
-        FAE_LAUNCH(ctx, (norm_bwd_kernel<TX, TY, LANES, THREADS, NV, norm_bwd_depth(NV, norm_chunk<TX>(), THREADS, DROP), ENDS, DROP>), dim3(s.blocks), dim3(s.threads), 0,
+        FAE_LAUNCH(ctx, (norm_bwd_kernel<TX, TY, LANES, THREADS, NV, norm_bwd_depth(NV, norm_chunk<TX>(), THREADS), ENDS, DROP>), dim3(s.blocks), dim3(s.threads), 0,
                    ctx->stream, a);
     else
         FAE_LAUNCH(ctx, (norm_fwd_kernel<TX, TY, LANES, THREADS, NV, norm_fwd_rows(NV), ENDS, DROP>), dim3(s.blocks), dim3(s.threads), 0, ctx->stream, a);
