@@ -44,11 +44,6 @@ template <typename T, int E> struct fae_vec {
     typedef type loose __attribute__((aligned(sizeof(T))));
 };
 
-template <typename T, int E> __device__ __forceinline__ typename fae_vec<T, E>::type fae_load(const T *p)
-{
-    return *(const typename fae_vec<T, E>::loose *)p;
-}
-
 // Where a lane's chunk of E values lies in a row of `width`.  Loads have no branch per lane or value (a load behind one waits for the
 // loads in front of it): a chunk that the row's end cuts is loaded as the E values that end with the row and moved down when they
 // are there, and lanes behind the row load that chunk too.  Rows shorter than a chunk are the exception.

@@ -308,3 +308,53 @@ def test_many_rows_past_32_bits(hp):
     gx2, dg2, db2 = hp.layer_norm_backward(x.contiguous(), want)
     hp.sync()
     assert torch.equal(y, want) and torch.equal(gx, gx2) and torch.equal(dg, dg2) and torch.equal(db, db2)
+
+
+@pytest.mark.parametrize("tx,ty", TYPES)
+@pytest.mark.parametrize("width", [8, 16, 32, 128, 256, 512, 1024, 2048, 4096, 8192, 16384])
+def test_whole_rows_with_dropout(hp, width, tx, ty):
+    """Rows that fill their lanes, dropout on top; more rows than the backward's one launch takes."""
+    n = 600 if width <= 64 else 150 if width <= 1024 else 40
+    x, gy, gamma, beta = _make(width, n, 1, width, tx, ty)
+    _check(hp, x, gy, gamma, beta, ty, p=0.2)
+
+
+@pytest.mark.parametrize("seed", range(60))
+def test_random_shapes(hp, seed):
+    rng = np.random.default_rng(seed)
+    tx, ty = TYPES[rng.integers(len(TYPES))]
+    parts = int(rng.choice([1, 1, 2, 3, 6, 11, 26, 64]))
+    width = int(np.exp(rng.uniform(0, np.log(16384 if parts == 1 else 400))))
+    n = max(1, min(int(np.exp(rng.uniform(0, np.log(20000)))), 3_000_000 // (parts * width)))
+    pad, lead = (int(v) for v in rng.integers(0, 9, 2)) if rng.random() < 0.5 else (0, 0)
+    x, gy, gamma, beta = _make(seed, n, parts, width, tx, ty, rng.random() < 0.8, pad, lead)
+    counter = torch.full((1,), 12, dtype=torch.int64, device="cuda") if rng.random() < 0.3 else None
+    _check(hp, x, gy, gamma, beta, ty, p=float(rng.choice([0.0, 0.1, 0.6])), pad=pad, lead=lead, counter=counter)
+
+
+def test_refused_calls_leave_their_outputs(hp):
+    x = torch.randn((20, 2, 32), device="cuda")
+    y = torch.full_like(x, 5.0)
+    wide = torch.zeros((2, B.FAE_NORM_MAX_WIDTH + 1), device="cuda")
+    refused = [
+        (B.FaeError, lambda: hp.layer_norm(x.half(), out=y.to(BF16))),
+        (B.FaeError, lambda: hp.layer_norm(x.half(), out=y)),
+        (B.FaeError, lambda: hp.layer_norm(wide)),
+        (B.FaeError, lambda: hp.layer_norm(x, eps=0.0, out=y)),
+        (B.FaeError, lambda: hp.layer_norm(x, drop=B.Drop(1.5, 1), out=y)),
+        (B.FaeError, lambda: hp.layer_norm(x[:1].expand(20, 2, 32), out=y)),
+        (B.FaeError, lambda: hp.layer_norm(y.view(-1)[:640].view(10, 2, 32), out=y.view(-1)[32:672].view(10, 2, 32))),
+        (B.FaeError, lambda: B.fae_layer_norm_bwd(hp.ctx, B.Norm(20, 2, 32), x, x, y, None, None, torch.empty(16, dtype=torch.uint8, device="cuda"))),
+        (ValueError, lambda: hp.layer_norm(x, torch.ones(32, device="cuda"), out=y)),
+        (ValueError, lambda: hp.layer_norm(x, out=y[:10])),
+        (ValueError, lambda: hp.layer_norm(x.transpose(1, 2), out=y)),
+        (ValueError, lambda: hp.dropout(x, B.Drop(0.5, 1), out=y[:, :1])),
+        (TypeError, lambda: hp.layer_norm(x.double(), out=y)),
+        (TypeError, lambda: hp.layer_norm(x.cpu(), out=y)),
+        (TypeError, lambda: hp.layer_norm(x, torch.ones((2, 32), device="cuda", dtype=BF16), out=y)),
+    ]
+    for kind, call in refused:
+        with pytest.raises(kind):
+            call()
+    hp.sync()
+    assert bool((y == 5.0).all())
