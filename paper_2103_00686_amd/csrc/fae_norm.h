@@ -313,9 +313,9 @@ __global__ __launch_bounds__(THREADS) void norm_fwd_kernel(NormArgs a)
 
 // The rows' gradient, and the team's sums of the weights' gradients in registers over all its rows.  DEPTH rows of a team are held:
 // the loads of the next DEPTH - 1 go out before the present one's sums are taken (into registers of their own, with no
-// copies between them, which would wait for the loads).  All teams walk with one stride: rows in flight then lie side by side
+// copies between them, which would wait for the loads).  EARLY: a row's own registers are loaded again as soon as its values are taken.  All teams walk with one stride: rows in flight then lie side by side
 // (16 384 x 26 x 64 73 -> 67 us against a stretch of rows for every few workgroups).
-template <typename TX, typename TY, int LANES, int THREADS, int NV, int DEPTH, int ENDS, bool DROP>
+template <typename TX, typename TY, int LANES, int THREADS, int NV, int DEPTH, bool EARLY, int ENDS, bool DROP>
 __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
 {
     constexpr int E = norm_chunk<TX>();
@@ -339,7 +339,7 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
     };
     if (row < end) {
 #pragma unroll
-        for (int k = 0; k < DEPTH - 1; ++k)
+        for (int k = 0; k < (EARLY ? DEPTH : DEPTH - 1); ++k)
             load(k, k);
     }
     const uint64_t offset = DROP ? fae_drop_offset(a.drop) : 0;
@@ -355,7 +355,8 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
     while (row < end) {
 #pragma unroll
         for (int k = 0; k < DEPTH; ++k) {
-            load((k + DEPTH - 1) % DEPTH, DEPTH - 1);
+            if constexpr (!EARLY)
+                load((k + DEPTH - 1) % DEPTH, DEPTH - 1);
             if constexpr (DROP) {
                 if constexpr (NV > 1)
                     norm_row_masks<E, NV>(mask[k & 1], at.at, row, offset, a.drop);
@@ -365,6 +366,8 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
             float v[NV][E], g[NV][E];
             inx[k].get(0, a, at.at, v);
             ing[k].get(0, a, at.at, g);
+            if constexpr (EARLY)
+                load(k, DEPTH);
             const float rstd = norm_center<ENDS, LANES, WAVES, NV, E>(v, at.at, a, team);
             float c1 = 0.f, c2 = 0.f;
 #pragma unroll
@@ -470,9 +473,15 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
 // ---------------------------------------------------------------------------------
 // rows of a team whose loads go out together: up to 64 bytes of a lane
 constexpr int norm_fwd_rows(int nv) { return nv == 1 ? 4 : nv == 2 ? 2 : 1; }
-// Rows of a team that are held in the backward: two (four: 16 384 x 26 x 64 62 -> 65 us, 50 001 x 26 x 64 with dropout 152 -> 160); one where
-// a workgroup of 1024 has no registers for more (4096 x 16 384 bf16 148 -> 97 us).
-constexpr int norm_bwd_depth(int nv, int chunk, int threads) { return threads == 1024 && nv * chunk > 8 ? 1 : 2; }
+// How the backward's loads run ahead.  Two rows held (four: 16 384 x 26 x 64 62 -> 65 us, 50 001 x 26 x 64 with dropout 152 -> 160); fp32 rows of
+// several waves with one row's registers, filled again as soon as its values are taken (16 384 x 4096 150 -> 140 us, 40 000 x 2048 with
+// dropout 171 -> 158; 16-bit rows, with twice the values per lane, 133 -> 139 for 65 536 x 1664); one row and nothing ahead where a
+// workgroup of 1024 has no registers for more (4096 x 16 384 bf16 148 -> 97 us, with one filled early 136).
+constexpr bool norm_bwd_early(int nv, int chunk, int threads) { return threads == 512 && nv * chunk <= 8; }
+constexpr int norm_bwd_depth(int nv, int chunk, int threads)
+{
+    return norm_bwd_early(nv, chunk, threads) || (threads == 1024 && nv * chunk > 8) ? 1 : 2;
+}
 
 // Chunks per lane at most, as long as a workgroup of 1024 then holds the row: 16 values in the forward; two in the backward, where a value
 // takes eight registers (16 384 x 4096 fp32 with two and four 147 and 160 us; with one, bf16, 16 384 x 1664 53 instead of 48).
@@ -496,7 +505,7 @@ template <bool BWD, typename TX, typename TY, int LANES, int THREADS, int NV, in
 static void norm_launch(fae_ctx *ctx, const NormShape &s, const NormArgs &a)
 {
     if constexpr (BWD)
-        FAE_LAUNCH(ctx, (norm_bwd_kernel<TX, TY, LANES, THREADS, NV, norm_bwd_depth(NV, norm_chunk<TX>(), THREADS), ENDS, DROP>), dim3(s.blocks), dim3(s.threads), 0,
+        FAE_LAUNCH(ctx, (norm_bwd_kernel<TX, TY, LANES, THREADS, NV, norm_bwd_depth(NV, norm_chunk<TX>(), THREADS), norm_bwd_early(NV, norm_chunk<TX>(), THREADS), ENDS, DROP>), dim3(s.blocks), dim3(s.threads), 0,
                    ctx->stream, a);
     else
         FAE_LAUNCH(ctx, (norm_fwd_kernel<TX, TY, LANES, THREADS, NV, norm_fwd_rows(NV), ENDS, DROP>), dim3(s.blocks), dim3(s.threads), 0, ctx->stream, a);
