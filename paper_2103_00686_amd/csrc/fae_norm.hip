@@ -3,7 +3,8 @@
 
 #include "fae_norm.h"
 
-// dgamma (z = 0) and dbeta (z = 1) of a part from its rows of sums: L lanes of four columns each, 256 / L rows of sums at a time.
+// dgamma (z = 0) and dbeta (z = 1) of a part from its rows of sums: L lanes of four columns each, THREADS / L rows of sums
+// at a time.
 struct NormWeightArgs {
     const float *sums[2];
     float *out[2];
@@ -11,10 +12,9 @@ struct NormWeightArgs {
     uint32_t n_sums;  // rows of sums of a part
     uint32_t teams;   // of a workgroup if it left a row per part, 0 if it left one per team
 };
-// From this many columns on, workgroups of 64 columns are enough for the chip and read whole lines; below, of 16 (64 and 16 columns,
-// us of a whole backward: 512 x 8192 bf16 16.2 and 17.2, 4096 x 16384 bf16 96.7 and 101, 16384 x 8192 bf16 147 and 150;
-// 6007 x 4 x 100 fp32 16.0 and 15.3, 400 000 x 64 fp32 59.5 and 58.8).
-#define NORM_WIDE_SUMS 4096
+// From this many columns on, workgroups of 32 columns are enough for the chip and waste less of a line than those of 16 (us of a whole backward
+// with 32 | 16 columns: 4096 x 1664 bf16 17.0 | 18.3, 4096 x 4000 26.9 | 29.7; 4000 x 1024 fp32 16.2 | 15.9, 6007 x 4 x 100 12.5 | 12.1).
+#define NORM_WIDE_SUMS 1536
 template <int L, int THREADS> __global__ __launch_bounds__(THREADS) void norm_weights_kernel(NormWeightArgs a)
 {
     constexpr int ROWS = THREADS / L;
@@ -271,7 +271,7 @@ extern "C" int32_t fae_layer_norm_bwd(fae_ctx *ctx, const fae_norm *norm, const 
     if (!s.direct && (dgamma || dbeta)) {
         fae_ktimer kt(ctx, FAE_K_NORM_WEIGHTS);
         if ((int64_t)a.n_parts * s.pitch >= NORM_WIDE_SUMS)
-            FAE_LAUNCH(ctx, (norm_weights_kernel<16, 1024>), dim3((s.pitch + 63) / 64, a.n_parts, 2), dim3(1024), 0, ctx->stream, w);
+            FAE_LAUNCH(ctx, (norm_weights_kernel<8, 512>), dim3((s.pitch + 31) / 32, a.n_parts, 2), dim3(512), 0, ctx->stream, w);
         else
             FAE_LAUNCH(ctx, (norm_weights_kernel<4, 256>), dim3((s.pitch + 15) / 16, a.n_parts, 2), dim3(256), 0, ctx->stream, w);
         FAE_LAUNCH_CHECK(ctx);
