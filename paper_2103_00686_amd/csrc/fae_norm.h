@@ -147,7 +147,7 @@ __device__ __forceinline__ void norm_row_masks(norm_mask<E> (&m)[NV], const fae_
 template <typename TX> constexpr int norm_chunk() { return sizeof(TX) == 2 ? 8 : 4; } // values in 16 bytes of x
 
 // where a thread stands
-template <int LANES, bool WAVES, int NV, int E> struct norm_place {
+template <int LANES, int THREADS, bool WAVES, int NV, int E> struct norm_place {
     uint32_t q;      // team of the launch
     int l;           // lane of the team
     int lanes;       // lanes of the team
@@ -159,7 +159,7 @@ template <int LANES, bool WAVES, int NV, int E> struct norm_place {
             l = threadIdx.x;
             lanes = blockDim.x;
         } else {
-            q = blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+            q = blockIdx.x * (THREADS / LANES) + threadIdx.x / LANES;
             l = threadIdx.x % LANES;
             lanes = LANES;
         }
@@ -256,14 +256,13 @@ template <typename T, int E, int NV, int U, int ENDS, bool MAY_SHORT> struct nor
     }
 };
 
-template <typename TX, typename TY, int LANES, int THREADS, int NV, int U, int ENDS, bool DROP>
+template <typename TX, typename TY, int LANES, int THREADS, bool WAVES, int NV, int U, int ENDS, bool DROP>
 __global__ __launch_bounds__(THREADS) void norm_fwd_kernel(NormArgs a)
 {
     constexpr int E = norm_chunk<TX>();
-    constexpr bool WAVES = THREADS > 256;
     __shared__ float2 red[2][16];
     norm_team<LANES, WAVES> team{red};
-    const norm_place<LANES, WAVES, NV, E> at(a.width);
+    const norm_place<LANES, THREADS, WAVES, NV, E> at(a.width);
     if (at.q >= a.step || at.q >= a.n_rows)
         return;
     const uint32_t s0 = at.q / a.n_parts, part = at.q - s0 * a.n_parts;
@@ -315,14 +314,13 @@ __global__ __launch_bounds__(THREADS) void norm_fwd_kernel(NormArgs a)
 // the loads of the next DEPTH - 1 go out before the present one's sums are taken (into registers of their own, with no
 // copies between them, which would wait for the loads).  EARLY: a row's own registers are loaded again as soon as its values are taken.  All teams walk with one stride: rows in flight then lie side by side
 // (16 384 x 26 x 64 73 -> 67 us against a stretch of rows for every few workgroups).
-template <typename TX, typename TY, int LANES, int THREADS, int NV, int DEPTH, bool EARLY, int ENDS, bool DROP>
+template <typename TX, typename TY, int LANES, int THREADS, bool WAVES, int NV, int DEPTH, bool EARLY, int ENDS, bool DROP>
 __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
 {
     constexpr int E = norm_chunk<TX>();
-    constexpr bool WAVES = THREADS > 256;
     __shared__ float2 red[2][16];
     norm_team<LANES, WAVES> team{red};
-    const norm_place<LANES, WAVES, NV, E> at(a.width);
+    const norm_place<LANES, THREADS, WAVES, NV, E> at(a.width);
     const uint32_t s0 = at.q / a.n_parts, part = at.q - s0 * a.n_parts;
     const uint32_t end = a.n_rows;
     uint32_t row = at.q < a.step ? at.q : end;
@@ -429,8 +427,8 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
         return;
     }
     if constexpr (!WAVES) {
-        constexpr int TEAMS = 256 / LANES, ROW = LANES * NV * E;
-        __shared__ float sums[TEAMS * ROW], pieces[256];
+        constexpr int TEAMS = THREADS / LANES, ROW = LANES * NV * E;
+        __shared__ float sums[TEAMS * ROW], pieces[THREADS];
         for (int which = 0; which < 2; ++which) {
             float *out = which ? a.pbeta : a.pgamma;
             __syncthreads();
@@ -443,8 +441,8 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
             if (!out)
                 continue;
             // several threads to an output where there are fewer of these than threads
-            const uint32_t n = a.part_rows * a.width, split = n < 256 ? 256 / n : 1;
-            for (uint32_t i = threadIdx.x; i < n * split; i += 256) {
+            const uint32_t n = a.part_rows * a.width, split = n < THREADS ? THREADS / n : 1;
+            for (uint32_t i = threadIdx.x; i < n * split; i += THREADS) {
                 const uint32_t piece = i / n, o = i - piece * n, k = o / a.width, c = o - k * a.width;
                 float s = 0.f;
                 for (uint32_t t = k + piece * a.n_parts; t < TEAMS; t += split * a.n_parts)
@@ -477,10 +475,10 @@ constexpr int norm_fwd_rows(int nv) { return nv == 1 ? 4 : nv == 2 ? 2 : 1; }
 // several waves with one row's registers, filled again as soon as its values are taken (16 384 x 4096 150 -> 140 us, 40 000 x 2048 with
 // dropout 171 -> 158; 16-bit rows, with twice the values per lane, 133 -> 139 for 65 536 x 1664); one row and nothing ahead where a
 // workgroup of 1024 has no registers for more (4096 x 16 384 bf16 148 -> 97 us, with one filled early 136).
-constexpr bool norm_bwd_early(int nv, int chunk, int threads) { return threads == 512 && nv * chunk <= 8; }
-constexpr int norm_bwd_depth(int nv, int chunk, int threads)
+constexpr bool norm_bwd_early(int nv, int chunk, int threads, bool waves) { return waves && threads == 512 && nv * chunk <= 8; }
+constexpr int norm_bwd_depth(int nv, int chunk, int threads, bool waves)
 {
-    return norm_bwd_early(nv, chunk, threads) || (threads == 1024 && nv * chunk > 8) ? 1 : 2;
+    return norm_bwd_early(nv, chunk, threads, waves) || (threads == 1024 && nv * chunk > 8) ? 1 : 2;
 }
 
 // Chunks per lane at most, as long as a workgroup of 1024 then holds the row: 16 values in the forward; two in the backward, where a value
@@ -501,63 +499,69 @@ struct NormShape {
     uint32_t pitch;
 };
 
-template <bool BWD, typename TX, typename TY, int LANES, int THREADS, int NV, int ENDS, bool DROP>
+template <bool BWD, typename TX, typename TY, int LANES, int THREADS, bool WAVES, int NV, int ENDS, bool DROP>
 static void norm_launch(fae_ctx *ctx, const NormShape &s, const NormArgs &a)
 {
     if constexpr (BWD)
-        FAE_LAUNCH(ctx, (norm_bwd_kernel<TX, TY, LANES, THREADS, NV, norm_bwd_depth(NV, norm_chunk<TX>(), THREADS), norm_bwd_early(NV, norm_chunk<TX>(), THREADS), ENDS, DROP>), dim3(s.blocks), dim3(s.threads), 0,
+        FAE_LAUNCH(ctx, (norm_bwd_kernel<TX, TY, LANES, THREADS, WAVES, NV, norm_bwd_depth(NV, norm_chunk<TX>(), THREADS, WAVES), norm_bwd_early(NV, norm_chunk<TX>(), THREADS, WAVES), ENDS, DROP>), dim3(s.blocks), dim3(s.threads), 0,
                    ctx->stream, a);
     else
-        FAE_LAUNCH(ctx, (norm_fwd_kernel<TX, TY, LANES, THREADS, NV, norm_fwd_rows(NV), ENDS, DROP>), dim3(s.blocks), dim3(s.threads), 0, ctx->stream, a);
+        FAE_LAUNCH(ctx, (norm_fwd_kernel<TX, TY, LANES, THREADS, WAVES, NV, norm_fwd_rows(NV), ENDS, DROP>), dim3(s.blocks), dim3(s.threads), 0, ctx->stream, a);
 }
 
-template <bool BWD, typename TX, typename TY, int LANES, int THREADS, int NV, bool DROP>
+template <bool BWD, typename TX, typename TY, int LANES, int THREADS, bool WAVES, int NV, bool DROP>
 static void norm_by_end(fae_ctx *ctx, const NormShape &s, const NormArgs &a)
 {
     if (a.ends == FAE_WHOLE)
-        norm_launch<BWD, TX, TY, LANES, THREADS, NV, FAE_WHOLE, DROP>(ctx, s, a);
+        norm_launch<BWD, TX, TY, LANES, THREADS, WAVES, NV, FAE_WHOLE, DROP>(ctx, s, a);
     else if (a.ends == FAE_CHUNKS)
-        norm_launch<BWD, TX, TY, LANES, THREADS, NV, FAE_CHUNKS, DROP>(ctx, s, a);
+        norm_launch<BWD, TX, TY, LANES, THREADS, WAVES, NV, FAE_CHUNKS, DROP>(ctx, s, a);
     else
-        norm_launch<BWD, TX, TY, LANES, THREADS, NV, FAE_ANY, DROP>(ctx, s, a);
+        norm_launch<BWD, TX, TY, LANES, THREADS, WAVES, NV, FAE_ANY, DROP>(ctx, s, a);
 }
 
-template <bool BWD, typename TX, typename TY, int LANES, int THREADS, int NV> static void norm_run(fae_ctx *ctx, const NormShape &s, const NormArgs &a)
+template <bool BWD, typename TX, typename TY, int LANES, int THREADS, bool WAVES, int NV> static void norm_run(fae_ctx *ctx, const NormShape &s, const NormArgs &a)
 {
     if (a.drop.below)
-        norm_by_end<BWD, TX, TY, LANES, THREADS, NV, true>(ctx, s, a);
+        norm_by_end<BWD, TX, TY, LANES, THREADS, WAVES, NV, true>(ctx, s, a);
     else
-        norm_by_end<BWD, TX, TY, LANES, THREADS, NV, false>(ctx, s, a);
+        norm_by_end<BWD, TX, TY, LANES, THREADS, WAVES, NV, false>(ctx, s, a);
+}
+
+template <bool BWD, typename TX, typename TY, int THREADS> static void norm_teams(fae_ctx *ctx, const NormShape &s, const NormArgs &a)
+{
+    switch (s.lanes) {
+    case 2: norm_run<BWD, TX, TY, 2, THREADS, false, 1>(ctx, s, a); return;
+    case 4: norm_run<BWD, TX, TY, 4, THREADS, false, 1>(ctx, s, a); return;
+    case 8: norm_run<BWD, TX, TY, 8, THREADS, false, 1>(ctx, s, a); return;
+    case 16: norm_run<BWD, TX, TY, 16, THREADS, false, 1>(ctx, s, a); return;
+    case 32: norm_run<BWD, TX, TY, 32, THREADS, false, 1>(ctx, s, a); return;
+    }
+    if (s.nv == 1)
+        norm_run<BWD, TX, TY, 64, THREADS, false, 1>(ctx, s, a);
+    else if (s.nv == 2)
+        norm_run<BWD, TX, TY, 64, THREADS, false, 2>(ctx, s, a);
+    else if constexpr (norm_chunks(BWD, norm_chunk<TX>()) >= 4)
+        norm_run<BWD, TX, TY, 64, THREADS, false, 4>(ctx, s, a);
 }
 
 template <bool BWD, typename TX, typename TY> static void norm_by_width(fae_ctx *ctx, const NormShape &s, const NormArgs &a)
 {
     constexpr int MOST = norm_chunks(BWD, norm_chunk<TX>()), ALL = FAE_NORM_MAX_WIDTH / norm_chunk<TX>() / 1024; // per lane
-    switch (s.lanes) {
-    case 2: norm_run<BWD, TX, TY, 2, 256, 1>(ctx, s, a); return;
-    case 4: norm_run<BWD, TX, TY, 4, 256, 1>(ctx, s, a); return;
-    case 8: norm_run<BWD, TX, TY, 8, 256, 1>(ctx, s, a); return;
-    case 16: norm_run<BWD, TX, TY, 16, 256, 1>(ctx, s, a); return;
-    case 32: norm_run<BWD, TX, TY, 32, 256, 1>(ctx, s, a); return;
-    case 64: break;
-    default:
-        if (s.lanes <= 512)
-            norm_run<BWD, TX, TY, 64, 512, MOST>(ctx, s, a);
-        else if (s.nv == MOST)
-            norm_run<BWD, TX, TY, 64, 1024, MOST>(ctx, s, a);
-        else if constexpr (ALL > MOST)
-            norm_run<BWD, TX, TY, 64, 1024, ALL>(ctx, s, a);
-        return;
-    }
-    if (s.nv == 1) {
-        norm_run<BWD, TX, TY, 64, 256, 1>(ctx, s, a);
-        return;
-    }
-    if (s.nv == 2)
-        norm_run<BWD, TX, TY, 64, 256, 2>(ctx, s, a);
-    if constexpr (MOST >= 4)
-        if (s.nv == 4)
-            norm_run<BWD, TX, TY, 64, 256, 4>(ctx, s, a);
+    if (s.lanes <= 64) {
+        if constexpr (BWD) {
+            if (s.threads == 512) {
+                norm_teams<BWD, TX, TY, 512>(ctx, s, a);
+                return;
+            }
+        }
+        norm_teams<BWD, TX, TY, 256>(ctx, s, a);
+    } else if (s.lanes <= 512)
+        norm_run<BWD, TX, TY, 64, 512, true, MOST>(ctx, s, a);
+    else if (s.nv == MOST)
+        norm_run<BWD, TX, TY, 64, 1024, true, MOST>(ctx, s, a);
+    else if constexpr (ALL > MOST)
+        norm_run<BWD, TX, TY, 64, 1024, true, ALL>(ctx, s, a);
 }
 
 // a file each, so that they are compiled beside each other

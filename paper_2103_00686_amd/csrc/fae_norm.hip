@@ -59,6 +59,22 @@ template <int L, int THREADS> __global__ __launch_bounds__(THREADS) void norm_we
 
 static uint32_t norm_gcd(uint32_t a, uint32_t b) { return b ? norm_gcd(b, a % b) : a; }
 
+// rows of a team that one launch takes
+static int norm_few_rows(int lanes, uint32_t threads) { return lanes > 64 ? 4 : threads == 512 ? 6 : 8; }
+
+// Workgroups of 512 lanes or 256 for teams of up to a wave, in the backward.  Where a workgroup adds up its teams' sums in LDS (more teams
+// than parts) 512 leave half as many rows of sums, which pays once the launch is as large as it gets (us with 512 | 256: 6007 x 4 x 100 fp32
+// 11.1 | 12.3, 2403 x 13 x 64 11.1 | 12.8, 4096 x 256 8.2 | 8.8, 65 536 x 512 76.4 | 78.7; below, 4096 x 64 7.2 | 6.9; and where teams'
+// sums go out as they are 1201 x 26 x 64 11.8 | 9.0), or where one launch is then enough (717 x 16 6.0 | 6.4).
+static bool norm_wide_workgroup(int64_t rows, uint32_t parts, int lanes)
+{
+    const uint32_t teams = 256 / lanes;
+    if (teams <= parts)
+        return false;
+    const int64_t few = teams / parts * parts, few_wide = 2 * teams / parts * parts;
+    return rows >= 2LL * 512 * teams || (rows > few * norm_few_rows(lanes, 256) && rows <= few_wide * norm_few_rows(lanes, 512));
+}
+
 static NormShape norm_shape(const fae_norm *n, bool bwd)
 {
     NormShape s;
@@ -75,10 +91,11 @@ static NormShape norm_shape(const fae_norm *n, bool bwd)
         s.nv *= 2;
     if (s.nv * 64 < chunks)
         s.lanes = 64 * ((chunks + 64 * s.nv - 1) / (64 * s.nv));
-    s.threads = s.lanes > 64 ? s.lanes : 256;
-    s.teams = s.threads / s.lanes;
     const int64_t rows = n->n_rows * n->n_parts;
-    const uint32_t parts = n->n_parts, whole = parts / norm_gcd(parts, s.teams); // workgroups whose teams are a multiple of the parts
+    const uint32_t parts = n->n_parts;
+    s.threads = s.lanes > 64 ? s.lanes : bwd && norm_wide_workgroup(rows, parts, s.lanes) ? 512 : 256;
+    s.teams = s.threads / s.lanes;
+    const uint32_t whole = parts / norm_gcd(parts, s.teams); // workgroups whose teams are a multiple of the parts
     s.pitch = (n->width + 3) / 4 * 4;
     s.part_rows = s.teams > parts ? parts : s.teams;
     // Rows of a team at least.  Backward: fewer where a workgroup adds up its teams' sums before it writes them (2 and 4, us: 717 x 16
@@ -92,7 +109,7 @@ static NormShape norm_shape(const fae_norm *n, bool bwd)
     // launch.  Up to eight rows each, four where a team is whole waves (us with one launch | two: 128 x 64 fp32 5.5 | 6.3, 256 x 64
     // with 16 rows each 8.2 | 6.4, 16 x 256 4.2 | 6.1, 4 x 26 x 64 3.4 | 6.1, 8 x 8192 bf16 with eight rows each 16.2 | 12.3).
     const uint32_t few = parts * (s.teams > parts ? s.teams / parts : 1);
-    if (bwd && rows <= (s.lanes > 64 ? 4 : 8) * (int64_t)few) {
+    if (bwd && rows <= norm_few_rows(s.lanes, s.threads) * (int64_t)few) {
         s.direct = true;
         s.step = few;
         s.blocks = (s.step + s.teams - 1) / s.teams;
