@@ -326,27 +326,27 @@ int32_t fae_embbag_bwd_opts(fae_ctx *ctx, const fae_tables *hot_tables, float *c
  * [r*row_stride + p*width + c]: the pooled output with one row per table (n_parts tables of
  * dim `width`, each with its own weights), or any matrix (n_parts = 1).  A row stride is in
  * values and >= n_parts*width.  Values between the samples are neither read nor written.
- * Types: FAE_F32, FAE_BF16, FAE_F16 (two bytes each); x and y have the same type, or one of
- * them is FAE_F32 where a call says so.  Every sum, mean and product is fp32 whatever the types; a result is rounded
- * to its type once, to nearest even.  Buffers need the alignment of their values, nothing more
- * (widths, strides and addresses on 16 bytes are fastest).  An output may be the
- * input it has the shape of (same address, stride and type); every other overlap of a call's buffers is not
- * allowed, and refused with FAE_EINVAL where rows of input and output share bytes. */
+ * Types: FAE_F32, and FAE_BF16 and FAE_F16 of two bytes.  Every sum, mean and product is fp32
+ * whatever the types; a result is rounded to its type once, to nearest even.  Buffers need the
+ * alignment of their values, nothing more (widths, strides and addresses on 16 bytes are
+ * fastest).  An output may be the input that it has the shape of (same address, stride and
+ * type); every other overlap of a call's buffers is not allowed, and refused with FAE_EINVAL
+ * where rows of input and output share bytes. */
 #define FAE_F32 0
 #define FAE_BF16 1
 #define FAE_F16 2
 
 /* Dropout.  The generator is Philox4x32-10 (Salmon, Moraes, Dror, Shaw: "Parallel random
- * numbers: as easy as 1, 2, 3", 2011): the mask is made where it is needed and never stored, forward and
- * backward make the same one from the same seed and offset, and no value depends on how a kernel shares out the
- * work.  With R = r*n_parts + p and O = offset + (d_offset ? *d_offset : 0) modulo 2^64,
+ * numbers: as easy as 1, 2, 3", 2011): the mask is made where it is needed and never stored,
+ * forward and backward make the same one from the same seed and offset, and no value depends on
+ * how a kernel shares out the work.  With R = r*n_parts + p and O = offset + (d_offset ? *d_offset : 0) modulo 2^64,
  *   counter = (c >> 3, R, O low word, O high word), key = (seed low word, seed high word),
- * and the four words of the result are eight 16-bit numbers, the low half of a word first; number c & 7
- * belongs to value c.  With T = p * 65536 rounded to the nearest integer (ties to even), a value whose number is below T is
- * dropped (0, whatever it was), and every other is multiplied by 65536 / (65536 - T).  So p is kept to 2^-17:
- * 0 and 1 are taken (p = 1 drops everything), other p that would round to them are refused.  A caller
- * uses another offset for every call (or adds to *d_offset on the device between replays
- * of a captured step). */
+ * and the four words of the result are eight 16-bit numbers, the low half of a word first;
+ * number c & 7 belongs to value c.  With T = p * 65536 rounded to the nearest integer (ties to
+ * even), a value whose number is below T is dropped (0, whatever it was), and every other is
+ * multiplied by 65536 / (65536 - T).  So p is kept to 2^-17: 0 and 1 are taken (p = 1 drops
+ * everything), other p that would round to them are refused.  A caller uses another offset for
+ * every call (or adds to *d_offset on the device between replays of a captured step). */
 typedef struct {
     double p; /* share that is dropped, 0 <= p <= 1 */
     uint64_t seed;
@@ -357,8 +357,8 @@ typedef struct {
 /* Layer norm over the rows:
  *   h = (x - mean(x)) / sqrt(var(x) + eps) with the mean and the (biased) variance of the row's width values,
  *   y = gamma[p][c] * h + beta[p][c], then dropout if asked for.
- * A row of zeros (an empty bag) has h = 0, one of another value everywhere at most
- * 2^-45 of that value / sqrt(eps).  The sum of the squared deviations of a row has to be a number of fp32
+ * A row of zeros (an empty bag) has h = 0, one of another value everywhere at most 2^-38 of that
+ * value / sqrt(eps).  The sum of the squared deviations of a row has to be a number of fp32
  * (deviations below about 1e17). */
 typedef struct {
     int64_t n_rows;
@@ -374,19 +374,22 @@ typedef struct {
 /* y from x; drop may be NULL.  Nothing is kept for the backward but x.  Asynchronous. */
 int32_t fae_layer_norm_fwd(fae_ctx *ctx, const fae_norm *norm, const void *x, int64_t x_row_stride, void *y,
                            int64_t y_row_stride, const fae_drop *drop);
-/* The gradients of fae_layer_norm_fwd (beta is not read).  With g = gy through the same dropout (the same drop as in the forward):
+/* The gradients of fae_layer_norm_fwd (beta is not read).  With g = gy through the same dropout
+ * (the same drop as in the forward):
  *   gx = (a - mean(a) - h * mean(a * h)) / sqrt(var(x) + eps) with a = gamma * g, means over the row,
  *   dgamma[p][c] = sum over r of g * h,  dbeta[p][c] = sum over r of g.
- * dgamma and dbeta (device fp32[n_parts*width]) are overwritten (zeros if n_rows is 0); either may be NULL.  gx may be gy (same
- * address, stride and type) or x.  The sums are taken in an order that depends on the sizes alone, so a call's results are
- * the same every time.  Two calls that may overlap (two streams, two captured graphs) need a
- * workspace each.  Asynchronous. */
+ * dgamma and dbeta (device fp32[n_parts*width]) are overwritten (zeros if n_rows is 0); either
+ * may be NULL.  gx may be gy (same address, stride and type) or x.  The sums are taken in an
+ * order that depends on the sizes alone, so a call's results are the same every time.  ws is on
+ * 16 bytes; two calls that may overlap (two streams, two captured graphs) need one each.
+ * Asynchronous. */
 size_t fae_layer_norm_bwd_workspace_bytes(const fae_norm *norm);
 int32_t fae_layer_norm_bwd(fae_ctx *ctx, const fae_norm *norm, const void *x, int64_t x_row_stride, const void *gy,
                            int64_t gy_row_stride, void *gx, int64_t gx_row_stride, float *dgamma, float *dbeta,
                            const fae_drop *drop, void *ws, size_t ws_bytes);
-/* y = x through dropout, and its gradient gx = gy through the same dropout.  n_rows * n_parts < 2^32; n_parts * width <
- * 2^31; x and y have the same type or one of them is FAE_F32.  Asynchronous. */
+/* y = x through dropout, and its gradient gx = gy through the same dropout.  n_rows * n_parts <
+ * 2^32; n_parts * width < 2^31; x and y have the same type or one of them is FAE_F32.
+ * Asynchronous. */
 int32_t fae_dropout_fwd(fae_ctx *ctx, const fae_drop *drop, int64_t n_rows, int32_t n_parts, int32_t width, const void *x,
                         int32_t x_type, int64_t x_row_stride, void *y, int32_t y_type, int64_t y_row_stride);
 int32_t fae_dropout_bwd(fae_ctx *ctx, const fae_drop *drop, int64_t n_rows, int32_t n_parts, int32_t width, const void *gy,

@@ -310,10 +310,10 @@ __global__ __launch_bounds__(THREADS) void norm_fwd_kernel(NormArgs a)
     }
 }
 
-// The rows' gradient, and the team's sums of the weights' gradients in registers over all its rows.  DEPTH rows of a team are held:
-// the loads of the next DEPTH - 1 go out before the present one's sums are taken (into registers of their own, with no
-// copies between them, which would wait for the loads).  EARLY: a row's own registers are loaded again as soon as its values are taken.  All teams walk with one stride: rows in flight then lie side by side
-// (16 384 x 26 x 64 73 -> 67 us against a stretch of rows for every few workgroups).
+// The rows' gradient, and the team's sums of the weights' gradients in registers over all its rows.  DEPTH rows of a team are held: the
+// loads of the next DEPTH - 1 go out before the present one's sums are taken (into registers of their own, with no copies between them,
+// which would wait for the loads).  EARLY: a row's own registers are loaded again as soon as its values are taken.  All teams walk with
+// one stride: rows in flight then lie side by side (16 384 x 26 x 64 73 -> 67 us against a stretch of rows for every few workgroups).
 template <typename TX, typename TY, int LANES, int THREADS, bool WAVES, int NV, int DEPTH, bool EARLY, int ENDS, bool DROP>
 __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
 {
