@@ -102,9 +102,10 @@ static NormShape norm_shape(const fae_norm *n, bool bwd)
     // 6.5 and 7.0; 8 instead of 4 where it does not: 4096 x 1664 bf16 27.9 against 22.3, 512 x 8192 bf16 22.0 against 17.2).
     const int64_t per_team = bwd ? (s.teams > parts ? 2 : 4) : norm_fwd_rows(s.nv);
     int64_t blocks = (rows + per_team * s.teams - 1) / (per_team * s.teams);
-    // The backward's workgroups walk on, 512 lanes of them to a compute unit: with twice as many the rows in flight lie further apart
+    // The backward's workgroups walk on, up to 512 lanes of them to a compute unit: with twice as many the rows in flight lie further apart
     // and more sums go out (16 384 x 26 x 64 fp32 62 us | 67, 16 384 x 4096 147 | 156), with half as many too little is in flight (91, 154).
-    const int64_t most_blocks = bwd ? (s.threads > 512 ? 256 : 128 * 1024 / s.threads) : blocks;
+    // The same number for every compute unit: 341 workgroups of six waves took as long as 512 (16 384 x 6000 bf16 128 us | 180).
+    const int64_t most_blocks = bwd ? (s.threads > 256 ? 256 : 256 * (512 / s.threads)) : blocks;
     // Few rows: as many teams as one workgroup holds (or one per part) take them all, and their sums are the gradients, which saves a
     // launch.  Up to eight rows each, four where a team is whole waves (us with one launch | two: 128 x 64 fp32 5.5 | 6.3, 256 x 64
     // with 16 rows each 8.2 | 6.4, 16 x 256 4.2 | 6.1, 4 x 26 x 64 3.4 | 6.1, 8 x 8192 bf16 with eight rows each 16.2 | 12.3).
