@@ -221,10 +221,18 @@ __device__ __forceinline__ void norm_weights(const float *w, float none, const N
 #pragma unroll
             for (int e = 0; e < E; ++e)
                 out[j][e] = v[e];
-        } else { // columns that do not exist get the last one's
+        } else { // four at a time, as rows that end anywhere
+            const int ends = a.width < 4 ? FAE_SHORT : FAE_CROOKED;
 #pragma unroll
-            for (int e = 0; e < E; ++e)
-                out[j][e] = w[part * a.width + (at[j].col + e < a.width ? at[j].col + e : a.width - 1)];
+            for (int h = 0; h < E; h += 4) {
+                fae_place<4> p;
+                p.set(at[j].col + h, a.width);
+                float v[4];
+                fae_settle<float, 4, FAE_ANY>(fae_load<float, 4, FAE_ANY>(w + part * a.width, p, ends), p, ends, v);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    out[j][h + e] = v[e];
+            }
         }
         if constexpr (DROP) {
 #pragma unroll
