@@ -144,6 +144,10 @@ __device__ __forceinline__ void norm_row_masks(norm_mask<E> (&m)[NV], const fae_
         norm_masks<E>(m[j], m[j + 1], at[j].col, row, at[j + 1].col, row, offset, d);
 }
 
+// The first half of a lane's chunks exist and are whole, as a lane is only given two and more where its team has more than half of them.
+// (Teams of 64 lanes with NV chunks hold more than NV / 2 x 64; teams of w waves, w > 1, more than NV x 64 (w - 1).)
+template <int NV> constexpr bool norm_sure(int j) { return j < NV / 2; }
+
 template <typename TX> constexpr int norm_chunk() { return sizeof(TX) == 2 ? 8 : 4; } // values in 16 bytes of x
 
 // where a thread stands
@@ -181,16 +185,17 @@ __device__ __forceinline__ float norm_center(float (&v)[NV][E], const fae_place<
 #pragma unroll
         for (int e = 0; e < E; ++e)
             s += v[j][e];
-    const float m = team.sum(s) * a.inv_width;
+    float m = team.sum(s) * a.inv_width;
+    asm("" : "+v"(m)); // one value: not a product that is rounded for some chunks and fused into the difference for others
     float d1 = 0.f, d2 = 0.f;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            if constexpr (ENDS == FAE_ANY)
+            if (ENDS == FAE_ANY && !norm_sure<NV>(j))
                 v[j][e] = e < at[j].there ? v[j][e] - m : 0.f;
             else
-                v[j][e] -= ENDS == FAE_WHOLE || at[j].there > 0 ? m : 0.f; // an absent chunk's values are zeros
+                v[j][e] -= ENDS == FAE_WHOLE || norm_sure<NV>(j) || at[j].there > 0 ? m : 0.f; // an absent chunk's values are zeros
             d1 += v[j][e];
             d2 += v[j][e] * v[j][e];
         }
@@ -260,7 +265,7 @@ template <typename T, int E, int NV, int U, int ENDS, bool MAY_SHORT> struct nor
     {
 #pragma unroll
         for (int j = 0; j < NV; ++j)
-            fae_settle<T, E, ENDS>(raw[u][j], at[j], a.ends, v[j]);
+            fae_settle<T, E, ENDS>(raw[u][j], at[j], a.ends, v[j], norm_sure<NV>(j));
     }
 };
 
@@ -307,7 +312,7 @@ __global__ __launch_bounds__(THREADS) void norm_fwd_kernel(NormArgs a)
                     v[j][e] = v[j][e] * rstd * gamma[j][e] + beta[j][e];
                 if constexpr (DROP)
                     mask[u & 1][j].drop(v[j], a.drop);
-                fae_store<TY, E, ENDS>(y + u * a.y_step, v[j], at.at[j]);
+                fae_store<TY, E, ENDS>(y + u * a.y_step, v[j], at.at[j], norm_sure<NV>(j));
             }
         }
         row += U * a.step;
@@ -398,7 +403,7 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(NormArgs a)
 #pragma unroll
                 for (int e = 0; e < E; ++e)
                     g[j][e] = rstd * (g[j][e] - c1 - v[j][e] * c2);
-                fae_store<TX, E, ENDS>(gx, g[j], at.at[j]);
+                fae_store<TX, E, ENDS>(gx, g[j], at.at[j], norm_sure<NV>(j));
             }
             row += a.step;
             if (row >= end)

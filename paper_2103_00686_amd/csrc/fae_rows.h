@@ -67,7 +67,8 @@ static inline int32_t fae_row_end(int64_t width, int chunk, int64_t lanes_width)
 {
     return width == lanes_width ? FAE_WHOLE : (width < chunk ? FAE_SHORT : (width % chunk ? FAE_CROOKED : FAE_CHUNKS));
 }
-// ENDS: FAE_WHOLE, FAE_CHUNKS or FAE_ANY.  MAY_SHORT: a row may be shorter than a chunk (never where it has two)
+// ENDS: FAE_WHOLE, FAE_CHUNKS or FAE_ANY.  MAY_SHORT: a row may be shorter than a chunk (never where it has two).  sure: a chunk that is
+// known to be whole whatever the rows' end (a constant where it is true)
 template <typename T, int E, int ENDS, bool MAY_SHORT = true>
 __device__ __forceinline__ typename fae_vec<T, E>::type fae_load(const T *row, const fae_place<E> &at, int ends)
 {
@@ -80,12 +81,27 @@ __device__ __forceinline__ typename fae_vec<T, E>::type fae_load(const T *row, c
     }
     return *(const typename fae_vec<T, E>::loose *)(row + (ENDS == FAE_WHOLE ? at.col : at.from));
 }
-// what fae_load brought, as it belongs: zeros where the row has no values
+// what fae_load brought, as it belongs: zeros where the row has no values (a cut chunk gets them by being moved down)
 template <typename T, int E, int ENDS>
-__device__ __forceinline__ void fae_settle(typename fae_vec<T, E>::type v, const fae_place<E> &at, int ends, float (&out)[E])
+__device__ __forceinline__ void fae_settle(typename fae_vec<T, E>::type v, const fae_place<E> &at, int ends, float (&out)[E], bool sure = false)
 {
     static_assert(sizeof(v) == 8 || sizeof(v) == 16, "8 or 16 bytes");
-    if constexpr (ENDS == FAE_CHUNKS) {
+    if (ENDS != FAE_WHOLE && !sure) {
+        if (ENDS == FAE_ANY && ends == FAE_CROOKED && at.there > 0) {
+            const uint32_t sh = (at.col - at.from) * 8 * sizeof(T);
+            if constexpr (sizeof(v) == 8) {
+                v = __builtin_bit_cast(typename fae_vec<T, E>::type, __builtin_bit_cast(uint64_t, v) >> sh);
+            } else {
+                typedef uint64_t pair __attribute__((ext_vector_type(2)));
+                pair w = __builtin_bit_cast(pair, v);
+                const uint64_t lo = w[0], hi = w[1];
+                const uint32_t s = sh & 63;
+                const uint64_t h = hi >> s, l = (lo >> s) | ((hi << 1) << (63 - s));
+                w[0] = sh < 64 ? l : h;
+                w[1] = sh < 64 ? h : 0;
+                v = __builtin_bit_cast(typename fae_vec<T, E>::type, w);
+            }
+        }
         typedef uint32_t words __attribute__((ext_vector_type(sizeof(v) / 4)));
         words w = __builtin_bit_cast(words, v);
 #pragma unroll
@@ -93,34 +109,19 @@ __device__ __forceinline__ void fae_settle(typename fae_vec<T, E>::type v, const
             w[i] = at.there > 0 ? w[i] : 0u;
         v = __builtin_bit_cast(typename fae_vec<T, E>::type, w);
     }
-    if (ENDS == FAE_ANY && ends == FAE_CROOKED && at.there > 0) {
-        const uint32_t sh = (at.col - at.from) * 8 * sizeof(T);
-        if constexpr (sizeof(v) == 8) {
-            v = __builtin_bit_cast(typename fae_vec<T, E>::type, __builtin_bit_cast(uint64_t, v) >> sh);
-        } else {
-            typedef uint64_t pair __attribute__((ext_vector_type(2)));
-            pair w = __builtin_bit_cast(pair, v);
-            const uint64_t lo = w[0], hi = w[1];
-            const uint32_t s = sh & 63;
-            const uint64_t h = hi >> s, l = (lo >> s) | ((hi << 1) << (63 - s));
-            w[0] = sh < 64 ? l : h;
-            w[1] = sh < 64 ? h : 0;
-            v = __builtin_bit_cast(typename fae_vec<T, E>::type, w);
-        }
-    }
 #pragma unroll
     for (int e = 0; e < E; ++e)
-        out[e] = ENDS != FAE_ANY || e < at.there ? (float)v[e] : 0.f;
+        out[e] = (float)v[e];
 }
 
-template <typename T, int E, int ENDS> __device__ __forceinline__ void fae_store(T *row, const float (&v)[E], const fae_place<E> &at)
+template <typename T, int E, int ENDS> __device__ __forceinline__ void fae_store(T *row, const float (&v)[E], const fae_place<E> &at, bool sure = false)
 {
     T *p = row + at.col;
     typename fae_vec<T, E>::type o;
 #pragma unroll
     for (int e = 0; e < E; ++e)
         o[e] = (T)v[e];
-    if (ENDS == FAE_WHOLE || at.there == E) {
+    if (ENDS == FAE_WHOLE || sure || at.there == E) {
         *(typename fae_vec<T, E>::loose *)p = o;
     } else if (ENDS == FAE_ANY) {
 #pragma unroll
