@@ -368,16 +368,23 @@ class HotPath:
                      eps: float = 1e-5, drop: Optional[B.Drop] = None, out_dtype: torch.dtype = torch.float32,
                      pooling: int = B.FAE_POOL_SUM):
         """(pooled, y): the pooled rows of every table and their layer norm, dropped out, as the dense layers read it.
-        gamma and beta: [tables, dim].  ``backward_norm_sgd`` takes pooled."""
+        gamma and beta: [tables, dim].  ``backward_norm_sgd`` takes pooled, and the same pooling."""
         pooled = self.forward(hb, pooling=pooling)
         return pooled, self.layer_norm(pooled, gamma, beta, eps, drop, out_dtype)
 
     def backward_norm_sgd(self, hb: HotBatch, pooled: torch.Tensor, gy: torch.Tensor, lr: float,
-                          gamma: Optional[torch.Tensor] = None, eps: float = 1e-5, drop: Optional[B.Drop] = None):
-        """From y's gradient to the hot tables (sum pooling, SGD), with the forward's gamma, eps and drop; returns
+                          gamma: Optional[torch.Tensor] = None, eps: float = 1e-5, drop: Optional[B.Drop] = None,
+                          pooling: int = B.FAE_POOL_SUM):
+        """From y's gradient to the hot tables (SGD), with the forward's gamma, eps, drop and pooling; returns
         (dgamma, dbeta).  pooled is overwritten with its gradient."""
+        if pooling not in (B.FAE_POOL_SUM, B.FAE_POOL_MEAN):
+            raise ValueError(f"unknown pooling {pooling}")
         _, dgamma, dbeta = self.layer_norm_backward(pooled, gy, gamma, eps, drop, out=pooled)
-        self.backward_sgd(hb, pooled, lr)
+        if pooling == B.FAE_POOL_SUM:
+            self.backward_sgd(hb, pooled, lr)
+        else:
+            B.fae_embbag_bwd_opts(self.ctx, self.hot_tables, self.hotW, hb.batch(), pooled, self.nt * self.dim, lr,
+                                  self.bwd_workspace(hb), pooling)
         return dgamma, dbeta
 
     # pre-marshalled forms of the four, for tight loops: zero-argument callables
