@@ -6,7 +6,7 @@ mini-batch forward / backward / SGD).  No arithmetic of the method happens here.
 from __future__ import annotations
 
 from dataclasses import dataclass
-from typing import List, Optional, Sequence
+from typing import Dict, List, Optional, Sequence
 
 import torch
 
@@ -70,7 +70,11 @@ def step_sequence(rows: Sequence[int], dim: int, one_hot: bool, n_samples: int, 
 class HotPath:
     def __init__(self, rows: Sequence[int], dim: int, device: int = 0, stream: Optional[int] = None):
         """stream: a hipStream_t handle (e.g. ``torch.cuda.Stream().cuda_stream``); default is
-        torch's current stream at construction.  Every library call is queued there."""
+        torch's current stream at construction.  Every library call is queued there; outputs and workspaces are
+        allocated on torch's current stream, so a caller who works on another one orders the two.
+
+        The workspace of the sparse update is one for all steps of a HotPath (presort leaves the sorted pairs in it), as are
+        the tables that they change: graphs of such steps overlap neither each other nor eager steps."""
         self.dev = torch.device("cuda", device)
         self.ctx = B.Context(device, stream)
         self.tables = B.Tables(list(rows), dim)
@@ -81,16 +85,16 @@ class HotPath:
         self.profiled_samples = 0
         self.remap = self.hot_ids = self.hotW = None
         self.n_hot: List[int] = []
-        self._ws = {}
-        self._norm_ws: List[torch.Tensor] = []
+        self._ws: Dict[str, List[torch.Tensor]] = {}
 
     # -- plumbing -----------------------------------------------------------------
     def _workspace(self, name: str, nbytes: int) -> torch.Tensor:
-        ws = self._ws.get(name)
-        if ws is None or ws.numel() < nbytes:
-            ws = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=self.dev)
-            self._ws[name] = ws
-        return ws
+        """Grows by half at least and keeps the outgrown ones: a captured step, or one still queued, may use them."""
+        held = self._ws.setdefault(name, [])
+        if not held or held[-1].numel() < nbytes:
+            least = held[-1].numel() * 3 // 2 if held else 256
+            held.append(torch.empty(max(nbytes, least), dtype=torch.uint8, device=self.dev))
+        return held[-1]
 
     @property
     def hot_tables(self) -> B.Tables:
@@ -321,11 +325,7 @@ class HotPath:
         return B.Norm(x.shape[0], parts, x.shape[-1], gamma, beta, eps, x.dtype, y_dtype)
 
     def _norm_workspace(self, nbytes: int) -> torch.Tensor:
-        """Grows by doubling and keeps the outgrown ones: a captured step, or one still queued, may use them."""
-        if not self._norm_ws or self._norm_ws[-1].numel() < nbytes:
-            least = 2 * self._norm_ws[-1].numel() if self._norm_ws else 1 << 16
-            self._norm_ws.append(torch.empty(max(nbytes, least), dtype=torch.uint8, device=self.dev))
-        return self._norm_ws[-1]
+        return self._workspace("norm", max(nbytes, 1 << 16))
 
     def layer_norm(self, x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None,
                    eps: float = 1e-5, drop: Optional[B.Drop] = None, out_dtype: Optional[torch.dtype] = None,
@@ -394,7 +394,8 @@ class HotPath:
     def prepare_layer_norm_backward(self, norm: B.Norm, x: torch.Tensor, gy: torch.Tensor, gx: torch.Tensor,
                                     dgamma: Optional[torch.Tensor] = None, dbeta: Optional[torch.Tensor] = None,
                                     drop: Optional[B.Drop] = None):
-        """With a workspace of its own, so that captured steps share none."""
+        """With a workspace of its own, so that captured steps share none; the callable holds it, as it holds the tensors,
+        and has to live as long as a graph that captured a call of it."""
         ws = torch.empty(max(B.fae_layer_norm_bwd_workspace_bytes(norm), 256), dtype=torch.uint8, device=self.dev)
         return B.prepare_layer_norm_bwd(self.ctx, norm, x, gy, gx, dgamma, dbeta, ws, drop)
 

@@ -1,0 +1,47 @@
+"""Captured steps and their workspaces: a step outlives the sparse update's outgrown workspace."""
+import pytest
+import torch
+
+from paper_2103_00686_amd import binding as B
+from test_gpu_norm_step import _batch, _tables
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("pooling", [B.FAE_POOL_SUM, B.FAE_POOL_MEAN])
+def test_a_captured_step_outlives_the_workspaces(pooling):
+    rows, S, lr, dim = [500, 90, 40], 200, 0.05, 32
+    st = torch.cuda.Stream()
+    hp = _tables(rows, dim, st.cuda_stream)
+    hb, big = _batch(rows, S, 1, 5), _batch(rows, 60_000, 2, 5)
+    gy = torch.randn((S, 3, dim), device="cuda")
+    torch.cuda.synchronize()
+    start = [w.clone() for w in hp.hotW]
+
+    def step():
+        pooled, y = hp.forward_norm(hb, pooling=pooling)
+        return (y, *hp.backward_norm_sgd(hb, pooled, gy, lr, pooling=pooling))
+    first = step()
+    hp.sync()
+    want = [t.clone() for t in (*first, *hp.hotW)]
+    torch.cuda.synchronize()
+    small = hp.bwd_workspace(hb).data_ptr()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=st):
+        got = step()
+    torch.cuda.synchronize()
+    pooled, y = hp.forward_norm(big, pooling=pooling)
+    hp.sync()
+    hp.backward_norm_sgd(big, pooled, torch.ones_like(y), lr, pooling=pooling)
+    hp.sync()
+    assert hp.bwd_workspace(big).data_ptr() != small
+    fill = [torch.full((1 << 20,), float("nan"), device="cuda") for _ in range(64)]
+    for _ in range(3):
+        for w, s in zip(hp.hotW, start):
+            w.copy_(s)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip((*got, *hp.hotW), want):
+            assert torch.equal(a, b)
+    assert all(bool(torch.isnan(f).all()) for f in fill)
