@@ -270,6 +270,7 @@ class Context:
         if stream is None:
             stream = torch.cuda.current_stream(device).cuda_stream
         self.device = device
+        self.stream = int(stream)
         self._h = C.c_void_p()
         rc = lib.fae_create(C.byref(self._h), C.c_int32(device), C.c_void_p(stream))
         if rc != FAE_OK:

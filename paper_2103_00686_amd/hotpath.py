@@ -73,8 +73,9 @@ class HotPath:
         torch's current stream at construction.  Every library call is queued there; outputs and workspaces are
         allocated on torch's current stream, so a caller who works on another one orders the two.
 
-        The workspace of the sparse update is one for all steps of a HotPath (presort leaves the sorted pairs in it), as are
-        the tables that they change: graphs of such steps overlap neither each other nor eager steps."""
+        Steps captured into graphs: ``layer_norm_backward`` has a workspace of its own in each graph.  The sparse
+        update's is one for all steps of a HotPath (presort leaves the sorted pairs in it), as are the tables that they
+        change: graphs of such steps overlap neither each other nor eager steps."""
         self.dev = torch.device("cuda", device)
         self.ctx = B.Context(device, stream)
         self.tables = B.Tables(list(rows), dim)
@@ -325,7 +326,14 @@ class HotPath:
         return B.Norm(x.shape[0], parts, x.shape[-1], gamma, beta, eps, x.dtype, y_dtype)
 
     def _norm_workspace(self, nbytes: int) -> torch.Tensor:
-        return self._workspace("norm", max(nbytes, 1 << 16))
+        """One for all eager calls, which the context's stream puts in order.  A captured call has its own, in its graph's
+        memory: graphs may be replayed beside each other and beside eager calls."""
+        if not torch.cuda.is_current_stream_capturing():
+            return self._workspace("norm", max(nbytes, 1 << 16))
+        ws = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=self.dev)
+        if torch.cuda.current_stream(self.dev).cuda_stream != self.ctx.stream:  # it is dropped before the kernels there have run
+            ws.record_stream(torch.cuda.ExternalStream(self.ctx.stream, device=self.dev))
+        return ws
 
     def layer_norm(self, x: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None,
                    eps: float = 1e-5, drop: Optional[B.Drop] = None, out_dtype: Optional[torch.dtype] = None,

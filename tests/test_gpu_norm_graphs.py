@@ -1,8 +1,10 @@
-"""Captured steps and their workspaces: a step outlives the sparse update's outgrown workspace."""
+"""Captured steps and their workspaces: a step outlives the sparse update's outgrown workspace, and graphs of layer norm's
+backward run beside each other and beside eager calls."""
 import pytest
 import torch
 
 from paper_2103_00686_amd import binding as B
+from paper_2103_00686_amd.hotpath import HotPath
 from test_gpu_norm_step import _batch, _tables
 
 pytestmark = pytest.mark.gpu
@@ -45,3 +47,45 @@ def test_a_captured_step_outlives_the_workspaces(pooling):
         for a, b in zip((*got, *hp.hotW), want):
             assert torch.equal(a, b)
     assert all(bool(torch.isnan(f).all()) for f in fill)
+
+
+@pytest.mark.parametrize("forked", [False, True])
+def test_graphs_beside_each_other(forked):
+    """Two graphs of one HotPath on two streams, an eager call between them.  forked: the capture starts on another stream than
+    the HotPath's, which joins it."""
+    st, other = torch.cuda.Stream(), torch.cuda.Stream()
+    hp = HotPath([1], 4, stream=st.cuda_stream)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(3)
+    shapes = [(3000, 26, 64), (2000, 1, 1000), (5000, 3, 100)]
+    x, gy = ([torch.randn(s, device="cuda", generator=gen) for s in shapes] for _ in range(2))
+    torch.cuda.synchronize()
+    want = [hp.layer_norm_backward(x[i], gy[i]) for i in range(3)]
+    hp.sync()
+    graphs, got = [], []
+    for i in range(2):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[i], stream=other if forked else st):
+            if forked:
+                st.wait_stream(other)
+            got.append([hp.layer_norm_backward(x[i], gy[i]) for _ in range(4)])
+            if forked:
+                other.wait_stream(st)
+    lanes = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(3):
+        for outs in got:
+            for out in outs:
+                for t in out:
+                    t.fill_(float("nan"))
+        torch.cuda.synchronize()
+        for graph, lane in zip(graphs, lanes):
+            with torch.cuda.stream(lane):
+                graph.replay()
+        eager = hp.layer_norm_backward(x[2], gy[2])
+        torch.cuda.synchronize()
+        for i in range(2):
+            for out in got[i]:
+                for a, b in zip(out, want[i]):
+                    assert torch.equal(a, b)
+        for a, b in zip(eager, want[2]):
+            assert torch.equal(a, b)
