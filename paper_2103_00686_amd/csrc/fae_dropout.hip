@@ -61,7 +61,8 @@ struct DropArgs {
     const void *x;
     void *y;
     int64_t x_stride, y_stride;
-    int64_t n_groups;     // groups of eight values in all rows
+    int64_t first;        // the launch's first group of eight values
+    int64_t n_groups;     // groups in all rows
     uint32_t per_row;     // of them in a row
     uint32_t per_row_inv; // 2^18 / per_row, rounded up (for rows of fewer than DROP_TILE groups)
     uint32_t n_parts, width;
@@ -70,6 +71,7 @@ struct DropArgs {
 };
 
 #define DROP_TILE 256
+#define DROP_LAUNCH (1LL << 31) // groups of one launch, a thread each: a grid holds fewer than 2^32 threads
 
 // A thread takes a group of eight values, a workgroup DROP_TILE consecutive groups: one division per workgroup finds its first row,
 // and a group's row is a small number of rows on: none or one where rows are as long as the tile, else a product with
@@ -81,7 +83,7 @@ struct DropArgs {
 template <typename TX, typename TY, int ENDS> __global__ __launch_bounds__(DROP_TILE) void dropout_kernel(DropArgs a)
 {
     constexpr int E = sizeof(TX) == 2 ? 8 : 4; // values in 16 bytes
-    const int64_t base = (int64_t)blockIdx.x * DROP_TILE;
+    const int64_t base = a.first + (int64_t)blockIdx.x * DROP_TILE;
     if (base + threadIdx.x >= a.n_groups)
         return;
     const int64_t row0 = fae_div_small(base, a.per_row);
@@ -156,12 +158,14 @@ static int32_t dropout_impl(fae_ctx *ctx, const char *who, const fae_drop *drop,
         a.n_parts = 1;
         a.x_stride = a.y_stride = width;
     }
-    const int64_t blocks = (a.n_groups + DROP_TILE - 1) / DROP_TILE;
-    if (blocks > 2147483647LL)
-        return fae_fail(ctx, FAE_EINVAL, "%s: too many values for one launch", who);
+    if (a.n_groups > (1LL << 39)) // 4 TiB and more: no such buffers
+        return fae_fail(ctx, FAE_EINVAL, "%s: too many values", who);
     FAE_HIP(ctx, hipSetDevice(ctx->device));
     fae_ktimer kt(ctx, FAE_K_DROPOUT);
-    const dim3 grid((unsigned)blocks), block(256);
+    const dim3 block(DROP_TILE);
+    for (a.first = 0; a.first < a.n_groups; a.first += DROP_LAUNCH) {
+        const int64_t groups = a.n_groups - a.first < DROP_LAUNCH ? a.n_groups - a.first : DROP_LAUNCH;
+        const dim3 grid((unsigned)((groups + DROP_TILE - 1) / DROP_TILE));
 #define DROP_CASE(TX, TX_, TY, TY_)                                                              \
     if (x.type == TX && y.type == TY) {                                                          \
         if (a.ends == FAE_WHOLE)                                                                 \
@@ -169,15 +173,16 @@ static int32_t dropout_impl(fae_ctx *ctx, const char *who, const fae_drop *drop,
         else                                                                                     \
             FAE_LAUNCH(ctx, (dropout_kernel<TX_, TY_, FAE_ANY>), grid, block, 0, ctx->stream, a);  \
     }
-    DROP_CASE(FAE_F32, float, FAE_F32, float)
-    DROP_CASE(FAE_F32, float, FAE_BF16, fae_bf16)
-    DROP_CASE(FAE_F32, float, FAE_F16, fae_f16)
-    DROP_CASE(FAE_BF16, fae_bf16, FAE_F32, float)
-    DROP_CASE(FAE_F16, fae_f16, FAE_F32, float)
-    DROP_CASE(FAE_BF16, fae_bf16, FAE_BF16, fae_bf16)
-    DROP_CASE(FAE_F16, fae_f16, FAE_F16, fae_f16)
+        DROP_CASE(FAE_F32, float, FAE_F32, float)
+        DROP_CASE(FAE_F32, float, FAE_BF16, fae_bf16)
+        DROP_CASE(FAE_F32, float, FAE_F16, fae_f16)
+        DROP_CASE(FAE_BF16, fae_bf16, FAE_F32, float)
+        DROP_CASE(FAE_F16, fae_f16, FAE_F32, float)
+        DROP_CASE(FAE_BF16, fae_bf16, FAE_BF16, fae_bf16)
+        DROP_CASE(FAE_F16, fae_f16, FAE_F16, fae_f16)
 #undef DROP_CASE
-    FAE_LAUNCH_CHECK(ctx);
+        FAE_LAUNCH_CHECK(ctx);
+    }
     return FAE_OK;
 }
 
