@@ -127,6 +127,15 @@ static NormShape norm_shape(const fae_norm *n, bool bwd)
     return s;
 }
 
+// Samples of one forward launch: 2^21 workgroups of up to 1024 lanes, as a grid holds fewer than 2^32 threads
+static int64_t norm_launch_samples(const fae_norm *n)
+{
+    fae_norm one = *n;
+    one.n_rows = 1;
+    const NormShape s = norm_shape(&one, false); // how teams hold a row depends on the row alone
+    return ((int64_t)norm_fwd_rows(s.nv) * s.teams << 21) / n->n_parts;
+}
+
 static void norm_place_rows(const NormShape &s, NormArgs *a)
 {
     const int64_t samples = s.step / a->n_parts;
@@ -183,19 +192,26 @@ extern "C" int32_t fae_layer_norm_fwd(fae_ctx *ctx, const fae_norm *norm, const 
         rc = fae_check_overlap(ctx, who, by, bx, norm->n_rows, row);
     if (rc != FAE_OK)
         return rc;
-    a.x = x;
-    a.y = y;
     a.x_stride = x_row_stride;
     a.y_stride = y_row_stride;
     FAE_HIP(ctx, hipSetDevice(ctx->device));
     fae_ktimer kt(ctx, FAE_K_NORM);
-    const NormShape s = norm_shape(norm, false);
-    norm_place_rows(s, &a);
-    if (norm->x_type == FAE_F32)
-        norm_fwd_by_type(ctx, norm, s, a);
-    else
-        norm_fwd16_by_type(ctx, norm, s, a);
-    FAE_LAUNCH_CHECK(ctx);
+    fae_norm some = *norm; // of as many samples as a launch takes
+    const int64_t most = norm_launch_samples(norm);
+    for (int64_t first = 0; first < norm->n_rows; first += most) {
+        some.n_rows = norm->n_rows - first < most ? norm->n_rows - first : most;
+        a.x = (const char *)x + first * x_row_stride * fae_type_size(norm->x_type);
+        a.y = (char *)y + first * y_row_stride * fae_type_size(norm->y_type);
+        a.row0 = (uint32_t)(first * a.n_parts);
+        a.n_rows = (uint32_t)(some.n_rows * a.n_parts);
+        const NormShape s = norm_shape(&some, false);
+        norm_place_rows(s, &a);
+        if (norm->x_type == FAE_F32)
+            norm_fwd_by_type(ctx, norm, s, a);
+        else
+            norm_fwd16_by_type(ctx, norm, s, a);
+        FAE_LAUNCH_CHECK(ctx);
+    }
     return FAE_OK;
 }
 

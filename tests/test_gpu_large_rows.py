@@ -80,3 +80,38 @@ def test_dropout_of_long_rows_past_a_grid(hp):
         cols = np.unique(np.concatenate([rng.integers(0, width, 4000), np.arange(100), width - 1 - np.arange(100)]))
         got = x[r][torch.from_numpy(cols).cuda()].float().cpu().numpy()
         assert np.array_equal(got, np.where(_numbers(np.full(len(cols), r), cols, seed, 9) < 16384, 0.0, four))
+
+
+# More workgroups than one grid takes: teams of two lanes (four rows each at a time), of two waves with one row at a time, several parts
+# whose number does not divide the teams.
+@pytest.mark.parametrize("dtype,rows,parts,width,p", [(BF16, (1 << 30) + 777, 1, 2, 0.0), (BF16, (1 << 31) - 1, 1, 1, 0.5), (BF16, (1 << 30) // 3 + 5000, 3, 3, 0.25),
+                                                      (BF16, (1 << 25) + 99, 1, 264, 0.0), (torch.float32, (1 << 21) + 1234, 1, 1028, 0.25)])
+def test_layer_norm_past_a_grid(hp, dtype, rows, parts, width, p):
+    """Every row is what a call on a few rows gives, and is dropped as dropout alone drops it."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(width)
+    x = torch.empty((rows, parts * width), dtype=dtype, device="cuda")
+    x.uniform_(-3, 3, generator=gen)
+    x = x.view(rows, parts, width)
+    gamma, beta = (torch.randn((parts, width), device="cuda", generator=gen) for _ in range(2))
+    beta += torch.where(beta < 0, -40.0, 40.0)  # no kept value is zero: |gamma h| < 40, as |h| < 2 for uniform values
+    drop = B.Drop(p, 21, 4) if p > 0 else None
+    y = torch.full_like(x, float("nan"))
+    hp.layer_norm(x, gamma, beta, drop=drop, out=y)
+    hp.sync()
+    flat = y.view(-1)
+    assert not any(bool(flat[i:i + PIECE].isnan().any()) for i in range(0, flat.numel(), PIECE))
+    if drop is not None:
+        mask = hp.dropout(torch.ones_like(x), drop)
+        hp.sync()
+        mask = mask.view(-1)
+        for i in range(0, flat.numel(), PIECE):
+            assert torch.equal(flat[i:i + PIECE] != 0, mask[i:i + PIECE] != 0)
+    step = max(1, PIECE // (parts * width))
+    scale = torch.tensor(65536 / (65536 - round(65536 * p)), device="cuda")  # dropout's factor is in the weights
+    for i in range(0, rows, step):
+        part = x[i:i + step]
+        want = hp.layer_norm(part, gamma * scale, beta * scale)
+        hp.sync()
+        got = y[i:i + step]
+        assert torch.equal(got, want) if drop is None else bool(((got == want) | (got == 0)).all())
