@@ -146,6 +146,12 @@ static void norm_place_rows(const NormShape &s, NormArgs *a)
     a->ends = fae_row_end(a->width, s.chunk, (int64_t)s.lanes * s.nv * s.chunk);
 }
 
+// n_rows * n_parts within [0, 2^31), for 1 to FAE_MAX_TABLES parts
+static bool norm_rows_fit(const fae_norm *n)
+{
+    return n->n_rows >= 0 && n->n_rows < 2147483648LL && n->n_rows * n->n_parts < 2147483648LL;
+}
+
 static int32_t norm_check(fae_ctx *ctx, const char *who, const fae_norm *n, const fae_drop *drop, NormArgs *a)
 {
     if (!ctx)
@@ -155,7 +161,7 @@ static int32_t norm_check(fae_ctx *ctx, const char *who, const fae_norm *n, cons
     if (n->n_parts < 1 || n->n_parts > FAE_MAX_TABLES || n->width < 1 || n->width > FAE_NORM_MAX_WIDTH)
         return fae_fail(ctx, FAE_EINVAL, "%s: n_parts=%d outside [1,%d] or width=%d outside [1,%d]", who, n->n_parts, FAE_MAX_TABLES,
                         n->width, FAE_NORM_MAX_WIDTH);
-    if (n->n_rows < 0 || n->n_rows >= 2147483648LL / n->n_parts)
+    if (!norm_rows_fit(n))
         return fae_fail(ctx, FAE_EINVAL, "%s: n_rows=%lld of %d parts outside [0,2^31)", who, (long long)n->n_rows, n->n_parts);
     if (n->x_type < FAE_F32 || n->x_type > FAE_F16 || n->y_type < FAE_F32 || n->y_type > FAE_F16 ||
         (n->x_type != n->y_type && n->x_type != FAE_F32))
@@ -218,8 +224,8 @@ extern "C" int32_t fae_layer_norm_fwd(fae_ctx *ctx, const fae_norm *norm, const 
 // Both sums of every workgroup, a row per team or part; at least 256 bytes
 extern "C" size_t fae_layer_norm_bwd_workspace_bytes(const fae_norm *norm)
 {
-    if (!norm || norm->n_rows < 0 || norm->n_parts < 1 || norm->n_parts > FAE_MAX_TABLES || norm->width < 1 ||
-        norm->width > FAE_NORM_MAX_WIDTH || norm->n_rows >= 2147483648LL / norm->n_parts || norm->x_type < FAE_F32 || norm->x_type > FAE_F16)
+    if (!norm || norm->n_parts < 1 || norm->n_parts > FAE_MAX_TABLES || norm->width < 1 || norm->width > FAE_NORM_MAX_WIDTH ||
+        !norm_rows_fit(norm) || norm->x_type < FAE_F32 || norm->x_type > FAE_F16)
         return 0;
     const NormShape s = norm_shape(norm, true);
     return s.direct ? 256 : 2 * fae_align_up((size_t)s.n_sums * norm->n_parts * s.pitch * sizeof(float), 256);

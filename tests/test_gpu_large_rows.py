@@ -115,3 +115,24 @@ def test_layer_norm_past_a_grid(hp, dtype, rows, parts, width, p):
         hp.sync()
         got = y[i:i + step]
         assert torch.equal(got, want) if drop is None else bool(((got == want) | (got == 0)).all())
+
+
+@pytest.mark.parametrize("parts", [1, 3])
+def test_backward_of_the_most_rows(hp, parts):
+    """n_rows * n_parts as near to 2^31 as it goes; gradients of zero but for a few samples at the end, so that the sums are theirs."""
+    rows, width, last = ((1 << 31) - 1) // parts, 2, 700
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(parts)
+    x = torch.empty((rows, parts, width), dtype=BF16, device="cuda").uniform_(-3, 3, generator=gen)
+    gy = torch.zeros_like(x)
+    gy[-last:] = torch.randn((last, parts, width), device="cuda", generator=gen).to(BF16)
+    gamma = torch.randn((parts, width), device="cuda", generator=gen)
+    gx = torch.full_like(x, float("nan"))
+    _, dgamma, dbeta = hp.layer_norm_backward(x, gy, gamma, out=gx)
+    hp.sync()
+    (rx, rg, rb), (tx, tg, tb) = R.NormRef(x[-last:], gamma, None, 1e-5).backward(gy[-last:], BF16)
+    R.assert_within(gx[-last:], rx, tx, "gx")
+    R.assert_within(dgamma.reshape(parts, width), rg, tg, "dgamma")
+    R.assert_within(dbeta.reshape(parts, width), rb, tb, "dbeta")
+    flat = gx[:-last].reshape(-1)
+    assert not any(bool((flat[i:i + PIECE] != 0).any()) for i in range(0, flat.numel(), PIECE))
