@@ -381,8 +381,9 @@ int32_t fae_layer_norm_fwd(fae_ctx *ctx, const fae_norm *norm, const void *x, in
  * dgamma and dbeta (device fp32[n_parts*width]) are overwritten (zeros if n_rows is 0); either
  * may be NULL.  gx may be gy (same address, stride and type) or x.  The sums are taken in an
  * order that depends on the sizes alone, so a call's results are the same every time.  ws is on
- * 16 bytes; two calls that may overlap (two streams, two captured graphs) need one each.
- * Asynchronous. */
+ * 16 bytes, and needed also where dgamma and dbeta are NULL.  Its size does not fall with n_rows: one for the
+ * largest batch is enough for the others.  Two calls that may overlap (two streams, two captured graphs)
+ * need one each.  Asynchronous. */
 size_t fae_layer_norm_bwd_workspace_bytes(const fae_norm *norm);
 int32_t fae_layer_norm_bwd(fae_ctx *ctx, const fae_norm *norm, const void *x, int64_t x_row_stride, const void *gy,
                            int64_t gy_row_stride, void *gx, int64_t gx_row_stride, float *dgamma, float *dbeta,

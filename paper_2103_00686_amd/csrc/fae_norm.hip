@@ -75,6 +75,18 @@ static bool norm_wide_workgroup(int64_t rows, uint32_t parts, int lanes)
     return rows >= 2LL * 512 * teams || (rows > few * norm_few_rows(lanes, 256) && rows <= few_wide * norm_few_rows(lanes, 512));
 }
 
+// Rows of a team at least, backward: fewer where a workgroup adds up its teams' sums before it writes them (2 and 4, us: 717 x 16
+// 6.5 and 7.0; 8 instead of 4 where it does not: 4096 x 1664 bf16 27.9 against 22.3, 512 x 8192 bf16 22.0 against 17.2).
+static int64_t norm_bwd_rows(uint32_t teams, uint32_t parts) { return teams > parts ? 2 : 4; }
+
+// The backward's workgroups walk on, up to 512 lanes of them to a compute unit: with twice as many the rows in flight lie further apart
+// and more sums go out (16 384 x 26 x 64 fp32 62 us | 67, 16 384 x 4096 147 | 156), with half as many too little is in flight (91, 154).
+// The same number for every compute unit: 341 workgroups of six waves took as long as 512 (16 384 x 6000 bf16 128 us | 180).
+static int64_t norm_bwd_most_blocks(uint32_t threads) { return threads > 256 ? 256 : 256 * (512 / threads); }
+
+// workgroups whose teams are a multiple of the parts
+static uint32_t norm_whole_blocks(uint32_t teams, uint32_t parts) { return parts / norm_gcd(parts, teams); }
+
 static NormShape norm_shape(const fae_norm *n, bool bwd)
 {
     NormShape s;
@@ -95,17 +107,12 @@ static NormShape norm_shape(const fae_norm *n, bool bwd)
     const uint32_t parts = n->n_parts;
     s.threads = s.lanes > 64 ? s.lanes : bwd && norm_wide_workgroup(rows, parts, s.lanes) ? 512 : 256;
     s.teams = s.threads / s.lanes;
-    const uint32_t whole = parts / norm_gcd(parts, s.teams); // workgroups whose teams are a multiple of the parts
+    const uint32_t whole = norm_whole_blocks(s.teams, parts);
     s.pitch = (n->width + 3) / 4 * 4;
     s.part_rows = s.teams > parts ? parts : s.teams;
-    // Rows of a team at least.  Backward: fewer where a workgroup adds up its teams' sums before it writes them (2 and 4, us: 717 x 16
-    // 6.5 and 7.0; 8 instead of 4 where it does not: 4096 x 1664 bf16 27.9 against 22.3, 512 x 8192 bf16 22.0 against 17.2).
-    const int64_t per_team = bwd ? (s.teams > parts ? 2 : 4) : norm_fwd_rows(s.nv);
+    const int64_t per_team = bwd ? norm_bwd_rows(s.teams, parts) : norm_fwd_rows(s.nv);
     int64_t blocks = (rows + per_team * s.teams - 1) / (per_team * s.teams);
-    // The backward's workgroups walk on, up to 512 lanes of them to a compute unit: with twice as many the rows in flight lie further apart
-    // and more sums go out (16 384 x 26 x 64 fp32 62 us | 67, 16 384 x 4096 147 | 156), with half as many too little is in flight (91, 154).
-    // The same number for every compute unit: 341 workgroups of six waves took as long as 512 (16 384 x 6000 bf16 128 us | 180).
-    const int64_t most_blocks = bwd ? (s.threads > 256 ? 256 : 256 * (512 / s.threads)) : blocks;
+    const int64_t most_blocks = bwd ? norm_bwd_most_blocks(s.threads) : blocks;
     // Few rows: as many teams as one workgroup holds (or one per part) take them all, and their sums are the gradients, which saves a
     // launch.  Up to eight rows each, four where a team is whole waves (us with one launch | two: 128 x 64 fp32 5.5 | 6.3, 256 x 64
     // with 16 rows each 8.2 | 6.4, 16 x 256 4.2 | 6.1, 4 x 26 x 64 3.4 | 6.1, 8 x 8192 bf16 with eight rows each 16.2 | 12.3).
@@ -221,14 +228,28 @@ extern "C" int32_t fae_layer_norm_fwd(fae_ctx *ctx, const fae_norm *norm, const 
     return FAE_OK;
 }
 
-// Both sums of every workgroup, a row per team or part; at least 256 bytes
+// Both sums of every workgroup, a row per team or part; at least 256 bytes.  More rows may take fewer workgroups (a last one's teams rounded
+// up to the parts, workgroups of 512 lanes instead of 256): the size is what any number of rows up to these would need, so that it does not fall.
 extern "C" size_t fae_layer_norm_bwd_workspace_bytes(const fae_norm *norm)
 {
     if (!norm || norm->n_parts < 1 || norm->n_parts > FAE_MAX_TABLES || norm->width < 1 || norm->width > FAE_NORM_MAX_WIDTH ||
         !norm_rows_fit(norm) || norm->x_type < FAE_F32 || norm->x_type > FAE_F16)
         return 0;
     const NormShape s = norm_shape(norm, true);
-    return s.direct ? 256 : 2 * fae_align_up((size_t)s.n_sums * norm->n_parts * s.pitch * sizeof(float), 256);
+    if (s.direct)
+        return 256;
+    const int64_t rows = norm->n_rows * norm->n_parts;
+    const uint32_t parts = norm->n_parts;
+    int64_t sums = 0; // rows of them, of all parts
+    for (uint32_t threads = s.lanes > 64 ? s.threads : 256; threads <= (s.lanes > 64 ? s.threads : 512u); threads += 256) {
+        const uint32_t teams = threads / s.lanes, whole = norm_whole_blocks(teams, parts);
+        const int64_t per = norm_bwd_rows(teams, parts) * teams, most = norm_bwd_most_blocks(threads);
+        int64_t blocks = (rows + per - 1) / per;
+        blocks = ((blocks < most ? blocks : most) + whole - 1) / whole * whole;
+        const int64_t n = blocks * (teams > parts ? parts : teams);
+        sums = n > sums ? n : sums;
+    }
+    return 2 * fae_align_up((size_t)sums * s.pitch * sizeof(float), 256);
 }
 
 extern "C" int32_t fae_layer_norm_bwd(fae_ctx *ctx, const fae_norm *norm, const void *x, int64_t x_row_stride, const void *gy,

@@ -1,5 +1,5 @@
-"""Captured steps and their workspaces: a step outlives the sparse update's outgrown workspace, and graphs of layer norm's
-backward run beside each other and beside eager calls."""
+"""Workspaces in use: a captured step outlives the sparse update's outgrown one, graphs of layer norm's backward run beside each
+other and beside eager calls, and one for the largest batch does for all."""
 import pytest
 import torch
 
@@ -89,3 +89,20 @@ def test_graphs_beside_each_other(forked):
                     assert torch.equal(a, b)
         for a, b in zip(eager, want[2]):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("parts,width,rows", [(1, 64, [16537, 16213, 9000, 70]), (13, 64, [1283, 1258, 40]), (4, 100, [2049, 2009, 300]), (1, 2000, [3000, 900, 5])])
+def test_the_largest_batch_s_workspace_for_all(parts, width, rows):
+    """Smaller batches in it leave what lies behind it as it was, and have the results of a call with their own."""
+    hp = HotPath([1], 4)
+    need = B.fae_layer_norm_bwd_workspace_bytes(B.Norm(rows[0], parts, width))
+    buf = torch.full((need + 4096,), 0x5A, dtype=torch.uint8, device="cuda")
+    for n in rows:
+        x, gy = torch.randn((2, n, parts, width), device="cuda")
+        want = hp.layer_norm_backward(x, gy)
+        gx, dg, db = torch.empty_like(x), *torch.empty((2, parts, width), device="cuda")
+        B.fae_layer_norm_bwd(hp.ctx, B.Norm(n, parts, width), x, gy, gx, dg, db, buf[:need])
+        hp.sync()
+        for a, b in zip((gx, dg, db), want):
+            assert torch.equal(a, b)
+        assert bool((buf[need:] == 0x5A).all())

@@ -29,3 +29,18 @@ def test_products_that_overflow(n_rows):
         n = _norm(n_rows=n_rows, n_parts=parts, width=1)
         assert _fwd(n)[0] == B.FAE_EINVAL and _bwd(n) == B.FAE_EINVAL
         assert B.load().fae_layer_norm_bwd_workspace_bytes(C.byref(n)) == 0
+
+
+@host
+@pytest.mark.parametrize("x_type,y_type", [(B.FAE_F32, B.FAE_F32), (B.FAE_BF16, B.FAE_BF16)])
+@pytest.mark.parametrize("parts,width", [(1, 16), (1, 64), (1, 100), (1, 513), (1, 1664), (1, 9001), (2, 7), (3, 40), (4, 100), (5, 128), (7, 16), (8, 64), (13, 64),
+                                         (26, 64), (26, 256), (33, 20), (63, 512), (64, 8)])
+def test_a_workspace_is_enough_for_fewer_rows(parts, width, x_type, y_type):
+    """A program sizes it for its largest batch and has a smaller one at the end."""
+    lib, n, before = B.load(), _norm(n_parts=parts, width=width, x_type=x_type, y_type=y_type), 0
+    rows = sorted({*range(0, 3000), *range(3000, 70_000, 13), *(1 << k for k in range(16, 24)), ((1 << 31) - 1) // parts})
+    for n.n_rows in rows:
+        need = lib.fae_layer_norm_bwd_workspace_bytes(C.byref(n))
+        assert need >= max(before, 256)
+        before = need
+    assert before <= 2 * 4 * (1024 + 64) * parts * (width + 3) + 512  # a row of sums for each part and workgroup, whatever the rows
