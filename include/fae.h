@@ -358,8 +358,8 @@ typedef struct {
  *   h = (x - mean(x)) / sqrt(var(x) + eps) with the mean and the (biased) variance of the row's width values,
  *   y = gamma[p][c] * h + beta[p][c], then dropout if asked for.
  * A row of zeros (an empty bag) has h = 0, one of another value everywhere at most 2^-38 of that
- * value / sqrt(eps).  The sum of the squared deviations of a row has to be a number of fp32
- * (deviations below about 1e17). */
+ * value / sqrt(eps).  The sum of a row's values has to be a number of fp32 (values below 3.4e38 / width are
+ * safe), and so has that of the squared deviations (deviations below about 1e17) unless all values are equal. */
 typedef struct {
     int64_t n_rows;
     int32_t n_parts; /* 1 .. FAE_MAX_TABLES; n_rows * n_parts < 2^31 */
