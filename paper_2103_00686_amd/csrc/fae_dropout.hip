@@ -61,8 +61,8 @@ struct DropArgs {
     const void *x;
     void *y;
     int64_t x_stride, y_stride;
-    int64_t first;        // the launch's first group of eight values
-    int64_t n_groups;     // groups in all rows
+    uint32_t row0;        // the launch's first row (of all parts)
+    uint32_t n_groups;    // groups of eight values in its rows
     uint32_t per_row;     // of them in a row
     uint32_t per_row_inv; // 2^18 / per_row, rounded up (for rows of fewer than DROP_TILE groups)
     uint32_t n_parts, width;
@@ -71,7 +71,7 @@ struct DropArgs {
 };
 
 #define DROP_TILE 256
-#define DROP_LAUNCH (1LL << 31) // groups of one launch, a thread each: a grid holds fewer than 2^32 threads
+#define DROP_LAUNCH (1LL << 31) // groups of one launch at most, a thread each: a grid holds fewer than 2^32 threads
 
 // A thread takes a group of eight values, a workgroup DROP_TILE consecutive groups: one division per workgroup finds its first row,
 // and a group's row is a small number of rows on: none or one where rows are as long as the tile, else a product with
@@ -83,13 +83,13 @@ struct DropArgs {
 template <typename TX, typename TY, int ENDS> __global__ __launch_bounds__(DROP_TILE) void dropout_kernel(DropArgs a)
 {
     constexpr int E = sizeof(TX) == 2 ? 8 : 4; // values in 16 bytes
-    const int64_t base = a.first + (int64_t)blockIdx.x * DROP_TILE;
+    const uint32_t base = blockIdx.x * DROP_TILE;
     if (base + threadIdx.x >= a.n_groups)
         return;
-    const int64_t row0 = fae_div_small(base, a.per_row);
-    const uint32_t q = (uint32_t)(base - row0 * a.per_row) + threadIdx.x;
+    const uint32_t row0 = base / a.per_row;
+    const uint32_t q = base - row0 * a.per_row + threadIdx.x;
     const uint32_t on = a.per_row >= DROP_TILE ? (q >= a.per_row ? 1 : 0) : (q * a.per_row_inv) >> 18;
-    const uint32_t group = q - on * a.per_row, row = (uint32_t)row0 + on;
+    const uint32_t group = q - on * a.per_row, row = row0 + on;
     uint32_t r = row, part = 0;
     if (a.n_parts > 1) {
         r = row / a.n_parts;
@@ -104,7 +104,7 @@ template <typename TX, typename TY, int ENDS> __global__ __launch_bounds__(DROP_
         at[h].set(group * 8 + h * E, a.width);
         v[h] = fae_load<TX, E, ENDS>(x, at[h], a.ends);
     }
-    const fae_mask8 m = fae_philox(group, row, fae_drop_offset(a.drop), a.drop.key[0], a.drop.key[1]);
+    const fae_mask8 m = fae_philox(group, a.row0 + row, fae_drop_offset(a.drop), a.drop.key[0], a.drop.key[1]);
 #pragma unroll
     for (int h = 0; h < 8 / E; ++h) {
         float o[E];
@@ -144,28 +144,31 @@ static int32_t dropout_impl(fae_ctx *ctx, const char *who, const fae_drop *drop,
         rc = fae_check_overlap(ctx, who, y, x, n_rows, row);
     if (rc != FAE_OK)
         return rc;
-    a.x = x.p;
-    a.y = (void *)y.p;
     a.x_stride = x.stride;
     a.y_stride = y.stride;
     a.per_row = ((uint32_t)width + 7) / 8;
     a.per_row_inv = ((1u << 18) + a.per_row - 1) / a.per_row;
-    a.n_groups = n_rows * n_parts * (int64_t)a.per_row;
     a.n_parts = n_parts;
     a.width = width;
     a.ends = fae_row_end(width, 16 / fae_type_size(x.type), a.per_row * 8LL);
+    if (n_rows * n_parts * (int64_t)a.per_row > (1LL << 39)) // 8 TiB and more: no such buffers
+        return fae_fail(ctx, FAE_EINVAL, "%s: too many values", who);
+    int64_t samples = n_rows;
     if (x.stride == row && y.stride == row) { // the parts are rows
+        samples *= n_parts;
         a.n_parts = 1;
         a.x_stride = a.y_stride = width;
     }
-    if (a.n_groups > (1LL << 39)) // 4 TiB and more: no such buffers
-        return fae_fail(ctx, FAE_EINVAL, "%s: too many values", who);
     FAE_HIP(ctx, hipSetDevice(ctx->device));
     fae_ktimer kt(ctx, FAE_K_DROPOUT);
     const dim3 block(DROP_TILE);
-    for (a.first = 0; a.first < a.n_groups; a.first += DROP_LAUNCH) {
-        const int64_t groups = a.n_groups - a.first < DROP_LAUNCH ? a.n_groups - a.first : DROP_LAUNCH;
-        const dim3 grid((unsigned)((groups + DROP_TILE - 1) / DROP_TILE));
+    const int64_t groups = (int64_t)a.n_parts * a.per_row, most = DROP_LAUNCH / groups; // of a sample; samples of a launch
+    for (int64_t first = 0; first < samples; first += most) {
+        a.x = (const char *)x.p + first * a.x_stride * fae_type_size(x.type);
+        a.y = (char *)y.p + first * a.y_stride * fae_type_size(y.type);
+        a.row0 = (uint32_t)(first * a.n_parts);
+        a.n_groups = (uint32_t)((samples - first < most ? samples - first : most) * groups);
+        const dim3 grid((a.n_groups + DROP_TILE - 1) / DROP_TILE);
 #define DROP_CASE(TX, TX_, TY, TY_)                                                              \
     if (x.type == TX && y.type == TY) {                                                          \
         if (a.ends == FAE_WHOLE)                                                                 \

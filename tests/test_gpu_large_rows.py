@@ -136,3 +136,22 @@ def test_backward_of_the_most_rows(hp, parts):
     R.assert_within(dbeta.reshape(parts, width), rb, tb, "dbeta")
     flat = gx[:-last].reshape(-1)
     assert not any(bool((flat[i:i + PIECE] != 0).any()) for i in range(0, flat.numel(), PIECE))
+
+
+def test_dropout_of_samples_with_gaps_past_a_grid(hp):
+    """Three parts and a gap in every sample: launches start at a sample, rows count on."""
+    n, parts = (1 << 31) // 3 + 70_001, 3
+    flat = torch.ones((n, 4), dtype=F16, device="cuda")
+    x = flat[:, :3].unflatten(1, (parts, 1))
+    hp.dropout(x, B.Drop(0.5, 3, 8), out=x)
+    hp.sync()
+    step = PIECE // 4
+    for i in range(0, n, step):
+        v = flat[i:i + step]
+        assert bool((v[:, 3] == 1).all()) and bool(((v[:, :3] == 0) | (v[:, :3] == 2)).all())
+    rng = np.random.default_rng(3)
+    border = (1 << 31) // 3
+    samples = np.unique(np.concatenate([rng.integers(0, n, 8000), np.arange(300), border - 150 + np.arange(300), n - 1 - np.arange(300)]))
+    got = flat[torch.from_numpy(samples).cuda(), :3].float().cpu().numpy().ravel()
+    rows = (samples[:, None] * 3 + np.arange(3)).ravel()
+    assert np.array_equal(got, np.where(_numbers(rows, 0 * rows, 3, 8) < 32768, 0.0, 2.0))
