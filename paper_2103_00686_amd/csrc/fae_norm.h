@@ -8,9 +8,11 @@
 // q + 2 step, ... (the forward one batch of them); step, the number of teams, is a multiple of the parts, so a team stays with one part, holds its weights in
 // registers, and can add up their gradient over all its rows.
 //
-// What bounds it: memory where there are many rows (the forward writes 16 384 x 26 x 64 fp32 in 40 us, 5.4 TB/s, as a copy of that size
-// takes; the backward 61 us, 5.3 TB/s, where adding two such buffers up into a third takes 59), the chain of a row's three
-// reductions where there are few (about half a microsecond a row, one where a team is several waves).
+// What bounds it: memory where there are many rows of whole chunks (the forward of 16 384 x 26 x 64 fp32 takes 40 us, 5.4 TB/s, where
+// copying such a buffer takes 39; the backward 61 us, 5.4 TB/s, where adding two of them up into a third takes 56), the chain of a row's three
+// reductions where there are few (about half a microsecond a row, one where a team is several waves).  Rows that end inside a chunk, above
+// all of two-byte values, are bound by the vector units' work on that chunk (bf16 rows of 100 values 3.6 TB/s forward, 3.8 backward; fp32
+// 5.2 and 5.0), rows just above what a wave holds by their empty lanes (1030 values: fp32 4.1 and 4.0, bf16 3.1 and 2.9).
 struct NormArgs {
     const void *x, *gy;
     void *y; // forward: y, backward: gx
@@ -482,7 +484,10 @@ constexpr int norm_fwd_rows(int nv) { return nv == 1 ? 4 : nv == 2 ? 2 : 1; }
 // How the backward's loads run ahead.  Two rows held (four: 16 384 x 26 x 64 62 -> 65 us, 50 001 x 26 x 64 with dropout 152 -> 160); fp32 rows of
 // several waves with one row's registers, filled again as soon as its values are taken (16 384 x 4096 150 -> 140 us, 40 000 x 2048 with
 // dropout 171 -> 158; 16-bit rows, with twice the values per lane, 133 -> 139 for 65 536 x 1664); one row and nothing ahead where a
-// workgroup of 1024 has no registers for more (4096 x 16 384 bf16 148 -> 97 us, with one filled early 136).
+// workgroup of 1024 lanes, with 128 registers each, holds 16 values in a lane (4096 x 16 384 bf16 148 -> 97 us, with one filled early 136).
+// Those 16 values take up to eight registers each (x, g, their raw words, gamma, the two sums), and do not all fit: fp32 rows above 8192
+// values keep 6 to 40 registers' worth in scratch, 28 to 164 bytes a lane, 16-bit ones with dropout on rows that do not fill
+// the lanes 6 to 17 (2441 x 16 384 fp32 112 us, 4.3 TB/s; bf16 67 us, 3.6).
 constexpr bool norm_bwd_early(int nv, int chunk, int threads, bool waves) { return waves && threads == 512 && nv * chunk <= 8; }
 constexpr int norm_bwd_depth(int nv, int chunk, int threads, bool waves)
 {

@@ -59,13 +59,15 @@ template <int L, int THREADS> __global__ __launch_bounds__(THREADS) void norm_we
 
 static uint32_t norm_gcd(uint32_t a, uint32_t b) { return b ? norm_gcd(b, a % b) : a; }
 
-// rows of a team that one launch takes
+// Rows of a team that one launch takes: eight, four where a team is whole waves, six for workgroups of 512 lanes (fp32, us in one launch of
+// 512 lanes | in two: 768 x 16 6.0 | 6.4, 192 x 64 5.6 | 6.1, 48 x 256 6.1 | 6.1; 48 x 512 7.4 | 7.1; eight rows: 60 x 256 6.7 | 6.1).
 static int norm_few_rows(int lanes, uint32_t threads) { return lanes > 64 ? 4 : threads == 512 ? 6 : 8; }
 
 // Workgroups of 512 lanes or 256 for teams of up to a wave, in the backward.  Where a workgroup adds up its teams' sums in LDS (more teams
 // than parts) 512 leave half as many rows of sums, which pays once the launch is as large as it gets (us with 512 | 256: 6007 x 4 x 100 fp32
 // 11.1 | 12.3, 2403 x 13 x 64 11.1 | 12.8, 4096 x 256 8.2 | 8.8, 65 536 x 512 76.4 | 78.7; below, 4096 x 64 7.2 | 6.9; and where teams'
-// sums go out as they are 1201 x 26 x 64 11.8 | 9.0), or where one launch is then enough (717 x 16 6.0 | 6.4).
+// sums go out as they are 1201 x 26 x 64 11.8 | 9.0), or where one launch is then enough (520 x 16 5.4 | 6.4, 717 x 16 6.0 | 6.4,
+// 130 x 4 x 16 4.7 | 6.1, 60 x 3 x 64 5.4 | 6.0).
 static bool norm_wide_workgroup(int64_t rows, uint32_t parts, int lanes)
 {
     const uint32_t teams = 256 / lanes;
@@ -79,7 +81,7 @@ static bool norm_wide_workgroup(int64_t rows, uint32_t parts, int lanes)
 // 6.5 and 7.0; 8 instead of 4 where it does not: 4096 x 1664 bf16 27.9 against 22.3, 512 x 8192 bf16 22.0 against 17.2).
 static int64_t norm_bwd_rows(uint32_t teams, uint32_t parts) { return teams > parts ? 2 : 4; }
 
-// The backward's workgroups walk on, up to 512 lanes of them to a compute unit: with twice as many the rows in flight lie further apart
+// The backward's workgroups walk on, up to 512 lanes of them to a compute unit (or one workgroup that is larger): with twice as many the rows in flight lie further apart
 // and more sums go out (16 384 x 26 x 64 fp32 62 us | 67, 16 384 x 4096 147 | 156), with half as many too little is in flight (91, 154).
 // The same number for every compute unit: 341 workgroups of six waves took as long as 512 (16 384 x 6000 bf16 128 us | 180).
 static int64_t norm_bwd_most_blocks(uint32_t threads) { return threads > 256 ? 256 : 256 * (512 / threads); }
@@ -114,8 +116,8 @@ static NormShape norm_shape(const fae_norm *n, bool bwd)
     int64_t blocks = (rows + per_team * s.teams - 1) / (per_team * s.teams);
     const int64_t most_blocks = bwd ? norm_bwd_most_blocks(s.threads) : blocks;
     // Few rows: as many teams as one workgroup holds (or one per part) take them all, and their sums are the gradients, which saves a
-    // launch.  Up to eight rows each, four where a team is whole waves (us with one launch | two: 128 x 64 fp32 5.5 | 6.3, 256 x 64
-    // with 16 rows each 8.2 | 6.4, 16 x 256 4.2 | 6.1, 4 x 26 x 64 3.4 | 6.1, 8 x 8192 bf16 with eight rows each 16.2 | 12.3).
+    // launch (us with one launch | two: 128 x 64 fp32 5.5 | 6.3, 256 x 64 with 16 rows each 8.2 | 6.4, 16 x 256 4.2 | 6.1,
+    // 4 x 26 x 64 3.4 | 6.1, 8 x 8192 bf16 with eight rows each 16.2 | 12.3).
     const uint32_t few = parts * (s.teams > parts ? s.teams / parts : 1);
     if (bwd && rows <= norm_few_rows(s.lanes, s.threads) * (int64_t)few) {
         s.direct = true;
