@@ -27,7 +27,7 @@
  *   - Types: row ids, hot slots, sample ids and CSR offsets are int32; access
  *     counts are uint32 (precondition: fewer than 2^32 accesses per row);
  *     weights, pooled outputs and gradients are fp32, row-major.
- *     (Layer norm and dropout also take bf16 and fp16 rows.)
+ *     (Layer norm, dropout, the softmax loss and gradients' norm and clipping also take bf16 and fp16.)
  *   - Limits: n_tables <= FAE_MAX_TABLES; dim >= 1 (dim % 4 == 0 takes the
  *     16-byte vector path); lookups per table per call < 2^31; rows per table < 2^31.
  */
@@ -149,7 +149,11 @@ int32_t fae_set_option(fae_ctx *ctx, const char *name, int64_t value);
 #define FAE_K_NORM 19        /* layer norm, forward and the rows' gradient       */
 #define FAE_K_NORM_WEIGHTS 20 /* layer norm: its weights' gradient from partial sums */
 #define FAE_K_DROPOUT 21     /* dropout, both directions                         */
-#define FAE_K_COUNT 22
+#define FAE_K_LOSS 22        /* softmax loss: products with the classes, statistics */
+#define FAE_K_LOSS_JOIN 23   /* softmax loss: partial results put together      */
+#define FAE_K_LOSS_BWD 24    /* softmax loss: gradient of the classes           */
+#define FAE_K_GRADS 25       /* norm of gradients and clipping                  */
+#define FAE_K_COUNT 26
 int32_t fae_timing_enable(fae_ctx *ctx, int32_t on);
 int32_t fae_timing_reset(fae_ctx *ctx);
 int32_t fae_timing_read(fae_ctx *ctx, int32_t kernel_class, double *h_total_ms, int64_t *h_launches);
@@ -395,6 +399,72 @@ int32_t fae_dropout_fwd(fae_ctx *ctx, const fae_drop *drop, int64_t n_rows, int3
                         int32_t x_type, int64_t x_row_stride, void *y, int32_t y_type, int64_t y_row_stride);
 int32_t fae_dropout_bwd(fae_ctx *ctx, const fae_drop *drop, int64_t n_rows, int32_t n_parts, int32_t width, const void *gy,
                         int32_t y_type, int64_t gy_row_stride, void *gx, int32_t x_type, int64_t gx_row_stride);
+
+/* ---- softmax cross entropy over the rows of a table --------------------------------
+ * Which row of a table comes next: the classes are rows of a (hot) table or of any matrix w, the scores of a
+ * row x[r] are its products with all of them, and neither scores nor probabilities are ever stored.
+ *   z[r][v] = scale * <x[r], w[v]> + bias[v]
+ *   lse[r]  = log sum_v exp z[r][v]
+ *   loss[r] = lse[r] - z[r][target[r]],  0 for a row without a target
+ * x is [n_rows] rows of `width` values, x_row_stride values apart, w [n_classes] rows, w_row_stride apart, of one type:
+ * FAE_F32, FAE_BF16 or FAE_F16.  Values between rows are neither read nor written, buffers need the alignment of
+ * their values.  Products of 16-bit values are exact and their sums fp32; fp32 values are taken as three bf16 numbers
+ * each, whose six largest products are summed in fp32 (what is left out is below 2^-23 of a product).  Probabilities enter the
+ * gradients' sums rounded to the type (fp32: as three bf16 numbers again).  x and w have to be finite.
+ *   targets: int32 or int64 (target_bits), one per row.  A negative one is a row without a target (a cold row, padding):
+ *     its loss is 0, its gradients are 0 and it adds nothing to gw and gbias.  One of n_classes or more is treated so too,
+ *     and reported as FAE_ERANGE by the next synchronising call.
+ *   bias: may be -infinity (a class that is not offered: probability 0).  A row for which no class is offered has
+ *     lse = -infinity, loss 0 and no gradients; one whose target is not offered has loss +infinity and finite gradients. */
+typedef struct {
+    int64_t n_rows;    /* 0 .. 2^31 - 1 */
+    int64_t n_classes; /* 1 .. 2^31 - 1 */
+    int32_t width;     /* 1 .. FAE_LOSS_MAX_WIDTH */
+    int32_t type;      /* of x, w and their gradients */
+    float scale;       /* finite */
+    int32_t target_bits; /* 32 or 64 */
+    const void *targets; /* device int32 or int64 [n_rows] */
+    const float *bias;   /* device fp32[n_classes], or NULL: zeros */
+} fae_softmax_loss;
+#define FAE_LOSS_MAX_WIDTH 256
+/* loss and lse: device fp32[n_rows], either may be NULL.  mean: NULL, or device fp32[n_rows * width], what a training step keeps
+ * for its backward:
+ *   mean[r] = sum over the classes v other than r's target of exp(z[r][v] - lse[r]) * w[v].
+ * No output may share memory with another or with an input.  ws is on 16 bytes; its size does not fall with
+ * n_rows or n_classes (one for the largest call is enough for the others), and calls that may overlap need one each.  Sums
+ * are taken in an order that depends on the sizes alone.  Asynchronous. */
+size_t fae_softmax_loss_fwd_workspace_bytes(const fae_softmax_loss *what);
+int32_t fae_softmax_loss_fwd(fae_ctx *ctx, const fae_softmax_loss *what, const void *x, int64_t x_row_stride, const void *w,
+                             int64_t w_row_stride, float *loss, float *lse, float *mean, void *ws, size_t ws_bytes);
+/* The gradients.  With gloss[r] (device fp32[n_rows]) the gradient of loss[r], lse the forward's and
+ * G[r][v] = gloss[r] * (exp(z[r][v] - lse[r]) - (v == target[r])):
+ *   gx[r] = scale * sum_v G[r][v] * w[v],  gw[v] = scale * sum_r G[r][v] * x[r],  gbias[v] = sum_r G[r][v].
+ * All are overwritten (gw and gbias with zeros if n_rows is 0); each may be NULL.  mean: the forward's, or NULL (then gx
+ * costs what the forward costs).  Everything else as in the forward.  Asynchronous. */
+size_t fae_softmax_loss_bwd_workspace_bytes(const fae_softmax_loss *what);
+int32_t fae_softmax_loss_bwd(fae_ctx *ctx, const fae_softmax_loss *what, const void *x, int64_t x_row_stride, const void *w,
+                             int64_t w_row_stride, const float *lse, const float *mean, const float *gloss, void *gx,
+                             int64_t gx_row_stride, void *gw, int64_t gw_row_stride, float *gbias, void *ws, size_t ws_bytes);
+
+/* ---- norm of all gradients together, and clipping by it --------------------------------
+ * Over a list of tensors of any sizes and types:
+ *   norm = |scale| * sqrt(sum of all squares),  out = g * scale * min(1, max_norm / norm).
+ * Squares and their sums are fp64, so no gradient is too large or too small for its square; a sum's order depends on the sizes
+ * alone.  scale: one over a loss scale, or 1.  norm: device fp32, also beyond fp32's range (then it is infinite).  A
+ * gradient that is infinite makes the norm infinite, finite values 0 and infinite ones NaN, and a NaN makes all of them NaN: what comes
+ * out says that the step is lost. */
+typedef struct {
+    const void *g; /* device, n values; may be NULL if n is 0 */
+    void *out;     /* fae_grad_clip: device, n values; g itself, or memory that no other tensor of the list has */
+    int64_t n;     /* 0 .. 2^40 */
+    int32_t type;  /* FAE_F32, FAE_BF16 or FAE_F16, of both */
+} fae_grad;
+#define FAE_MAX_GRADS 65536
+/* ws is on 16 bytes; its size does not fall with n_grads or the tensors' sizes.  Calls that may overlap need one each.  Asynchronous. */
+size_t fae_grad_workspace_bytes(int32_t n_grads, const fae_grad *h_grads);
+int32_t fae_grad_norm(fae_ctx *ctx, int32_t n_grads, const fae_grad *h_grads, float scale, float *norm, void *ws, size_t ws_bytes);
+int32_t fae_grad_clip(fae_ctx *ctx, int32_t n_grads, const fae_grad *h_grads, float scale, float max_norm, float *norm, void *ws,
+                      size_t ws_bytes);
 
 /* ---- embedding synchronisation between the hot tables and the full tables ----
  * (Sec. 3 (4); Sec. 6.2, "Embedding Synchronization") */

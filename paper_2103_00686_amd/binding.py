@@ -23,6 +23,8 @@ FAE_POOL_SUM, FAE_POOL_MEAN = 0, 1
 FAE_OPT_SGD, FAE_OPT_ROWWISE_ADAGRAD = 0, 1
 FAE_F32, FAE_BF16, FAE_F16 = 0, 1, 2
 FAE_NORM_MAX_WIDTH = 16384
+FAE_LOSS_MAX_WIDTH = 256
+FAE_MAX_GRADS = 65536
 
 EXPORTS = [
     "fae_create", "fae_destroy", "fae_last_error", "fae_version", "fae_sync", "fae_set_option",
@@ -37,6 +39,8 @@ EXPORTS = [
     "fae_embbag_fwd_opts", "fae_embbag_bwd_opts",
     "fae_layer_norm_fwd", "fae_layer_norm_bwd_workspace_bytes", "fae_layer_norm_bwd",
     "fae_dropout_fwd", "fae_dropout_bwd",
+    "fae_softmax_loss_fwd_workspace_bytes", "fae_softmax_loss_fwd", "fae_softmax_loss_bwd_workspace_bytes", "fae_softmax_loss_bwd",
+    "fae_grad_workspace_bytes", "fae_grad_norm", "fae_grad_clip",
 ]
 
 
@@ -83,6 +87,15 @@ class _Norm(C.Structure):
                 ("y_type", C.c_int32), ("eps", C.c_float), ("gamma", C.c_void_p), ("beta", C.c_void_p)]
 
 
+class _SoftmaxLoss(C.Structure):
+    _fields_ = [("n_rows", C.c_int64), ("n_classes", C.c_int64), ("width", C.c_int32), ("type", C.c_int32), ("scale", C.c_float),
+                ("target_bits", C.c_int32), ("targets", C.c_void_p), ("bias", C.c_void_p)]
+
+
+class _Grad(C.Structure):
+    _fields_ = [("g", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("type", C.c_int32)]
+
+
 class _Sched(C.Structure):
     _fields_ = [("rate", C.c_double), ("prev", C.c_double), ("u", C.c_int32), ("falls", C.c_int32),
                 ("reports", C.c_int32)]
@@ -107,7 +120,8 @@ def load():
     lib.fae_version.restype = C.c_char_p
     for name in ("fae_choose_cutoff_workspace_bytes", "fae_build_workspace_bytes",
                  "fae_partition_workspace_bytes", "fae_bwd_workspace_bytes", "fae_estimate_workspace_bytes",
-                 "fae_bwd_static_workspace_bytes", "fae_layer_norm_bwd_workspace_bytes"):
+                 "fae_bwd_static_workspace_bytes", "fae_layer_norm_bwd_workspace_bytes",
+                 "fae_softmax_loss_fwd_workspace_bytes", "fae_softmax_loss_bwd_workspace_bytes", "fae_grad_workspace_bytes"):
         getattr(lib, name).restype = C.c_size_t
     lib.fae_destroy.restype = None
     lib.fae_kernel_name.restype = C.c_char_p
@@ -203,6 +217,31 @@ class Norm:
                   _ptr_on(self.gamma, torch.float32, device), _ptr_on(self.beta, torch.float32, device))
         n._keep = (self.gamma, self.beta)
         return n
+
+
+@dataclass
+class SoftmaxLoss:
+    """Softmax cross entropy of n_rows rows of width values over n_classes rows of a table, all of dtype.  targets: device int32 or
+    int64 [n_rows], negative where a row has none; bias: device fp32[n_classes] or None."""
+    n_rows: int
+    n_classes: int
+    width: int
+    targets: torch.Tensor
+    bias: Optional[torch.Tensor] = None
+    scale: float = 1.0
+    dtype: torch.dtype = torch.float32
+
+    def c(self, device: int):
+        if self.targets.dtype not in (torch.int32, torch.int64):
+            raise TypeError(f"targets: need int32 or int64, got {self.targets.dtype}")
+        for name, t, n in (("targets", self.targets, self.n_rows), ("bias", self.bias, self.n_classes)):
+            if t is not None and t.numel() != n:
+                raise ValueError(f"{name}: need {n} values, got {tuple(t.shape)}")
+        what = _SoftmaxLoss(int(self.n_rows), int(self.n_classes), int(self.width), _type(self.dtype), float(self.scale),
+                            self.targets.element_size() * 8, _ptr_on(self.targets, self.targets.dtype, device),
+                            _ptr_on(self.bias, torch.float32, device))
+        what._keep = (self.targets, self.bias)
+        return what
 
 
 _TYPES = {torch.float32: FAE_F32, torch.bfloat16: FAE_BF16, torch.float16: FAE_F16}
@@ -304,7 +343,7 @@ def fae_set_option(ctx: Context, name: str, value: int):
     ctx.check(load().fae_set_option(ctx._h, name.encode(), C.c_int64(value)))
 
 
-FAE_K_COUNT = 22
+FAE_K_COUNT = 26
 
 
 def fae_kernel_name(kernel_class: int) -> str:
@@ -592,6 +631,126 @@ def prepare_dropout_bwd(ctx: Context, drop: Drop, gy: torch.Tensor, gx: torch.Te
 
 def fae_dropout_bwd(ctx: Context, drop: Drop, gy: torch.Tensor, gx: torch.Tensor):
     prepare_dropout_bwd(ctx, drop, gy, gx)()
+
+
+def _loss_bytes(fn, what: SoftmaxLoss) -> int:
+    return int(fn(C.byref(_SoftmaxLoss(int(what.n_rows), int(what.n_classes), int(what.width), _type(what.dtype), float(what.scale), 32, None, None))))
+
+
+def _loss_rows(t: torch.Tensor, n: int, what: SoftmaxLoss, device: int):
+    if t.shape[0] != n:
+        raise ValueError(f"need {n} rows, got {tuple(t.shape)}")
+    return _rows(t, 1, what.width, what.dtype, device)
+
+
+def _loss_vector(name: str, t: Optional[torch.Tensor], n: int, device: int):
+    if t is not None and t.numel() != n:
+        raise ValueError(f"{name}: need {n} values, got {tuple(t.shape)}")
+    return _ptr_on(t, torch.float32, device)
+
+
+def fae_softmax_loss_fwd_workspace_bytes(what: SoftmaxLoss) -> int:
+    return _loss_bytes(load().fae_softmax_loss_fwd_workspace_bytes, what)
+
+
+def prepare_softmax_loss_fwd(ctx: Context, what: SoftmaxLoss, x: torch.Tensor, w: torch.Tensor, loss: Optional[torch.Tensor],
+                             lse: Optional[torch.Tensor], mean: Optional[torch.Tensor], ws: torch.Tensor):
+    """fae_softmax_loss_fwd of these tensors, marshalled once: a zero-argument callable."""
+    c, dev = what.c(ctx.device), ctx.device
+    return _prepare(ctx, load().fae_softmax_loss_fwd,
+                    (ctx._h, C.byref(c), *_loss_rows(x, what.n_rows, what, dev), *_loss_rows(w, what.n_classes, what, dev),
+                     _loss_vector("loss", loss, what.n_rows, dev), _loss_vector("lse", lse, what.n_rows, dev),
+                     _loss_vector("mean", mean, what.n_rows * what.width, dev), _ptr_on(ws, torch.uint8, dev), C.c_size_t(ws.numel())),
+                    (ctx, c, x, w, loss, lse, mean, ws))
+
+
+def fae_softmax_loss_fwd(ctx: Context, what: SoftmaxLoss, x: torch.Tensor, w: torch.Tensor, loss: Optional[torch.Tensor],
+                         lse: Optional[torch.Tensor], mean: Optional[torch.Tensor], ws: torch.Tensor):
+    prepare_softmax_loss_fwd(ctx, what, x, w, loss, lse, mean, ws)()
+
+
+def fae_softmax_loss_bwd_workspace_bytes(what: SoftmaxLoss) -> int:
+    return _loss_bytes(load().fae_softmax_loss_bwd_workspace_bytes, what)
+
+
+def prepare_softmax_loss_bwd(ctx: Context, what: SoftmaxLoss, x: torch.Tensor, w: torch.Tensor, lse: torch.Tensor,
+                             mean: Optional[torch.Tensor], gloss: torch.Tensor, gx: Optional[torch.Tensor], gw: Optional[torch.Tensor],
+                             gbias: Optional[torch.Tensor], ws: torch.Tensor):
+    """fae_softmax_loss_bwd of these tensors, marshalled once: a zero-argument callable."""
+    c, dev = what.c(ctx.device), ctx.device
+    none = (None, C.c_int64(0))
+    return _prepare(ctx, load().fae_softmax_loss_bwd,
+                    (ctx._h, C.byref(c), *_loss_rows(x, what.n_rows, what, dev), *_loss_rows(w, what.n_classes, what, dev),
+                     _loss_vector("lse", lse, what.n_rows, dev), _loss_vector("mean", mean, what.n_rows * what.width, dev),
+                     _loss_vector("gloss", gloss, what.n_rows, dev), *(none if gx is None else _loss_rows(gx, what.n_rows, what, dev)),
+                     *(none if gw is None else _loss_rows(gw, what.n_classes, what, dev)), _loss_vector("gbias", gbias, what.n_classes, dev),
+                     _ptr_on(ws, torch.uint8, dev), C.c_size_t(ws.numel())),
+                    (ctx, c, x, w, lse, mean, gloss, gx, gw, gbias, ws))
+
+
+def fae_softmax_loss_bwd(ctx: Context, what: SoftmaxLoss, x: torch.Tensor, w: torch.Tensor, lse: torch.Tensor, mean: Optional[torch.Tensor],
+                         gloss: torch.Tensor, gx: Optional[torch.Tensor], gw: Optional[torch.Tensor], gbias: Optional[torch.Tensor],
+                         ws: torch.Tensor):
+    prepare_softmax_loss_bwd(ctx, what, x, w, lse, mean, gloss, gx, gw, gbias, ws)()
+
+
+def _dense(t: torch.Tensor) -> bool:
+    """Whether its values fill one piece of memory, in any order of its dimensions."""
+    want = 1
+    for stride, n in sorted((s, n) for s, n in zip(t.stride(), t.shape) if n > 1):
+        if stride != want:
+            return False
+        want *= n
+    return True
+
+
+def _grads(grads: Sequence[torch.Tensor], out: Optional[Sequence[torch.Tensor]], device: int):
+    """fae_grad for every tensor.  Any order of dimensions will do, the same for a gradient and its output."""
+    if out is not None and len(out) != len(grads):
+        raise ValueError(f"{len(grads)} gradients, {len(out)} outputs")
+    arr = (_Grad * max(len(grads), 1))()
+    for i, (g, o) in enumerate(zip(grads, out if out is not None else grads)):
+        for t in (g, o):
+            if not t.is_cuda:
+                raise TypeError(f"tensor {i}: need a device tensor, got one on {t.device}")
+            if t.device.index != device:
+                raise ValueError(f"tensor {i}: need a tensor on device {device}, got {t.device}")
+        if g.numel() > 0 and not _dense(g):
+            raise ValueError(f"tensor {i}: its values have gaps, strides {g.stride()} of {tuple(g.shape)}")
+        if o.dtype != g.dtype or o.shape != g.shape or (o.numel() > 0 and any(a != b for a, b, n in zip(o.stride(), g.stride(), g.shape) if n > 1)):
+            raise ValueError(f"tensor {i}: an output needs its gradient's type, shape and strides")
+        arr[i] = _Grad(g.data_ptr() if g.numel() else None, o.data_ptr() if g.numel() else None, g.numel(), _type(g.dtype))
+    return arr
+
+
+def fae_grad_workspace_bytes(n_grads: int) -> int:
+    return int(load().fae_grad_workspace_bytes(C.c_int32(n_grads), None))
+
+
+def prepare_grad_norm(ctx: Context, grads: Sequence[torch.Tensor], scale: float, norm: torch.Tensor, ws: torch.Tensor):
+    """fae_grad_norm of these tensors, marshalled once: a zero-argument callable."""
+    arr = _grads(grads, None, ctx.device)
+    return _prepare(ctx, load().fae_grad_norm,
+                    (ctx._h, C.c_int32(len(grads)), arr, C.c_float(scale), _loss_vector("norm", norm, 1, ctx.device),
+                     _ptr_on(ws, torch.uint8, ctx.device), C.c_size_t(ws.numel())), (ctx, list(grads), norm, ws))
+
+
+def fae_grad_norm(ctx: Context, grads: Sequence[torch.Tensor], scale: float, norm: torch.Tensor, ws: torch.Tensor):
+    prepare_grad_norm(ctx, grads, scale, norm, ws)()
+
+
+def prepare_grad_clip(ctx: Context, grads: Sequence[torch.Tensor], scale: float, max_norm: float, norm: Optional[torch.Tensor],
+                      ws: torch.Tensor, out: Optional[Sequence[torch.Tensor]] = None):
+    """fae_grad_clip of these tensors (in place without out), marshalled once: a zero-argument callable."""
+    arr = _grads(grads, out, ctx.device)
+    return _prepare(ctx, load().fae_grad_clip,
+                    (ctx._h, C.c_int32(len(grads)), arr, C.c_float(scale), C.c_float(max_norm), _loss_vector("norm", norm, 1, ctx.device),
+                     _ptr_on(ws, torch.uint8, ctx.device), C.c_size_t(ws.numel())), (ctx, list(grads), list(out or ()), norm, ws))
+
+
+def fae_grad_clip(ctx: Context, grads: Sequence[torch.Tensor], scale: float, max_norm: float, norm: Optional[torch.Tensor],
+                  ws: torch.Tensor, out: Optional[Sequence[torch.Tensor]] = None):
+    prepare_grad_clip(ctx, grads, scale, max_norm, norm, ws, out)()
 
 
 def fae_sync_hot_rows(ctx: Context, tables: Tables, n_hot: Sequence[int], hot_ids: List[torch.Tensor],

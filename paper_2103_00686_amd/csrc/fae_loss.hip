@@ -1,0 +1,537 @@
+// Softmax cross entropy over the rows of a table: checks, workspaces, and the kernels over single rows.
+#include <math.h>
+
+#include "fae_loss.h"
+
+#define LOSS_GROUPS 512 // workgroups that a launch should have: two for each compute unit
+#define LOSS_MOST 0x7fff0000LL
+
+// ---------------------------------------------------------------------------------
+// kernels
+// ---------------------------------------------------------------------------------
+struct LossJoin {
+    const float *stat, *zt, *part;
+    const void *targets;
+    float *loss, *lse, *mean;
+    int32_t target_bits, n_classes, width, pitch;
+    int64_t n_rows;
+    uint32_t n_split, lanes; // lanes: of a part's row, a power of two
+    uint32_t *status;
+};
+
+// A wave per row: the parts' sums at one reference, loss and lse, and the weighted sum of the parts' means.
+__global__ __launch_bounds__(256) void loss_join_kernel(LossJoin a)
+{
+    const int lane = fae_lane();
+    const int64_t r = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
+    if (r >= a.n_rows)
+        return;
+    float most = -INFINITY;
+    for (uint32_t i = lane; i < a.n_split; i += 64)
+        most = fmaxf(most, a.stat[(i * a.n_rows + r) * 2]);
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1)
+        most = fmaxf(most, __shfl_xor(most, d, 64));
+    float sum = 0.f;
+    for (uint32_t i = lane; i < a.n_split; i += 64)
+        sum += a.stat[(i * a.n_rows + r) * 2 + 1] * __builtin_amdgcn_exp2f(a.stat[(i * a.n_rows + r) * 2] - most);
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1)
+        sum += __shfl_xor(sum, d, 64);
+    const float l2 = most + __log2f(sum);
+    if (lane == 0) {
+        const int32_t t = loss_target(a.targets, a.target_bits, r, a.n_classes, a.status);
+        if (a.lse)
+            a.lse[r] = l2 * 0.693147181f;
+        if (a.loss)
+            a.loss[r] = t < 0 || sum == 0.f ? 0.f : (l2 - a.zt[r]) * 0.693147181f;
+    }
+    if (!a.mean)
+        return;
+    const int col = (lane % a.lanes) * 4;
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    if (col < a.pitch)
+        for (uint32_t i = lane / a.lanes; i < a.n_split; i += 64 / a.lanes) {
+            const float f = __builtin_amdgcn_exp2f(a.stat[(i * a.n_rows + r) * 2] - most);
+            const float4 p = *(const float4 *)(a.part + (i * a.n_rows + r) * a.pitch + col);
+            v[0] += f * p.x;
+            v[1] += f * p.y;
+            v[2] += f * p.z;
+            v[3] += f * p.w;
+        }
+    for (uint32_t d = a.lanes; d < 64; d <<= 1)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            v[e] += __shfl_xor(v[e], d, 64);
+    if (lane < (int)a.lanes)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (col + e < a.width)
+                a.mean[r * a.width + col + e] = sum == 0.f ? 0.f : v[e] / sum;
+}
+
+struct LossRows {
+    const void *x, *w, *targets;
+    void *gx;
+    int64_t x_stride, w_stride, gx_stride, n_rows;
+    const float *bias, *lse, *mean, *gloss;
+    float *nlse, *g;
+    int32_t *t;
+    uint32_t *g_most;
+    int32_t target_bits, n_classes, width;
+    float scale;
+    uint32_t *status;
+};
+
+// A wave per row: gx from the mean of the other classes' rows and the target's own, whose share p - 1 is taken without the cancellation of a
+// confident row; and what the classes' gradient reads of every row.
+template <typename T> __global__ __launch_bounds__(256) void loss_rows_kernel(LossRows a)
+{
+    const int lane = fae_lane();
+    const int64_t r = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
+    if (r >= a.n_rows)
+        return;
+    int32_t t = loss_target(a.targets, a.target_bits, r, a.n_classes, a.status);
+    const float lse = a.lse[r];
+    if (lse == -INFINITY) // no class is offered
+        t = -1;
+    const float g = t < 0 ? 0.f : a.gloss[r];
+    if (lane == 0) {
+        a.nlse[r] = t < 0 ? -INFINITY : lse * -1.44269504f;
+        a.g[r] = g;
+        a.t[r] = t;
+        if (a.g_most)
+            atomicMax(a.g_most, __float_as_uint(fabsf(g)));
+    }
+    if (!a.gx)
+        return;
+    const T *x = (const T *)a.x + r * a.x_stride, *w = (const T *)a.w + t * a.w_stride;
+    T *gx = (T *)a.gx + r * a.gx_stride;
+    float wv[4], dot = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int c = lane + j * 64;
+        wv[j] = t >= 0 && c < a.width ? (float)w[c] : 0.f;
+        dot += t >= 0 && c < a.width ? wv[j] * (float)x[c] : 0.f;
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1)
+        dot += __shfl_xor(dot, d, 64);
+    const float share = t < 0 ? 0.f : expm1f(dot * a.scale + (a.bias ? a.bias[t] : 0.f) - lse);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int c = lane + j * 64;
+        if (c < a.width)
+            gx[c] = (T)(t < 0 ? 0.f : a.scale * g * (a.mean[r * a.width + c] + share * wv[j]));
+    }
+}
+
+struct LossClasses {
+    const float *part, *psum;
+    void *gw;
+    float *gbias;
+    int64_t gw_stride, n_classes;
+    uint32_t n_split;
+    int32_t width, pitch;
+    float scale;
+};
+
+// A thread per four values of a class: the sum of the parts, in their order.
+template <typename T> __global__ __launch_bounds__(256) void loss_classes_kernel(LossClasses a)
+{
+    const int per = a.pitch / 4;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, n = i / per;
+    const int col = (int)(i - n * per) * 4;
+    if (n >= a.n_classes)
+        return;
+    if (a.gw) {
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        for (uint32_t s = 0; s < a.n_split; ++s) {
+            const float4 p = *(const float4 *)(a.part + (s * a.n_classes + n) * a.pitch + col);
+            v[0] += p.x;
+            v[1] += p.y;
+            v[2] += p.z;
+            v[3] += p.w;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            v[e] *= a.scale;
+        fae_place<4> p;
+        p.set(col, a.width);
+        fae_store<T, 4, FAE_ANY>((T *)a.gw + n * a.gw_stride, v, p);
+    }
+    if (a.gbias && col == 0) {
+        float v = 0.f;
+        for (uint32_t s = 0; s < a.n_split; ++s)
+            v += a.psum[s * a.n_classes + n];
+        a.gbias[n] = v;
+    }
+}
+
+// ---------------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------------
+static bool loss_sizes_fit(const fae_softmax_loss *l)
+{
+    return l && l->n_rows >= 0 && l->n_rows < LOSS_MOST && l->n_classes >= 1 && l->n_classes < LOSS_MOST && l->width >= 1 &&
+           l->width <= FAE_LOSS_MAX_WIDTH && l->type >= FAE_F32 && l->type <= FAE_F16;
+}
+
+// n_own held rows in workgroups of LOSS_HELD, n_st streamed rows shared out among as many of them as fill the chip
+struct LossShape {
+    int64_t blocks, tiles, splits;
+    int32_t pitch;
+    int64_t part_rows; // rows of partial results that any n_own up to this one would need (a smaller one is shared out more)
+};
+static LossShape loss_shape(const fae_softmax_loss *l, int64_t n_own, int64_t n_st)
+{
+    LossShape s;
+    const int tile = loss_tile(l->type, loss_padded(l->width));
+    s.blocks = (n_own + LOSS_HELD - 1) / LOSS_HELD;
+    s.tiles = (n_st + tile - 1) / tile;
+    s.splits = s.blocks ? LOSS_GROUPS / s.blocks : 1;
+    s.splits = s.splits > s.tiles ? s.tiles : s.splits;
+    s.splits = s.splits < 1 ? 1 : (s.splits > 8 ? s.splits / 8 * 8 : s.splits);
+    s.pitch = (l->width + 3) / 4 * 4;
+    const int64_t most = (int64_t)LOSS_GROUPS * LOSS_HELD;
+    s.part_rows = n_own > most / (s.tiles ? s.tiles : 1) ? most : n_own * s.tiles;
+    s.part_rows = s.part_rows > n_own ? s.part_rows : n_own;
+    return s;
+}
+
+// what the forward takes: per part and row reference and sum, per row the target's score, and the parts' means
+static size_t loss_fwd_bytes(const fae_softmax_loss *l)
+{
+    const LossShape s = loss_shape(l, l->n_rows, l->n_classes);
+    return fae_align_up(s.part_rows * 8, 256) + fae_align_up(l->n_rows * 4, 256) + fae_align_up(s.part_rows * s.pitch * 4, 256);
+}
+static size_t loss_grad_bytes(const fae_softmax_loss *l)
+{
+    const LossShape s = loss_shape(l, l->n_classes, l->n_rows);
+    const int64_t rows = s.part_rows < (int64_t)LOSS_GROUPS * LOSS_HELD ? s.part_rows : (int64_t)LOSS_GROUPS * LOSS_HELD; // none in one part
+    return fae_align_up(rows * 4, 256) + fae_align_up(rows * s.pitch * 4, 256);
+}
+
+extern "C" size_t fae_softmax_loss_fwd_workspace_bytes(const fae_softmax_loss *what)
+{
+    return loss_sizes_fit(what) ? 256 + loss_fwd_bytes(what) : 0;
+}
+
+extern "C" size_t fae_softmax_loss_bwd_workspace_bytes(const fae_softmax_loss *what)
+{
+    if (!loss_sizes_fit(what))
+        return 0;
+    const size_t f = loss_fwd_bytes(what), g = loss_grad_bytes(what);
+    return 512 + 3 * fae_align_up(what->n_rows * 4, 256) + fae_align_up(what->n_rows * what->width * 4, 256) + (f > g ? f : g);
+}
+
+// bytes that rows take up
+struct LossSpan {
+    const char *what;
+    uintptr_t p;
+    int64_t stride, row, n; // in bytes; rows
+};
+static LossSpan loss_span(const char *what, const void *p, int64_t stride, int64_t row, int64_t n, int size)
+{
+    return {what, (uintptr_t)p, stride * size, row * size, p ? n : 0};
+}
+static bool loss_share(const LossSpan &a, const LossSpan &b)
+{
+    if (!a.n || !b.n)
+        return false;
+    const uintptr_t a1 = a.p + (a.n - 1) * a.stride + a.row, b1 = b.p + (b.n - 1) * b.stride + b.row;
+    if (a1 <= b.p || b1 <= a.p)
+        return false;
+    if (a.n > 1 && b.n > 1 && a.stride == b.stride) { // side by side in rows of one buffer
+        const int64_t d = (int64_t)(b.p > a.p ? (b.p - a.p) % a.stride : (a.stride - (int64_t)((a.p - b.p) % a.stride)) % a.stride);
+        return !(d >= a.row && d + b.row <= a.stride);
+    }
+    return true;
+}
+
+static int32_t loss_check(fae_ctx *ctx, const char *who, const fae_softmax_loss *l, const void *x, int64_t x_stride, const void *w, int64_t w_stride)
+{
+    if (!ctx)
+        return FAE_EINVAL;
+    if (!l)
+        return fae_fail(ctx, FAE_EINVAL, "%s: null description", who);
+    if (!loss_sizes_fit(l))
+        return fae_fail(ctx, FAE_EINVAL, "%s: n_rows=%lld n_classes=%lld width=%d type=%d out of range", who, (long long)l->n_rows,
+                        (long long)l->n_classes, l->width, l->type);
+    if (!isfinite(l->scale))
+        return fae_fail(ctx, FAE_EINVAL, "%s: scale=%g is not finite", who, l->scale);
+    if (l->target_bits != 32 && l->target_bits != 64)
+        return fae_fail(ctx, FAE_EINVAL, "%s: target_bits=%d is neither 32 nor 64", who, l->target_bits);
+    if ((uintptr_t)l->bias % 4 != 0 || (uintptr_t)l->targets % (l->target_bits / 8) != 0)
+        return fae_fail(ctx, FAE_EINVAL, "%s: bias or targets are not aligned to their values", who);
+    if (l->n_rows > 0 && !l->targets)
+        return fae_fail(ctx, FAE_EINVAL, "%s: null targets", who);
+    int32_t rc = l->n_rows > 0 ? fae_check_rows(ctx, who, "x", {x, l->type, x_stride}, l->n_rows, l->width) : FAE_OK;
+    if (rc == FAE_OK)
+        rc = fae_check_rows(ctx, who, "w", {w, l->type, w_stride}, l->n_classes, l->width);
+    return rc;
+}
+
+// no output on an input or another output
+static int32_t loss_check_outputs(fae_ctx *ctx, const char *who, const LossSpan *out, int n_out, const LossSpan *in, int n_in)
+{
+    for (int i = 0; i < n_out; ++i) {
+        for (int j = 0; j < n_in; ++j)
+            if (loss_share(out[i], in[j]))
+                return fae_fail(ctx, FAE_EINVAL, "%s: %s and %s overlap", who, out[i].what, in[j].what);
+        for (int j = 0; j < i; ++j)
+            if (loss_share(out[i], out[j]))
+                return fae_fail(ctx, FAE_EINVAL, "%s: %s and %s overlap", who, out[i].what, out[j].what);
+    }
+    return FAE_OK;
+}
+
+static int32_t loss_check_ws(fae_ctx *ctx, const char *who, const void *ws, size_t bytes, size_t need)
+{
+    if ((uintptr_t)ws % 16 != 0)
+        return fae_fail(ctx, FAE_EINVAL, "%s: the workspace is not on 16 bytes", who);
+    if (!ws || bytes < need)
+        return fae_fail(ctx, FAE_ENOSPC, "%s: workspace of %zu bytes, %zu needed", who, ws ? bytes : 0, need);
+    return FAE_OK;
+}
+
+static void loss_run(fae_ctx *ctx, int32_t type, int mode, const loss_args &a)
+{
+    if (type == FAE_F32)
+        loss_launch_f32(ctx, mode, a);
+    else if (type == FAE_BF16)
+        loss_launch_bf16(ctx, mode, a);
+    else
+        loss_launch_f16(ctx, mode, a);
+}
+
+static void loss_common(fae_ctx *ctx, const fae_softmax_loss *l, const LossShape &s, loss_args *a)
+{
+    memset(a, 0, sizeof(*a));
+    a->width = l->width;
+    a->flip = l->scale < 0.f;
+    a->c = fabsf(l->scale) * 1.44269504f;
+    a->scale = l->scale;
+    a->bias = l->bias;
+    a->targets = l->targets;
+    a->target_bits = l->target_bits;
+    a->n_classes = (int32_t)l->n_classes;
+    a->status = ctx->d_block;
+    a->pitch = s.pitch;
+    a->tiles = (int32_t)s.tiles;
+    a->n_blocks = (uint32_t)s.blocks;
+    a->n_split = (uint32_t)s.splits;
+}
+
+static int32_t loss_forward(fae_ctx *ctx, const fae_softmax_loss *l, const void *x, int64_t x_stride, const void *w, int64_t w_stride, float *loss,
+                            float *lse, float *mean, void *ws, size_t ws_bytes)
+{
+    const LossShape s = loss_shape(l, l->n_rows, l->n_classes);
+    fae_carver cv(ws, ws_bytes);
+    loss_args a;
+    loss_common(ctx, l, s, &a);
+    a.st = w;
+    a.own = x;
+    a.st_stride = w_stride;
+    a.own_stride = x_stride;
+    a.n_st = (int32_t)l->n_classes;
+    a.n_own = (int32_t)l->n_rows;
+    a.stat = cv.take<float>(s.splits * l->n_rows * 2);
+    a.zt = cv.take<float>(l->n_rows);
+    a.part = mean ? cv.take<float>(s.splits * l->n_rows * s.pitch) : nullptr;
+    if (!cv.ok)
+        return fae_fail(ctx, FAE_ENOSPC, "softmax loss: workspace too small");
+    {
+        fae_ktimer kt(ctx, FAE_K_LOSS);
+        loss_run(ctx, l->type, mean ? LOSS_MEAN : LOSS_STATS, a);
+        FAE_LAUNCH_CHECK(ctx);
+    }
+    LossJoin j;
+    memset(&j, 0, sizeof(j));
+    j.stat = a.stat;
+    j.zt = a.zt;
+    j.part = a.part;
+    j.targets = l->targets;
+    j.loss = loss;
+    j.lse = lse;
+    j.mean = mean;
+    j.target_bits = l->target_bits;
+    j.n_classes = (int32_t)l->n_classes;
+    j.width = l->width;
+    j.pitch = s.pitch;
+    j.n_rows = l->n_rows;
+    j.n_split = a.n_split;
+    j.lanes = 1;
+    while ((int)j.lanes * 4 < s.pitch)
+        j.lanes *= 2;
+    j.status = ctx->d_block;
+    fae_ktimer kt(ctx, FAE_K_LOSS_JOIN);
+    FAE_LAUNCH(ctx, loss_join_kernel, dim3((uint32_t)((l->n_rows + 3) / 4)), dim3(256), 0, ctx->stream, j);
+    FAE_LAUNCH_CHECK(ctx);
+    return FAE_OK;
+}
+
+extern "C" int32_t fae_softmax_loss_fwd(fae_ctx *ctx, const fae_softmax_loss *what, const void *x, int64_t x_row_stride, const void *w,
+                                        int64_t w_row_stride, float *loss, float *lse, float *mean, void *ws, size_t ws_bytes)
+{
+    const char *who = "fae_softmax_loss_fwd";
+    int32_t rc = loss_check(ctx, who, what, x, x_row_stride, w, w_row_stride);
+    if (rc != FAE_OK)
+        return rc;
+    const int64_t n = what->n_rows, v = what->n_classes, d = what->width;
+    const int size = fae_type_size(what->type);
+    if (((uintptr_t)loss | (uintptr_t)lse | (uintptr_t)mean) % 4 != 0)
+        return fae_fail(ctx, FAE_EINVAL, "%s: outputs are not aligned to their values", who);
+    const LossSpan out[] = {loss_span("loss", loss, 1, 1, n, 4), loss_span("lse", lse, 1, 1, n, 4), loss_span("mean", mean, d, d, n, 4),
+                            loss_span("workspace", ws, ws_bytes, ws_bytes, 1, 1)};
+    const LossSpan in[] = {loss_span("x", x, x_row_stride, d, n, size), loss_span("w", w, w_row_stride, d, v, size), loss_span("bias", what->bias, 1, 1, v, 4),
+                           loss_span("targets", what->targets, 1, 1, n, what->target_bits / 8)};
+    rc = loss_check_outputs(ctx, who, out, 4, in, 4);
+    if (rc != FAE_OK || n == 0)
+        return rc;
+    rc = loss_check_ws(ctx, who, ws, ws_bytes, fae_softmax_loss_fwd_workspace_bytes(what));
+    if (rc != FAE_OK)
+        return rc;
+    FAE_HIP(ctx, hipSetDevice(ctx->device));
+    return loss_forward(ctx, what, x, x_row_stride, w, w_row_stride, loss, lse, mean, ws, ws_bytes);
+}
+
+extern "C" int32_t fae_softmax_loss_bwd(fae_ctx *ctx, const fae_softmax_loss *what, const void *x, int64_t x_row_stride, const void *w,
+                                        int64_t w_row_stride, const float *lse, const float *mean, const float *gloss, void *gx,
+                                        int64_t gx_row_stride, void *gw, int64_t gw_row_stride, float *gbias, void *ws, size_t ws_bytes)
+{
+    const char *who = "fae_softmax_loss_bwd";
+    int32_t rc = loss_check(ctx, who, what, x, x_row_stride, w, w_row_stride);
+    if (rc != FAE_OK)
+        return rc;
+    const int64_t n = what->n_rows, v = what->n_classes, d = what->width;
+    const int size = fae_type_size(what->type);
+    if (((uintptr_t)lse | (uintptr_t)mean | (uintptr_t)gloss | (uintptr_t)gbias) % 4 != 0)
+        return fae_fail(ctx, FAE_EINVAL, "%s: lse, mean, gloss or gbias are not aligned to their values", who);
+    if (n > 0 && (!lse || !gloss))
+        return fae_fail(ctx, FAE_EINVAL, "%s: null %s", who, lse ? "gloss" : "lse");
+    if (gx && n > 0)
+        rc = fae_check_rows(ctx, who, "gx", {gx, what->type, gx_row_stride}, n, d);
+    if (rc == FAE_OK && gw)
+        rc = fae_check_rows(ctx, who, "gw", {gw, what->type, gw_row_stride}, v, d);
+    if (rc != FAE_OK)
+        return rc;
+    const LossSpan out[] = {loss_span("gx", gx, gx_row_stride, d, n, size), loss_span("gw", gw, gw_row_stride, d, v, size), loss_span("gbias", gbias, 1, 1, v, 4),
+                            loss_span("workspace", ws, ws_bytes, ws_bytes, 1, 1)};
+    const LossSpan in[] = {loss_span("x", x, x_row_stride, d, n, size), loss_span("w", w, w_row_stride, d, v, size), loss_span("bias", what->bias, 1, 1, v, 4),
+                           loss_span("targets", what->targets, 1, 1, n, what->target_bits / 8), loss_span("lse", lse, 1, 1, n, 4),
+                           loss_span("mean", mean, d, d, n, 4), loss_span("gloss", gloss, 1, 1, n, 4)};
+    rc = loss_check_outputs(ctx, who, out, 4, in, 7);
+    if (rc == FAE_OK)
+        rc = loss_check_ws(ctx, who, ws, ws_bytes, fae_softmax_loss_bwd_workspace_bytes(what));
+    if (rc != FAE_OK)
+        return rc;
+    FAE_HIP(ctx, hipSetDevice(ctx->device));
+    fae_carver cv(ws, ws_bytes);
+    uint32_t *g_most = cv.take<uint32_t>(1);
+    LossRows r;
+    memset(&r, 0, sizeof(r));
+    r.nlse = cv.take<float>(n);
+    r.g = cv.take<float>(n);
+    r.t = cv.take<int32_t>(n);
+    float *own_mean = cv.take<float>(n * d);
+    if (!cv.ok)
+        return fae_fail(ctx, FAE_ENOSPC, "%s: workspace too small", who);
+    void *rest = cv.base + cv.used;
+    const size_t rest_bytes = cv.cap - cv.used;
+    if (what->type == FAE_F16) {
+        rc = fae_fill_u32(ctx, g_most, 1, 0);
+        if (rc != FAE_OK)
+            return rc;
+    }
+    if (n > 0) {
+        if (gx && !mean) {
+            rc = loss_forward(ctx, what, x, x_row_stride, w, w_row_stride, nullptr, nullptr, own_mean, rest, rest_bytes);
+            if (rc != FAE_OK)
+                return rc;
+            mean = own_mean;
+        }
+        r.x = x;
+        r.w = w;
+        r.targets = what->targets;
+        r.gx = gx;
+        r.x_stride = x_row_stride;
+        r.w_stride = w_row_stride;
+        r.gx_stride = gx_row_stride;
+        r.n_rows = n;
+        r.bias = what->bias;
+        r.lse = lse;
+        r.mean = mean;
+        r.gloss = gloss;
+        r.g_most = what->type == FAE_F16 ? g_most : nullptr;
+        r.target_bits = what->target_bits;
+        r.n_classes = (int32_t)v;
+        r.width = (int32_t)d;
+        r.scale = what->scale;
+        r.status = ctx->d_block;
+        fae_ktimer kt(ctx, FAE_K_LOSS_JOIN);
+        const dim3 grid((uint32_t)((n + 3) / 4)), block(256);
+        if (what->type == FAE_F32)
+            FAE_LAUNCH(ctx, loss_rows_kernel<float>, grid, block, 0, ctx->stream, r);
+        else if (what->type == FAE_BF16)
+            FAE_LAUNCH(ctx, loss_rows_kernel<fae_bf16>, grid, block, 0, ctx->stream, r);
+        else
+            FAE_LAUNCH(ctx, loss_rows_kernel<fae_f16>, grid, block, 0, ctx->stream, r);
+        FAE_LAUNCH_CHECK(ctx);
+    }
+    if (!gw && !gbias)
+        return FAE_OK;
+    const LossShape s = loss_shape(what, v, n);
+    loss_args a;
+    loss_common(ctx, what, s, &a);
+    a.st = x;
+    a.own = w;
+    a.st_stride = x_row_stride;
+    a.own_stride = w_row_stride;
+    a.n_st = (int32_t)n;
+    a.n_own = (int32_t)v;
+    a.nlse = r.nlse;
+    a.g = r.g;
+    a.t = r.t;
+    a.g_most = g_most;
+    if (s.splits > 1) {
+        fae_carver more(rest, rest_bytes);
+        a.psum = gbias ? more.take<float>(s.splits * v) : nullptr;
+        a.part = gw ? more.take<float>(s.splits * v * s.pitch) : nullptr;
+        if (!more.ok)
+            return fae_fail(ctx, FAE_ENOSPC, "%s: workspace too small", who);
+    } else {
+        a.out = gw;
+        a.out_stride = gw_row_stride;
+        a.out_sum = gbias;
+    }
+    {
+        fae_ktimer kt(ctx, FAE_K_LOSS_BWD);
+        loss_run(ctx, what->type, LOSS_GRAD, a);
+        FAE_LAUNCH_CHECK(ctx);
+    }
+    if (s.splits > 1) {
+        LossClasses c;
+        memset(&c, 0, sizeof(c));
+        c.part = a.part;
+        c.psum = a.psum;
+        c.gw = gw;
+        c.gbias = gbias;
+        c.gw_stride = gw_row_stride;
+        c.n_classes = v;
+        c.n_split = a.n_split;
+        c.width = (int32_t)d;
+        c.pitch = s.pitch;
+        c.scale = what->scale;
+        fae_ktimer kt(ctx, FAE_K_LOSS_JOIN);
+        const dim3 grid((uint32_t)((v * (s.pitch / 4) + 255) / 256)), block(256);
+        if (what->type == FAE_F32)
+            FAE_LAUNCH(ctx, loss_classes_kernel<float>, grid, block, 0, ctx->stream, c);
+        else if (what->type == FAE_BF16)
+            FAE_LAUNCH(ctx, loss_classes_kernel<fae_bf16>, grid, block, 0, ctx->stream, c);
+        else
+            FAE_LAUNCH(ctx, loss_classes_kernel<fae_f16>, grid, block, 0, ctx->stream, c);
+        FAE_LAUNCH_CHECK(ctx);
+    }
+    return FAE_OK;
+}

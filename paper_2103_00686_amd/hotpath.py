@@ -73,7 +73,8 @@ class HotPath:
         torch's current stream at construction.  Every library call is queued there; outputs and workspaces are
         allocated on torch's current stream, so a caller who works on another one orders the two.
 
-        Steps captured into graphs: ``layer_norm_backward`` has a workspace of its own in each graph.  The sparse
+        Steps captured into graphs: ``layer_norm_backward``, ``softmax_loss``, ``clip_gradients`` and their like have a workspace of
+        their own in each graph.  The sparse
         update's is one for all steps of a HotPath (presort leaves the sorted pairs in it), as are the tables that they
         change: graphs of such steps overlap neither each other nor eager steps."""
         self.dev = torch.device("cuda", device)
@@ -326,10 +327,13 @@ class HotPath:
         return B.Norm(x.shape[0], parts, x.shape[-1], gamma, beta, eps, x.dtype, y_dtype)
 
     def _norm_workspace(self, nbytes: int) -> torch.Tensor:
+        return self._call_workspace("norm", nbytes)
+
+    def _call_workspace(self, name: str, nbytes: int) -> torch.Tensor:
         """One for all eager calls, which the context's stream puts in order.  A captured call has its own, in its graph's
         memory: graphs may be replayed beside each other and beside eager calls."""
         if not torch.cuda.is_current_stream_capturing():
-            return self._workspace("norm", max(nbytes, 1 << 16))
+            return self._workspace(name, max(nbytes, 1 << 16))
         ws = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=self.dev)
         if torch.cuda.current_stream(self.dev).cuda_stream != self.ctx.stream:  # it is dropped before the kernels there have run
             ws.record_stream(torch.cuda.ExternalStream(self.ctx.stream, device=self.dev))
@@ -412,6 +416,70 @@ class HotPath:
 
     def prepare_dropout_backward(self, drop: B.Drop, gy: torch.Tensor, gx: torch.Tensor):
         return B.prepare_dropout_bwd(self.ctx, drop, gy, gx)
+
+    # -- softmax cross entropy over the rows of a table, and its gradients ---------------------
+    def _classes(self, w) -> torch.Tensor:
+        """A matrix of classes, or the hot rows of a table by its number."""
+        return self.hotW[w][:self.n_hot[w]] if isinstance(w, int) else w
+
+    def softmax_loss(self, x: torch.Tensor, w, targets: torch.Tensor, bias: Optional[torch.Tensor] = None, scale: float = 1.0,
+                     keep: bool = False):
+        """(loss, lse) of every row of x, [rows, width], over the classes w: [classes, width], or a hot table's number (then
+        targets are slots, and -1, a cold row, is no target).  keep: (loss, lse, mean) for ``softmax_loss_backward``."""
+        w = self._classes(w)
+        what = B.SoftmaxLoss(x.shape[0], w.shape[0], x.shape[-1], targets, bias, scale, x.dtype)
+        loss, lse = (torch.empty(x.shape[0], dtype=torch.float32, device=self.dev) for _ in range(2))
+        mean = torch.empty(tuple(x.shape), dtype=torch.float32, device=self.dev) if keep else None
+        B.fae_softmax_loss_fwd(self.ctx, what, x, w, loss, lse, mean,
+                               self._call_workspace("loss", B.fae_softmax_loss_fwd_workspace_bytes(what)))
+        return (loss, lse, mean) if keep else (loss, lse)
+
+    def softmax_loss_backward(self, x: torch.Tensor, w, targets: torch.Tensor, lse: torch.Tensor, gloss: torch.Tensor,
+                              mean: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, scale: float = 1.0):
+        """(gx, gw), or (gx, gw, gbias) with a bias, from the gradient gloss of every row's loss; lse and mean from ``softmax_loss``."""
+        w = self._classes(w)
+        what = B.SoftmaxLoss(x.shape[0], w.shape[0], x.shape[-1], targets, bias, scale, x.dtype)
+        gx, gw = (torch.empty(tuple(t.shape), dtype=x.dtype, device=self.dev) for t in (x, w))
+        gbias = torch.empty(w.shape[0], dtype=torch.float32, device=self.dev) if bias is not None else None
+        B.fae_softmax_loss_bwd(self.ctx, what, x, w, lse, mean, gloss, gx, gw, gbias,
+                               self._call_workspace("loss", B.fae_softmax_loss_bwd_workspace_bytes(what)))
+        return (gx, gw) if bias is None else (gx, gw, gbias)
+
+    # -- norm of all gradients together, and clipping by it ------------------------------------
+    def gradient_norm(self, grads: Sequence[torch.Tensor], scale: float = 1.0) -> torch.Tensor:
+        """The norm of all values of all tensors, times |scale|, as one fp32 value on the device."""
+        norm = torch.empty((), dtype=torch.float32, device=self.dev)
+        B.fae_grad_norm(self.ctx, grads, scale, norm, self._call_workspace("grads", B.fae_grad_workspace_bytes(len(grads))))
+        return norm
+
+    def clip_gradients(self, grads: Sequence[torch.Tensor], max_norm: float, scale: float = 1.0,
+                       out: Optional[Sequence[torch.Tensor]] = None) -> torch.Tensor:
+        """Multiplies all gradients (in place, or into out) by scale and by what brings their norm down to max_norm; returns the norm
+        before that."""
+        norm = torch.empty((), dtype=torch.float32, device=self.dev)
+        B.fae_grad_clip(self.ctx, grads, scale, max_norm, norm, self._call_workspace("grads", B.fae_grad_workspace_bytes(len(grads))), out)
+        return norm
+
+    # their pre-marshalled forms, with workspaces of their own (prepare_layer_norm_backward says how long they have to live)
+    def _own_workspace(self, nbytes: int) -> torch.Tensor:
+        return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=self.dev)
+
+    def prepare_softmax_loss(self, what: B.SoftmaxLoss, x: torch.Tensor, w: torch.Tensor, loss: Optional[torch.Tensor],
+                             lse: Optional[torch.Tensor], mean: Optional[torch.Tensor] = None):
+        return B.prepare_softmax_loss_fwd(self.ctx, what, x, w, loss, lse, mean, self._own_workspace(B.fae_softmax_loss_fwd_workspace_bytes(what)))
+
+    def prepare_softmax_loss_backward(self, what: B.SoftmaxLoss, x: torch.Tensor, w: torch.Tensor, lse: torch.Tensor, gloss: torch.Tensor,
+                                      gx: Optional[torch.Tensor], gw: Optional[torch.Tensor], gbias: Optional[torch.Tensor] = None,
+                                      mean: Optional[torch.Tensor] = None):
+        return B.prepare_softmax_loss_bwd(self.ctx, what, x, w, lse, mean, gloss, gx, gw, gbias,
+                                          self._own_workspace(B.fae_softmax_loss_bwd_workspace_bytes(what)))
+
+    def prepare_gradient_norm(self, grads: Sequence[torch.Tensor], norm: torch.Tensor, scale: float = 1.0):
+        return B.prepare_grad_norm(self.ctx, grads, scale, norm, self._own_workspace(B.fae_grad_workspace_bytes(len(grads))))
+
+    def prepare_clip_gradients(self, grads: Sequence[torch.Tensor], max_norm: float, norm: Optional[torch.Tensor] = None, scale: float = 1.0,
+                               out: Optional[Sequence[torch.Tensor]] = None):
+        return B.prepare_grad_clip(self.ctx, grads, scale, max_norm, norm, self._own_workspace(B.fae_grad_workspace_bytes(len(grads))), out)
 
     def sync(self):
         B.fae_sync(self.ctx)
