@@ -408,9 +408,11 @@ int32_t fae_dropout_bwd(fae_ctx *ctx, const fae_drop *drop, int64_t n_rows, int3
  *   loss[r] = lse[r] - z[r][target[r]],  0 for a row without a target
  * x is [n_rows] rows of `width` values, x_row_stride values apart, w [n_classes] rows, w_row_stride apart, of one type:
  * FAE_F32, FAE_BF16 or FAE_F16.  Values between rows are neither read nor written, buffers need the alignment of
- * their values.  Products of 16-bit values are exact and their sums fp32; fp32 values are taken as three bf16 numbers
- * each, whose six largest products are summed in fp32 (what is left out is below 2^-23 of a product).  Probabilities enter the
- * gradients' sums rounded to the type (fp32: as three bf16 numbers again).  x and w have to be finite.
+ * their values.  Products of 16-bit values are exact and their sums fp32.  An fp32 value is taken as the sum of two fp16 numbers, after a power
+ * of two that brings the largest value of its row, or of all rows, to 2^14 .. 2^15 (calls with few rows: as three bf16 numbers, without one);
+ * of a product at most 2^-20 is lost, and a value below 2^-18 of that largest is kept to 2^-39 of it.  Probabilities enter the gradients'
+ * sums rounded to the type (fp32: as two or three numbers again).  x and w have to be finite; in the gradients, rows
+ * without a target may hold anything.
  *   targets: int32 or int64 (target_bits), one per row.  A negative one is a row without a target (a cold row, padding):
  *     its loss is 0, its gradients are 0 and it adds nothing to gw and gbias.  One of n_classes or more is treated so too,
  *     and reported as FAE_ERANGE by the next synchronising call.

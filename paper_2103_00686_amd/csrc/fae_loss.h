@@ -5,8 +5,8 @@
 
 // Both directions stream rows past rows that a wave holds: Z = (streamed rows) x (held rows)^T by matrix instructions, P = a function of Z in
 // registers, O += (streamed rows)^T x P by matrix instructions.
-//   LOSS_STATS  held: x, streamed: w; running maximum and sum of 2^Z for every row of x, and the target's Z
-//   LOSS_MEAN   the same, and O = the sum of 2^Z w of all classes but the target
+//   LOSS_STATS  held: x, streamed: w; reference and sum of 2^(Z - reference) for every row of x, and the target's Z
+//   LOSS_MEAN   the same, and O = the sum of 2^(Z - reference) w of all classes but the target
 //   LOSS_GRAD   held: w, streamed: x; P = gloss (2^(Z - lse) - (class is the target)), O = the sum of P x, and the sum of P (bias)
 // Z is in units of log 2 throughout.
 enum { LOSS_STATS, LOSS_MEAN, LOSS_GRAD };
@@ -20,9 +20,11 @@ struct loss_args {
     const float *bias;    // fp32[n_classes] or NULL
     const void *targets;  // forward
     int32_t target_bits, n_classes;
-    const float *nlse, *g;  // gradient, per streamed row: -lse * log2(e), gloss (0 without a target)
-    const int32_t *t;       // ... and its target or -1
-    const uint32_t *g_most; // fp16: the bits of the largest |gloss|
+    const float *st_most; // fp32 as fp16 numbers: n_most values, the largest of them is the largest streamed value
+    const float *g_most;  // gradient with fp16 numbers: the same of |gloss|
+    int32_t n_most;
+    const float *nlse, *g; // gradient, per streamed row: -lse * log2(e) + log2 |gloss|, gloss (-infinity and 0 without a target)
+    const int32_t *t;      // ... and its target or -1
     uint32_t *status;
     float *stat; // forward: [n_split][n_own][2]: reference, sum of 2^(Z - reference)
     float *zt;   // forward: [n_own] Z of the target
@@ -36,14 +38,36 @@ struct loss_args {
     uint32_t n_blocks, n_split;
 };
 
+// What a kernel is built for: the types, and fp32 in two ways (loss_type says how).
+enum { LOSS_F32, LOSS_BF16, LOSS_F16, LOSS_F32_WIDE };
+constexpr int loss_planes_of(int how) { return how == LOSS_F32 ? 3 : how == LOSS_F32_WIDE ? 2 : 1; }
 static inline int loss_padded(int32_t width) { return width <= 32 ? 32 : width <= 64 ? 64 : width <= 96 ? 96 : width <= 128 ? 128 : width <= 192 ? 192 : 256; }
-static inline int loss_tile(int32_t type, int dp) { return type == FAE_F32 && dp > 128 ? 32 : 64; }
+constexpr int loss_tile(int how, int dp) { return how == LOSS_F32 && dp > 128 ? 32 : 64; }
+// held rows of a wave, in blocks of 32: two where their registers leave room for two waves on a SIMD
+#ifdef TRY_NB
+constexpr int loss_blocks(int how, int dp, int mode) { return TRY_NB; }
+#else
+constexpr int loss_blocks(int how, int dp, int mode)
+{
+    return loss_planes_of(how) > 1 ? (dp <= 32 ? 2 : 1) : (dp <= (mode == LOSS_STATS ? 128 : 64) ? 2 : 1);
+}
+#endif
+// waves per SIMD that registers are left for: one where more than half of a SIMD's are needed
+constexpr int loss_waves(int how, int dp, int mode)
+{
+#ifdef TRY_W
+    if (dp <= 64)
+        return TRY_W;
+#endif
+    return mode == LOSS_STATS ? (loss_planes_of(how) > 1 && dp > 128 ? 1 : 2) : (dp <= (loss_planes_of(how) > 1 ? 64 : 128) ? 2 : 1);
+}
 #define LOSS_WAVES 4
-#define LOSS_HELD (LOSS_WAVES * 32) // held rows of a workgroup
+constexpr int loss_held(int how, int dp, int mode) { return LOSS_WAVES * 32 * loss_blocks(how, dp, mode); }
 
 void loss_launch_f32(fae_ctx *ctx, int mode, const loss_args &a);
 void loss_launch_bf16(fae_ctx *ctx, int mode, const loss_args &a);
 void loss_launch_f16(fae_ctx *ctx, int mode, const loss_args &a);
+void loss_launch_f32_wide(fae_ctx *ctx, int mode, const loss_args &a);
 
 // a row's target, or -1; one that is no class is reported
 #ifdef __HIPCC__
@@ -61,24 +85,39 @@ __device__ __forceinline__ int32_t loss_target(const void *targets, int32_t bits
 typedef float loss_f16v __attribute__((ext_vector_type(16)));
 typedef float loss_f4 __attribute__((ext_vector_type(4)));
 
-// How a type enters the matrix instructions: as PLANES numbers of E, whose sum is the value (fp32: 24 bits are three times eight;
-// fp32's own matrix instructions have a sixteenth of bf16's rate, six products of bf16 take three eighths of their time).
+// How values enter the matrix instructions: as PLANES numbers of E whose sum is the value, with the PRODUCTS largest products of them.  fp32's
+// own matrix instructions have a sixteenth of bf16's rate.
+//   LOSS_F32       three bf16 numbers, 24 bits with fp32's range: six products
+//   LOSS_F32_WIDE  two fp16 numbers, 22 bits and more (rounded to nearest both times), three products; values are multiplied by a power of two
+//                  first that brings the largest of a held row, or of all streamed rows, to 2^14 .. 2^15, where values down
+//                  to 2^-18 of it keep all their bits.  Costs a look at all streamed rows before.
 // SHIFT: probabilities are multiplied by 2^SHIFT (fp16 has nothing below 2^-24, and a million classes have probabilities of 2^-20).
-// SLACK: how far above 1 they may be before the reference moves (a running maximum that moves rarely).
-template <typename T> struct loss_type;
-template <> struct loss_type<fae_bf16> {
-    typedef fae_bf16 E;
-    static constexpr int PLANES = 1, PRODUCTS = 1, SHIFT = 0, SLACK = 16;
+// MOST: the reference moves when a lane's sum of 16 of them reaches it.  They are then below fp16's 65504; the other types, with
+// fp32's range, let the reference lag far behind the maximum, which costs no precision and spares them the search for it.
+template <int HOW> struct loss_type;
+template <> struct loss_type<LOSS_BF16> {
+    typedef fae_bf16 T, E;
+    static constexpr int PLANES = 1, PRODUCTS = 1, SHIFT = 0;
+    static constexpr float MOST = 0x1p40f;
 };
-template <> struct loss_type<fae_f16> {
+template <> struct loss_type<LOSS_F16> {
+    typedef fae_f16 T, E;
+    static constexpr int PLANES = 1, PRODUCTS = 1, SHIFT = 10;
+    static constexpr float MOST = 0x1p15f;
+};
+template <> struct loss_type<LOSS_F32> {
+    typedef float T;
+    typedef fae_bf16 E;
+    static constexpr int PLANES = 3, PRODUCTS = 6, SHIFT = 0;
+    static constexpr float MOST = 0x1p40f;
+};
+template <> struct loss_type<LOSS_F32_WIDE> {
+    typedef float T;
     typedef fae_f16 E;
-    static constexpr int PLANES = 1, PRODUCTS = 1, SHIFT = 12, SLACK = 3;
+    static constexpr int PLANES = 2, PRODUCTS = 3, SHIFT = 10;
+    static constexpr float MOST = 0x1p15f;
 };
-template <> struct loss_type<float> {
-    typedef fae_bf16 E;
-    static constexpr int PLANES = 3, PRODUCTS = 6, SHIFT = 0, SLACK = 16;
-};
-// the products of planes that are summed, small ones first; with one plane the last
+// the products of planes that are summed, small ones first: the last PRODUCTS of these
 static constexpr int LOSS_PA[6] = {2, 1, 0, 1, 0, 0}, LOSS_PB[6] = {0, 1, 2, 0, 1, 0};
 
 template <typename E> struct loss_vec {
@@ -95,22 +134,33 @@ __device__ __forceinline__ loss_f16v loss_mfma(loss_vec<fae_f16>::v8 a, loss_vec
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
 
-// fp32 values as three bf16 numbers each (rounded to nearest, so that what is left out has either sign)
-template <typename T, typename E> __device__ __forceinline__ void loss_split(const float (&v)[8], typename loss_vec<E>::v8 (&o)[loss_type<T>::PLANES])
+// eight fp32 values as planes, each rounded to nearest so that what is left has either sign
+template <int HOW> __device__ __forceinline__ void loss_split(const float (&v)[8], typename loss_vec<typename loss_type<HOW>::E>::v8 (&o)[loss_type<HOW>::PLANES])
 {
+    typedef typename loss_type<HOW>::E E;
     float r[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e)
         r[e] = v[e];
 #pragma unroll
-    for (int p = 0; p < loss_type<T>::PLANES; ++p) {
+    for (int p = 0; p < loss_type<HOW>::PLANES; ++p) {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
             o[p][e] = (E)r[e];
-        if (p + 1 < loss_type<T>::PLANES) {
+        if (p + 1 < loss_type<HOW>::PLANES) {
+            if constexpr (HOW == LOSS_F32_WIDE) { // a mixed product and sum reads the fp16 number where it is: one instruction
+                typedef uint32_t words __attribute__((ext_vector_type(4)));
+                const words w = __builtin_bit_cast(words, o[p]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                r[e] -= (float)o[p][e];
+                for (int e = 0; e < 8; e += 2) {
+                    asm("v_fma_mix_f32 %0, %0, 1.0, -%1 op_sel_hi:[0,0,1]" : "+v"(r[e]) : "v"(w[e / 2]));
+                    asm("v_fma_mix_f32 %0, %0, 1.0, -%1 op_sel:[0,0,1] op_sel_hi:[0,0,1]" : "+v"(r[e + 1]) : "v"(w[e / 2]));
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    r[e] -= (float)o[p][e];
+            }
         }
     }
 }
@@ -138,15 +188,28 @@ template <typename T> __device__ __forceinline__ loss_raw<T> loss_load(const T *
     }
     return o;
 }
-template <typename T, typename E> __device__ __forceinline__ void loss_planes(const loss_raw<T> &x, typename loss_vec<E>::v8 (&o)[loss_type<T>::PLANES])
+template <int HOW>
+__device__ __forceinline__ void loss_planes(const loss_raw<typename loss_type<HOW>::T> &x, float scale,
+                                            typename loss_vec<typename loss_type<HOW>::E>::v8 (&o)[loss_type<HOW>::PLANES])
 {
-    if constexpr (sizeof(T) == 2) {
+    if constexpr (HOW == LOSS_BF16 || HOW == LOSS_F16) {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
             o[0][e] = x.v[e];
     } else {
-        loss_split<T, E>(x.v, o);
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            v[e] = HOW == LOSS_F32_WIDE ? x.v[e] * scale : x.v[e];
+        loss_split<HOW>(v, o);
     }
+}
+
+// the power of two that brings `most` to 2^(top - 1) .. 2^top, and none for 0 and what is not finite
+__device__ __forceinline__ int loss_power(float most, int top)
+{
+    const int up = top - __builtin_amdgcn_frexp_expf(most);
+    return most > 0.f && most < INFINITY ? (up < 120 ? up : 120) : 0;
 }
 
 // A tile's row lies in LDS without padding; its 16-byte pieces are placed by an exclusive or with some bits of the row, so that both kinds of reads
@@ -157,18 +220,25 @@ template <int DP> __device__ __forceinline__ int loss_swizzle(int m)
     return u == 0 ? ((m & 3) << 2) | ((m >> 2) & 3) : u == 8 ? ((m & 2) << 1) | ((m >> 2) & 3) : (m >> 2) & 3;
 }
 
-template <typename T, int DP, int MODE> __global__ __launch_bounds__(LOSS_WAVES * 64) void loss_kernel(loss_args a)
+#define LOSS_LDS(T) __attribute__((address_space(3))) T
+
+template <int HOW, int DP, int MODE, bool BIAS>
+__global__ __launch_bounds__(LOSS_WAVES * 64) __attribute__((amdgpu_waves_per_eu(loss_waves(HOW, DP, MODE)))) void loss_kernel(loss_args a)
 {
-    typedef typename loss_type<T>::E E;
+    typedef loss_type<HOW> H;
+    typedef typename H::T T;
+    typedef typename H::E E;
     typedef typename loss_vec<E>::v8 v8;
     typedef typename loss_vec<E>::v4 v4;
-    constexpr int P = loss_type<T>::PLANES, NP = loss_type<T>::PRODUCTS, THREADS = LOSS_WAVES * 64;
-    constexpr int TM = P == 3 && DP > 128 ? 32 : 64;
-    constexpr int KS = DP / 16, NC = TM * DP / 8 / THREADS;
+    typedef short s4 __attribute__((ext_vector_type(4)));
+    constexpr int P = H::PLANES, NP = H::PRODUCTS, THREADS = LOSS_WAVES * 64, NB = loss_blocks(HOW, DP, MODE), TM = loss_tile(HOW, DP);
+    constexpr int KS = DP / 16, DS = DP / 32, NC = TM * DP / 8 / THREADS;
+    constexpr int PLANE = TM * DP * 2, TILE = P * PLANE; // bytes
     constexpr bool HAS_O = MODE != LOSS_STATS;
     static_assert(TM * DP / 8 % THREADS == 0, "whole pieces per thread");
-    __shared__ E tile[2][P][TM * DP];
-    __shared__ float side[2][3][TM]; // forward: bias; gradient: -lse, gloss, target
+    __shared__ __attribute__((aligned(16))) char tiles[2 * TILE];
+    __shared__ float side[2][3][TM]; // forward: bias; gradient: -lse + log |gloss|, gloss, target
+    __shared__ float mosts[2][LOSS_WAVES];
 
     const int lane = fae_lane(), wave = threadIdx.x / 64, ln = lane & 31, half = lane >> 5;
     uint32_t block, split;
@@ -181,38 +251,85 @@ template <typename T, int DP, int MODE> __global__ __launch_bounds__(LOSS_WAVES 
         block = blockIdx.x % a.n_blocks;
     }
     const int tile0 = (int)((int64_t)a.tiles * split / a.n_split), tile1 = (int)((int64_t)a.tiles * (split + 1) / a.n_split);
-    const int n = (int)(block * LOSS_HELD) + wave * 32 + ln; // this lane's held row (may lie behind the last)
-    const bool there = n < a.n_own;
+    const int first = (int)(block * (LOSS_WAVES * 32 * NB)) + wave * 32 * NB; // the wave's held rows; this lane's are first + ln + 32 b (they may lie behind the last)
 
-    // the held row: value 16 k + 8 half + j is element j of operand k
-    v8 q[KS][P];
-    {
+    // What was found before: the largest streamed value and gradient.  fp16 numbers of both are brought to a range that keeps them.
+    float st_scale = 1.f, g_scale = 1.f, g_log = 0.f, c_all = a.c, back = 1.f;
+    if (HOW == LOSS_F32_WIDE || (HOW == LOSS_F16 && MODE == LOSS_GRAD)) {
+        float most[2] = {0.f, 0.f};
+        for (int i = threadIdx.x; i < a.n_most; i += THREADS) {
+            if (HOW == LOSS_F32_WIDE)
+                most[0] = fmaxf(most[0], a.st_most[i]);
+            if (MODE == LOSS_GRAD)
+                most[1] = fmaxf(most[1], a.g_most[i]);
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+#pragma unroll
+            for (int d = 32; d > 0; d >>= 1)
+                most[k] = fmaxf(most[k], __shfl_xor(most[k], d, 64));
+            if (lane == 0)
+                mosts[k][wave] = most[k];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int i = 0; i < LOSS_WAVES; ++i)
+                most[k] = fmaxf(most[k], mosts[k][i]);
+        if (HOW == LOSS_F32_WIDE) {
+            const int up = loss_power(most[0], 15);
+            st_scale = __builtin_amdgcn_ldexpf(1.f, up);
+            back = __builtin_amdgcn_ldexpf(1.f, -up);
+            c_all *= back;
+        }
+        if (MODE == LOSS_GRAD) { // the largest P is 2^12
+            const int up = loss_power(most[1], 12);
+            g_scale = __builtin_amdgcn_ldexpf(1.f, up);
+            g_log = (float)up;
+        }
+    }
+
+    // held rows: value 16 k + 8 half + j is element j of operand k
+    v8 q[NB][KS][P];
+    int32_t target[NB];
+    float own_bias[NB], c[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        const int n = first + b * 32 + ln;
+        const bool there = n < a.n_own;
         const T *row = (const T *)a.own + (int64_t)n * a.own_stride;
+        float scale = a.flip ? -1.f : 1.f;
+        c[b] = c_all;
+        if (HOW == LOSS_F32_WIDE) {
+            float most = 0.f;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                const loss_raw<T> x = loss_load<T>(row, k * 16 + half * 8, a.width, there);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    most = fmaxf(most, fabsf((float)x.v[e]));
+            }
+            most = fmaxf(most, __shfl_xor(most, 32, 64));
+            const int up = loss_power(most, 15);
+            scale = __builtin_amdgcn_ldexpf(scale, up);
+            c[b] = __builtin_amdgcn_ldexpf(c_all, -up);
+        }
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
             loss_raw<T> x = loss_load<T>(row, k * 16 + half * 8, a.width, there);
-            if (a.flip) {
+            if (HOW != LOSS_F32_WIDE && a.flip) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
                     x.v[e] = -x.v[e];
             }
-            loss_planes<T, E>(x, q[k]);
+            loss_planes<HOW>(x, scale, q[b][k]);
         }
-    }
-    int32_t target = -1;
-    if (MODE != LOSS_GRAD && there)
-        target = loss_target(a.targets, a.target_bits, n, a.n_classes, a.status);
-    float own_bias = 0.f, g_scale = 1.f;
-    if (MODE == LOSS_GRAD) {
-        if (there && a.bias)
-            own_bias = a.bias[n] * 1.44269504f;
-        if (loss_type<T>::SHIFT) {
-            const float most = __uint_as_float(*a.g_most);
-            // 2^SHIFT is the largest P
-            g_scale = most > 0.f && most < INFINITY ? __builtin_amdgcn_ldexpf(1.f, loss_type<T>::SHIFT - __builtin_amdgcn_frexp_expf(most)) : 1.f;
-        }
+        target[b] = MODE != LOSS_GRAD && there ? loss_target(a.targets, a.target_bits, n, a.n_classes, a.status) : -1;
+        own_bias[b] = MODE == LOSS_GRAD && BIAS && there ? a.bias[n] * 1.44269504f : 0.f;
     }
 
+    // the next tile on its way from memory to LDS
     loss_raw<T> next[NC];
     int32_t next_t[NC];
     float next_side[3];
@@ -220,8 +337,8 @@ template <typename T, int DP, int MODE> __global__ __launch_bounds__(LOSS_WAVES 
         const int m0 = tl * TM;
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
-            const int piece = i * THREADS + threadIdx.x, m = piece / (DP / 8), c = piece % (DP / 8);
-            next[i] = loss_load<T>((const T *)a.st + (int64_t)(m0 + m) * a.st_stride, c * 8, a.width, m0 + m < a.n_st);
+            const int piece = i * THREADS + threadIdx.x, m = piece / (DP / 8), p = piece % (DP / 8);
+            next[i] = loss_load<T>((const T *)a.st + (int64_t)(m0 + m) * a.st_stride, p * 8, a.width, m0 + m < a.n_st);
             if (MODE == LOSS_GRAD)
                 next_t[i] = m0 + m < a.n_st ? a.t[m0 + m] : -1;
         }
@@ -229,27 +346,27 @@ template <typename T, int DP, int MODE> __global__ __launch_bounds__(LOSS_WAVES 
             const int m = m0 + threadIdx.x;
             const bool in = m < a.n_st;
             if (MODE == LOSS_GRAD) {
-                next_side[0] = in ? a.nlse[m] : -INFINITY;
+                next_side[0] = in ? a.nlse[m] + g_log : -INFINITY;
                 next_side[1] = in ? a.g[m] * g_scale : 0.f;
                 next_side[2] = __int_as_float(in ? a.t[m] : -1);
             } else
-                next_side[0] = !in ? -INFINITY : (a.bias ? a.bias[m] * 1.44269504f : 0.f);
+                next_side[0] = !in ? -INFINITY : (BIAS ? a.bias[m] * 1.44269504f : 0.f);
         }
     };
     auto place = [&](int buf) {
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
-            const int piece = i * THREADS + threadIdx.x, m = piece / (DP / 8), c = piece % (DP / 8);
+            const int piece = i * THREADS + threadIdx.x, m = piece / (DP / 8), p = piece % (DP / 8);
             v8 o[P];
             if (MODE == LOSS_GRAD) { // a row without a target may hold anything, and 0 times that is not always 0
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
                     next[i].v[e] = next_t[i] < 0 ? (T)0.f : next[i].v[e];
             }
-            loss_planes<T, E>(next[i], o);
+            loss_planes<HOW>(next[i], st_scale, o);
 #pragma unroll
-            for (int p = 0; p < P; ++p)
-                *(v8 *)&tile[buf][p][m * DP + (c ^ loss_swizzle<DP>(m)) * 8] = o[p];
+            for (int k = 0; k < P; ++k)
+                *(v8 *)&tiles[buf * TILE + k * PLANE + m * DP * 2 + (p ^ loss_swizzle<DP>(m)) * 16] = o[k];
         }
         if (threadIdx.x < TM) {
             side[buf][0][threadIdx.x] = next_side[0];
@@ -260,14 +377,31 @@ template <typename T, int DP, int MODE> __global__ __launch_bounds__(LOSS_WAVES 
         }
     };
 
-    loss_f16v o[HAS_O ? DP / 32 : 1];
-    if (HAS_O) {
+    // where this lane reads in a tile: for Z 16 bytes of row ln; for O 16 lanes take 4 rows of 16 columns, and each gets its column's 4 values
+    uint32_t z_at[KS], o_at[DS][2];
 #pragma unroll
-        for (int d = 0; d < DP / 32; ++d)
-            o[d] = (loss_f16v)(0.f);
-    }
+    for (int k = 0; k < KS; ++k)
+        z_at[k] = ln * DP * 2 + ((k * 2 + half) ^ loss_swizzle<DP>(ln)) * 16;
+#pragma unroll
+    for (int d = 0; d < DS; ++d)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int m = u * 8 + half * 4 + ((lane & 15) >> 2), p = d * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+            o_at[d][u] = m * DP * 2 + (p ^ loss_swizzle<DP>(m)) * 16 + (lane & 1) * 8;
+        }
+    LOSS_LDS(char) *const lds = (LOSS_LDS(char) *)tiles;
+
+    loss_f16v o[NB][HAS_O ? DS : 1];
     // Forward: 2^(Z - ref) is what is summed.  Gradient: sum is that of P.
-    float ref = -3.402823466e38f, sum = 0.f;
+    float ref[NB], sum[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+#pragma unroll
+        for (int d = 0; d < (HAS_O ? DS : 1); ++d)
+            o[b][d] = (loss_f16v)(0.f);
+        ref[b] = -3.402823466e38f;
+        sum[b] = 0.f;
+    }
     if (tile0 < tile1) {
         fetch(tile0);
         place(0);
@@ -278,125 +412,173 @@ template <typename T, int DP, int MODE> __global__ __launch_bounds__(LOSS_WAVES 
         const bool more = tl + 1 < tile1;
         if (more)
             fetch(tl + 1);
+        const bool biased = BIAS || (tl + 1) * (int64_t)TM > a.n_st; // forward: also where the last tile has fewer rows
 #pragma unroll 1
         for (int sb = 0; sb < TM / 32; ++sb) {
-            // Z: element i is streamed row 8 (i / 4) + 4 half + i % 4 and held row ln
-            loss_f16v z = (loss_f16v)(0.f);
-#pragma unroll
-            for (int k = 0; k < KS; ++k) {
-                v8 x[P];
+            // Z: element i is streamed row 8 (i / 4) + 4 half + i % 4 and held row ln.  One held block after the other: a matrix instruction that
+            // waits for the one before leaves the vector unit to the SIMD's other waves, one that waits for the matrix unit does not
+            // (24 of them beside 200 vector instructions: 503 ns in one chain, 577 in two).
+            loss_f16v z[NB];
+            auto streamed = [&](int k, v8 (&x)[P]) {
 #pragma unroll
                 for (int p = 0; p < P; ++p)
-                    x[p] = *(const v8 *)&tile[buf][p][(sb * 32 + ln) * DP + ((k * 2 + half) ^ loss_swizzle<DP>(ln)) * 8];
+                    x[p] = *(LOSS_LDS(const v8) *)(lds + (z_at[k] + buf * TILE) + (p * PLANE + sb * 32 * DP * 2));
+            };
+            v8 x[NB > 1 ? KS : 1][P];
 #pragma unroll
-                for (int u = 6 - NP; u < 6; ++u)
-                    z = loss_mfma(x[LOSS_PA[u]], q[k][LOSS_PB[u]], z);
+            for (int b = 0; b < NB; ++b) {
+                z[b] = (loss_f16v)(0.f);
+#pragma unroll
+                for (int k = 0; k < KS; ++k) {
+                    v8(&xk)[P] = x[NB > 1 ? k : 0];
+                    if (b == 0)
+                        streamed(k, xk);
+#pragma unroll
+                    for (int u = 6 - NP; u < 6; ++u)
+                        z[b] = loss_mfma(xk[LOSS_PA[u]], q[b][k][LOSS_PB[u]], z[b]);
+                }
             }
-            float pr[16];
+            float pr[NB][16];
             const float *sd = &side[buf][0][sb * 32 + half * 4];
             if (MODE == LOSS_GRAD) {
 #pragma unroll
-                for (int b = 0; b < 4; ++b) {
-                    const loss_f4 nl = *(const loss_f4 *)(sd + b * 8), g = *(const loss_f4 *)(sd + TM + b * 8);
+                for (int j = 0; j < 4; ++j) {
+                    const loss_f4 nl = *(const loss_f4 *)(sd + j * 8);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int i = b * 4 + e;
-                        pr[i] = __builtin_amdgcn_exp2f(fmaf(z[i], a.c, own_bias + nl[e])) * g[e];
-                    }
-                }
-                // a target in this wave's classes
-                const int32_t mine = __float_as_int(side[buf][2][sb * 32 + ln]);
-                const int first = (int)(block * LOSS_HELD) + wave * 32;
-                if (__any(mine >= first && mine < first + 32)) {
-#pragma unroll
-                    for (int b = 0; b < 4; ++b) {
-                        const loss_f4 g = *(const loss_f4 *)(sd + TM + b * 8), t = *(const loss_f4 *)(sd + 2 * TM + b * 8);
+                    for (int b = 0; b < NB; ++b)
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            pr[b * 4 + e] -= __float_as_int(t[e]) == n ? g[e] : 0.f;
+                            pr[b][j * 4 + e] = __builtin_amdgcn_exp2f(fmaf(z[b][j * 4 + e], c[b], BIAS ? own_bias[b] + nl[e] : nl[e]));
+                }
+                // a target in this wave's classes, or a gradient below 0: seldom
+                const int32_t mine = __float_as_int(side[buf][2][sb * 32 + ln]);
+                if (__any((mine >= first && mine < first + 32 * NB) || side[buf][1][sb * 32 + ln] < 0.f)) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const loss_f4 g = *(const loss_f4 *)(sd + TM + j * 8), t = *(const loss_f4 *)(sd + 2 * TM + j * 8);
+#pragma unroll
+                        for (int b = 0; b < NB; ++b)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const float v = pr[b][j * 4 + e];
+                                pr[b][j * 4 + e] = (g[e] < 0.f ? -v : v) - (__float_as_int(t[e]) == first + b * 32 + ln ? g[e] : 0.f);
+                            }
                     }
                 }
-                float some = 0.f;
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    some += pr[i];
-                sum += some;
-            } else {
-                float most = -INFINITY;
-#pragma unroll
-                for (int b = 0; b < 4; ++b) {
-                    const loss_f4 bs = *(const loss_f4 *)(sd + b * 8);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        z[b * 4 + e] = fmaf(z[b * 4 + e], a.c, bs[e]);
-                        most = fmaxf(most, z[b * 4 + e]);
-                    }
-                }
-                if (__any(most > ref + (float)loss_type<T>::SLACK)) {
-                    most = fmaxf(most, __shfl_xor(most, 32, 64));
-                    const float to = most > ref + (float)loss_type<T>::SLACK ? most : ref;
-                    const float f = __builtin_amdgcn_exp2f(ref - to);
-                    ref = to;
-                    sum *= f;
-                    if (HAS_O) {
-#pragma unroll
-                        for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-                            for (int i = 0; i < 16; ++i)
-                                o[d][i] *= f;
-                    }
-                }
-                float some = 0.f;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    pr[i] = __builtin_amdgcn_exp2f(z[i] - (ref - (float)loss_type<T>::SHIFT));
-                    some += pr[i];
-                }
-                sum += some;
-                const int at = target - tl * TM - sb * 32;
-                if (__any((unsigned)at < 32u)) {
+                for (int b = 0; b < NB; ++b) {
+                    float some = 0.f;
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
-                        if (8 * (i / 4) + 4 * half + i % 4 == at) {
-                            a.zt[n] = z[i];
-                            pr[i] = 0.f;
+                        some += pr[b][i];
+                    sum[b] += some;
+                }
+            } else {
+                float some[NB];
+                auto powers = [&](int b) {
+                    const float off = ref[b] - (float)H::SHIFT;
+                    if (biased) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const loss_f4 bs = *(const loss_f4 *)(sd + j * 8);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                pr[b][j * 4 + e] = __builtin_amdgcn_exp2f(fmaf(z[b][j * 4 + e], c[b], bs[e] - off));
                         }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            pr[b][i] = __builtin_amdgcn_exp2f(fmaf(z[b][i], c[b], -off));
+                    }
+                    some[b] = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        some[b] += pr[b][i];
+                };
+                bool over = false;
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    powers(b);
+                    over = over || !(some[b] < H::MOST);
+                }
+                if (__any(over)) { // a held row's reference (both halves of its lanes) moves to the maximum of its scores so far
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) {
+                        const bool moves = !(fmaxf(some[b], __shfl_xor(some[b], 32, 64)) < H::MOST) || some[b] != some[b];
+                        float to = ref[b];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const loss_f4 bs = *(const loss_f4 *)(sd + j * 8);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                to = fmaxf(to, fmaf(z[b][j * 4 + e], c[b], bs[e]));
+                        }
+                        const float pair = fmaxf(to, __shfl_xor(to, 32, 64));
+                        to = moves ? pair : ref[b];
+                        const float f = __builtin_amdgcn_exp2f(ref[b] - to);
+                        ref[b] = to;
+                        sum[b] *= f;
+                        if (HAS_O) {
+#pragma unroll
+                            for (int d = 0; d < DS; ++d)
+#pragma unroll
+                                for (int i = 0; i < 16; ++i)
+                                    o[b][d][i] *= f;
+                        }
+                        powers(b);
+                    }
+                }
+                bool hit = false;
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    sum[b] += some[b];
+                    hit = hit || (unsigned)(target[b] - tl * TM - sb * 32) < 32u;
+                }
+                if (__any(hit)) { // the target's score, and no part of it in the mean
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) {
+                        const int at = target[b] - tl * TM - sb * 32;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (8 * (i / 4) + 4 * half + i % 4 == at) {
+                                a.zt[first + b * 32 + ln] = fmaf(z[b][i], c[b], sd[i / 4 * 8 + i % 4]);
+                                pr[b][i] = 0.f;
+                            }
+                    }
                 }
             }
             if (HAS_O) {
                 // eight streamed rows of a lane are the eight of an operand: rows 16 t + 4 half + {0..3, 8..11}
-                v8 pb[2][P];
+                v8 pb[NB][2][P];
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    float v[8];
+                for (int b = 0; b < NB; ++b)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        v[e] = pr[t * 8 + e];
-                    loss_split<T, E>(v, pb[t]);
-                }
+                    for (int t = 0; t < 2; ++t) {
+                        float v[8];
 #pragma unroll
-                for (int d = 0; d < DP / 32; ++d) {
+                        for (int e = 0; e < 8; ++e)
+                            v[e] = pr[b][t * 8 + e];
+                        loss_split<HOW>(v, pb[b][t]);
+                    }
+#pragma unroll
+                for (int d = 0; d < DS; ++d) {
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
                         v8 x[P];
 #pragma unroll
                         for (int p = 0; p < P; ++p) {
-                            typedef short s4 __attribute__((ext_vector_type(4)));
-                            typedef __attribute__((address_space(3))) s4 *lds4;
                             s4 w[2];
 #pragma unroll
-                            for (int u = 0; u < 2; ++u) {
-                                // 16 lanes take 4 rows of 16 columns; each gets its column's 4 values
-                                const int m = sb * 32 + t * 16 + u * 8 + half * 4 + ((lane & 15) >> 2);
-                                const int c = d * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
-                                E *at = &tile[buf][p][m * DP + (c ^ loss_swizzle<DP>(m)) * 8 + (lane & 1) * 4];
-                                w[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)at);
-                            }
+                            for (int u = 0; u < 2; ++u)
+                                w[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                    (LOSS_LDS(s4) *)(lds + (o_at[d][u] + buf * TILE) + (p * PLANE + (sb * 32 + t * 16) * DP * 2)));
                             x[p] = __builtin_shufflevector(__builtin_bit_cast(v4, w[0]), __builtin_bit_cast(v4, w[1]), 0, 1, 2, 3, 4, 5, 6, 7);
                         }
 #pragma unroll
-                        for (int u = 6 - NP; u < 6; ++u)
-                            o[d] = loss_mfma(x[LOSS_PA[u]], pb[t][LOSS_PB[u]], o[d]);
+                        for (int b = 0; b < NB; ++b)
+#pragma unroll
+                            for (int u = 6 - NP; u < 6; ++u)
+                                o[b][d] = loss_mfma(x[LOSS_PA[u]], pb[b][t][LOSS_PB[u]], o[b][d]);
                     }
                 }
             }
@@ -406,67 +588,72 @@ template <typename T, int DP, int MODE> __global__ __launch_bounds__(LOSS_WAVES 
         __syncthreads();
     }
 
-    sum += __shfl_xor(sum, 32, 64);
-    if (!there)
-        return;
-    const int64_t at = (int64_t)split * a.n_own + n;
-    if (MODE != LOSS_GRAD) {
-        if (half == 0) {
-            a.stat[at * 2] = ref - (float)loss_type<T>::SHIFT;
-            a.stat[at * 2 + 1] = sum;
-        }
-    } else if (half == 0) {
-        if (a.n_split > 1 && a.psum)
-            a.psum[at] = sum / g_scale;
-        else if (a.n_split == 1 && a.out_sum)
-            a.out_sum[n] = sum / g_scale;
-    }
-    if (HAS_O) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        const int n = first + b * 32 + ln;
+        const float all = sum[b] + __shfl_xor(sum[b], 32, 64);
+        const int64_t at = (int64_t)split * a.n_own + n;
         const bool direct = MODE == LOSS_GRAD && a.n_split == 1;
-        const float f = MODE == LOSS_GRAD ? (direct ? a.scale : 1.f) / g_scale : 1.f;
-        if (direct && !a.out)
-            return;
+        if (n < a.n_own && half == 0) {
+            if (MODE != LOSS_GRAD) {
+                a.stat[at * 2] = ref[b] - (float)H::SHIFT;
+                a.stat[at * 2 + 1] = all;
+            } else if (!direct && a.psum)
+                a.psum[at] = all / g_scale;
+            else if (direct && a.out_sum)
+                a.out_sum[n] = all / g_scale;
+        }
+        if (HAS_O && n < a.n_own && (direct ? a.out != nullptr : a.part != nullptr)) {
+            const float f = MODE == LOSS_GRAD ? (direct ? a.scale : 1.f) / g_scale : 1.f;
 #pragma unroll
-        for (int d = 0; d < DP / 32; ++d) {
+            for (int d = 0; d < DS; ++d) {
 #pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                const int c = d * 32 + b * 8 + half * 4;
-                float v[4];
+                for (int j = 0; j < 4; ++j) {
+                    const int col = d * 32 + j * 8 + half * 4;
+                    float v[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    v[e] = o[d][b * 4 + e] * f;
-                if (!direct) {
-                    if (c < a.pitch && a.part)
-                        *(loss_f4 *)(a.part + at * a.pitch + c) = loss_f4{v[0], v[1], v[2], v[3]};
-                } else {
-                    fae_place<4> p;
-                    p.set(c, a.width);
-                    fae_store<T, 4, FAE_ANY>((T *)a.out + (int64_t)n * a.out_stride, v, p);
+                    for (int e = 0; e < 4; ++e)
+                        v[e] = o[b][d][j * 4 + e] * back * f;
+                    if (!direct) {
+                        if (col < a.pitch)
+                            *(loss_f4 *)(a.part + at * a.pitch + col) = loss_f4{v[0], v[1], v[2], v[3]};
+                    } else {
+                        fae_place<4> p;
+                        p.set(col, a.width);
+                        fae_store<T, 4, FAE_ANY>((T *)a.out + (int64_t)n * a.out_stride, v, p);
+                    }
                 }
             }
         }
     }
 }
 
-template <typename T, int DP> static void loss_launch_mode(fae_ctx *ctx, int mode, const loss_args &a)
+template <int HOW, int DP, bool BIAS> static void loss_launch_mode(fae_ctx *ctx, int mode, const loss_args &a)
 {
     const dim3 grid(a.n_blocks * a.n_split), block(LOSS_WAVES * 64);
     if (mode == LOSS_STATS)
-        FAE_LAUNCH(ctx, (loss_kernel<T, DP, LOSS_STATS>), grid, block, 0, ctx->stream, a);
+        FAE_LAUNCH(ctx, (loss_kernel<HOW, DP, LOSS_STATS, BIAS>), grid, block, 0, ctx->stream, a);
     else if (mode == LOSS_MEAN)
-        FAE_LAUNCH(ctx, (loss_kernel<T, DP, LOSS_MEAN>), grid, block, 0, ctx->stream, a);
+        FAE_LAUNCH(ctx, (loss_kernel<HOW, DP, LOSS_MEAN, BIAS>), grid, block, 0, ctx->stream, a);
     else
-        FAE_LAUNCH(ctx, (loss_kernel<T, DP, LOSS_GRAD>), grid, block, 0, ctx->stream, a);
+        FAE_LAUNCH(ctx, (loss_kernel<HOW, DP, LOSS_GRAD, BIAS>), grid, block, 0, ctx->stream, a);
 }
-template <typename T> static void loss_launch(fae_ctx *ctx, int mode, const loss_args &a)
+template <int HOW, int DP> static void loss_launch_bias(fae_ctx *ctx, int mode, const loss_args &a)
+{
+    if (a.bias)
+        loss_launch_mode<HOW, DP, true>(ctx, mode, a);
+    else
+        loss_launch_mode<HOW, DP, false>(ctx, mode, a);
+}
+template <int HOW> static void loss_launch(fae_ctx *ctx, int mode, const loss_args &a)
 {
     switch (loss_padded(a.width)) {
-    case 32: return loss_launch_mode<T, 32>(ctx, mode, a);
-    case 64: return loss_launch_mode<T, 64>(ctx, mode, a);
-    case 96: return loss_launch_mode<T, 96>(ctx, mode, a);
-    case 128: return loss_launch_mode<T, 128>(ctx, mode, a);
-    case 192: return loss_launch_mode<T, 192>(ctx, mode, a);
-    default: return loss_launch_mode<T, 256>(ctx, mode, a);
+    case 32: return loss_launch_bias<HOW, 32>(ctx, mode, a);
+    case 64: return loss_launch_bias<HOW, 64>(ctx, mode, a);
+    case 96: return loss_launch_bias<HOW, 96>(ctx, mode, a);
+    case 128: return loss_launch_bias<HOW, 128>(ctx, mode, a);
+    case 192: return loss_launch_bias<HOW, 192>(ctx, mode, a);
+    default: return loss_launch_bias<HOW, 256>(ctx, mode, a);
     }
 }
 

@@ -3,8 +3,14 @@
 
 #include "fae_loss.h"
 
+#ifdef TRY_W
+#define LOSS_GROUPS (256 * TRY_W)
+#else
 #define LOSS_GROUPS 512 // workgroups that a launch should have: two for each compute unit
+#endif
 #define LOSS_MOST 0x7fff0000LL
+#define LOSS_WIDE_ROWS 128
+#define LOSS_HELD_MOST 256 // held rows of a workgroup at most
 
 // ---------------------------------------------------------------------------------
 // kernels
@@ -77,53 +83,106 @@ struct LossRows {
     const float *bias, *lse, *mean, *gloss;
     float *nlse, *g;
     int32_t *t;
-    uint32_t *g_most;
+    float *g_most, *x_most; // a value for every workgroup
     int32_t target_bits, n_classes, width;
     float scale;
     uint32_t *status;
 };
+
+#define LOSS_MOSTS 512 // workgroups that look for a largest value, and slots for what they find
+
+// the workgroup's largest value into its slot
+__device__ __forceinline__ void loss_most_of(float v, float *slot)
+{
+    __shared__ float part[4];
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1)
+        v = fmaxf(v, __shfl_xor(v, d, 64));
+    __syncthreads();
+    if (fae_lane() == 0)
+        part[threadIdx.x / 64] = v;
+    __syncthreads();
+    if (threadIdx.x == 0)
+        *slot = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+}
+// (of finite values)
+__device__ __forceinline__ float loss_most(float most, float v)
+{
+    v = fabsf(v);
+    return v < INFINITY ? fmaxf(most, v) : most;
+}
+
+// The largest value of all rows of fp32.  Bound by memory.
+__global__ __launch_bounds__(256) void loss_most_kernel(const float *w, int64_t stride, int64_t n, int32_t width, float *slots)
+{
+    float most = 0.f;
+    const uint32_t per = ((uint32_t)width + 3) / 4, lanes = per <= 1 ? 1 : 1u << (32 - __clz(per - 1)); // lanes of a row, 4 values each
+    const uint32_t rows = 256 / lanes;
+    fae_place<4> at;
+    at.set((threadIdx.x % lanes) * 4, width);
+    for (int64_t r = (int64_t)blockIdx.x * rows + threadIdx.x / lanes; r < n; r += (int64_t)gridDim.x * rows) {
+        const float *row = w + r * stride;
+        if (width >= 4) {
+            const auto v = *(const typename fae_vec<float, 4>::loose *)(row + at.from);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                most = loss_most(most, v[e]);
+        } else
+            for (int e = 0; e < width; ++e)
+                most = loss_most(most, row[e]);
+    }
+    loss_most_of(most, slots + blockIdx.x);
+}
 
 // A wave per row: gx from the mean of the other classes' rows and the target's own, whose share p - 1 is taken without the cancellation of a
 // confident row; and what the classes' gradient reads of every row.
 template <typename T> __global__ __launch_bounds__(256) void loss_rows_kernel(LossRows a)
 {
     const int lane = fae_lane();
-    const int64_t r = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
-    if (r >= a.n_rows)
-        return;
-    int32_t t = loss_target(a.targets, a.target_bits, r, a.n_classes, a.status);
-    const float lse = a.lse[r];
-    if (lse == -INFINITY) // no class is offered
-        t = -1;
-    const float g = t < 0 ? 0.f : a.gloss[r];
-    if (lane == 0) {
-        a.nlse[r] = t < 0 ? -INFINITY : lse * -1.44269504f;
-        a.g[r] = g;
-        a.t[r] = t;
-        if (a.g_most)
-            atomicMax(a.g_most, __float_as_uint(fabsf(g)));
-    }
-    if (!a.gx)
-        return;
-    const T *x = (const T *)a.x + r * a.x_stride, *w = (const T *)a.w + t * a.w_stride;
-    T *gx = (T *)a.gx + r * a.gx_stride;
-    float wv[4], dot = 0.f;
+    float g_most = 0.f, x_most = 0.f;
+    for (int64_t r = (int64_t)blockIdx.x * 4 + threadIdx.x / 64; r < a.n_rows; r += (int64_t)gridDim.x * 4) {
+        int32_t t = loss_target(a.targets, a.target_bits, r, a.n_classes, a.status);
+        const float lse = a.lse[r];
+        if (lse == -INFINITY) // no class is offered
+            t = -1;
+        const float g = t < 0 ? 0.f : a.gloss[r];
+        g_most = loss_most(g_most, g);
+        if (lane == 0) {
+            a.nlse[r] = t < 0 ? -INFINITY : __log2f(fabsf(g)) - lse * 1.44269504f;
+            a.g[r] = g;
+            a.t[r] = t;
+        }
+        if (!a.gx && !a.x_most)
+            continue;
+        const T *x = (const T *)a.x + r * a.x_stride, *w = (const T *)a.w + t * a.w_stride;
+        float wv[4], dot = 0.f;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int c = lane + j * 64;
-        wv[j] = t >= 0 && c < a.width ? (float)w[c] : 0.f;
-        dot += t >= 0 && c < a.width ? wv[j] * (float)x[c] : 0.f;
-    }
+        for (int j = 0; j < 4; ++j) {
+            const int c = lane + j * 64;
+            const bool in = t >= 0 && c < a.width;
+            const float xv = in ? (float)x[c] : 0.f;
+            wv[j] = in && a.gx ? (float)w[c] : 0.f;
+            x_most = loss_most(x_most, xv);
+            dot += wv[j] * xv;
+        }
+        if (!a.gx)
+            continue;
+        T *gx = (T *)a.gx + r * a.gx_stride;
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1)
-        dot += __shfl_xor(dot, d, 64);
-    const float share = t < 0 ? 0.f : expm1f(dot * a.scale + (a.bias ? a.bias[t] : 0.f) - lse);
+        for (int d = 32; d > 0; d >>= 1)
+            dot += __shfl_xor(dot, d, 64);
+        const float share = t < 0 ? 0.f : expm1f(dot * a.scale + (a.bias ? a.bias[t] : 0.f) - lse);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int c = lane + j * 64;
-        if (c < a.width)
-            gx[c] = (T)(t < 0 ? 0.f : a.scale * g * (a.mean[r * a.width + c] + share * wv[j]));
+        for (int j = 0; j < 4; ++j) {
+            const int c = lane + j * 64;
+            if (c < a.width)
+                gx[c] = (T)(t < 0 ? 0.f : a.scale * g * (a.mean[r * a.width + c] + share * wv[j]));
+        }
     }
+    if (a.g_most)
+        loss_most_of(g_most, a.g_most + blockIdx.x);
+    if (a.x_most)
+        loss_most_of(x_most, a.x_most + blockIdx.x);
 }
 
 struct LossClasses {
@@ -177,39 +236,51 @@ static bool loss_sizes_fit(const fae_softmax_loss *l)
            l->width <= FAE_LOSS_MAX_WIDTH && l->type >= FAE_F32 && l->type <= FAE_F16;
 }
 
-// n_own held rows in workgroups of LOSS_HELD, n_st streamed rows shared out among as many of them as fill the chip
+// fp32 as two fp16 numbers or three bf16: the first take a look at all streamed rows before, which a forward of few rows does not pay for
+static int loss_how(const fae_softmax_loss *l, int mode)
+{
+    return l->type == FAE_BF16 ? LOSS_BF16 : l->type == FAE_F16 ? LOSS_F16 : mode == LOSS_GRAD || l->n_rows >= LOSS_WIDE_ROWS ? LOSS_F32_WIDE : LOSS_F32;
+}
+
+// n_own held rows in workgroups of some, n_st streamed rows shared out among as many of them as fill the chip
 struct LossShape {
+    int how;
     int64_t blocks, tiles, splits;
     int32_t pitch;
-    int64_t part_rows; // rows of partial results that any n_own up to this one would need (a smaller one is shared out more)
 };
-static LossShape loss_shape(const fae_softmax_loss *l, int64_t n_own, int64_t n_st)
+static LossShape loss_shape(const fae_softmax_loss *l, int mode)
 {
     LossShape s;
-    const int tile = loss_tile(l->type, loss_padded(l->width));
-    s.blocks = (n_own + LOSS_HELD - 1) / LOSS_HELD;
+    const int64_t n_own = mode == LOSS_GRAD ? l->n_classes : l->n_rows, n_st = mode == LOSS_GRAD ? l->n_rows : l->n_classes;
+    s.how = loss_how(l, mode);
+    const int dp = loss_padded(l->width), tile = loss_tile(s.how, dp), held = loss_held(s.how, dp, mode);
+    s.blocks = (n_own + held - 1) / held;
     s.tiles = (n_st + tile - 1) / tile;
     s.splits = s.blocks ? LOSS_GROUPS / s.blocks : 1;
     s.splits = s.splits > s.tiles ? s.tiles : s.splits;
     s.splits = s.splits < 1 ? 1 : (s.splits > 8 ? s.splits / 8 * 8 : s.splits);
     s.pitch = (l->width + 3) / 4 * 4;
-    const int64_t most = (int64_t)LOSS_GROUPS * LOSS_HELD;
-    s.part_rows = n_own > most / (s.tiles ? s.tiles : 1) ? most : n_own * s.tiles;
-    s.part_rows = s.part_rows > n_own ? s.part_rows : n_own;
     return s;
 }
 
-// what the forward takes: per part and row reference and sum, per row the target's score, and the parts' means
+// rows of partial results that any call up to this size would need: in a launch that is shared out, a workgroup's held rows for each workgroup
+static int64_t loss_part_rows(const fae_softmax_loss *l, int mode)
+{
+    const int64_t n_own = mode == LOSS_GRAD ? l->n_classes : l->n_rows, n_st = mode == LOSS_GRAD ? l->n_rows : l->n_classes;
+    const int64_t most = (int64_t)LOSS_GROUPS * LOSS_HELD_MOST, tiles = (n_st + 31) / 32;
+    const int64_t shared = tiles == 0 ? 0 : n_own > most / tiles ? most : n_own * tiles;
+    return mode == LOSS_GRAD || shared > n_own ? shared : n_own; // (the gradient in one part needs none)
+}
+// what the forward takes: the largest values, per part and row reference and sum, per row the target's score, and the parts' means
 static size_t loss_fwd_bytes(const fae_softmax_loss *l)
 {
-    const LossShape s = loss_shape(l, l->n_rows, l->n_classes);
-    return fae_align_up(s.part_rows * 8, 256) + fae_align_up(l->n_rows * 4, 256) + fae_align_up(s.part_rows * s.pitch * 4, 256);
+    const int64_t rows = loss_part_rows(l, LOSS_MEAN), pitch = (l->width + 3) / 4 * 4;
+    return fae_align_up(LOSS_MOSTS * 4, 256) + fae_align_up(rows * 8, 256) + fae_align_up(l->n_rows * 4, 256) + fae_align_up(rows * pitch * 4, 256);
 }
 static size_t loss_grad_bytes(const fae_softmax_loss *l)
 {
-    const LossShape s = loss_shape(l, l->n_classes, l->n_rows);
-    const int64_t rows = s.part_rows < (int64_t)LOSS_GROUPS * LOSS_HELD ? s.part_rows : (int64_t)LOSS_GROUPS * LOSS_HELD; // none in one part
-    return fae_align_up(rows * 4, 256) + fae_align_up(rows * s.pitch * 4, 256);
+    const int64_t rows = loss_part_rows(l, LOSS_GRAD), pitch = (l->width + 3) / 4 * 4;
+    return fae_align_up(rows * 4, 256) + fae_align_up(rows * pitch * 4, 256);
 }
 
 extern "C" size_t fae_softmax_loss_fwd_workspace_bytes(const fae_softmax_loss *what)
@@ -222,7 +293,7 @@ extern "C" size_t fae_softmax_loss_bwd_workspace_bytes(const fae_softmax_loss *w
     if (!loss_sizes_fit(what))
         return 0;
     const size_t f = loss_fwd_bytes(what), g = loss_grad_bytes(what);
-    return 512 + 3 * fae_align_up(what->n_rows * 4, 256) + fae_align_up(what->n_rows * what->width * 4, 256) + (f > g ? f : g);
+    return 512 + 2 * fae_align_up(LOSS_MOSTS * 4, 256) + 3 * fae_align_up(what->n_rows * 4, 256) + fae_align_up(what->n_rows * what->width * 4, 256) + (f > g ? f : g);
 }
 
 // bytes that rows take up
@@ -295,14 +366,16 @@ static int32_t loss_check_ws(fae_ctx *ctx, const char *who, const void *ws, size
     return FAE_OK;
 }
 
-static void loss_run(fae_ctx *ctx, int32_t type, int mode, const loss_args &a)
+static void loss_run(fae_ctx *ctx, int how, int mode, const loss_args &a)
 {
-    if (type == FAE_F32)
+    if (how == LOSS_F32)
         loss_launch_f32(ctx, mode, a);
-    else if (type == FAE_BF16)
+    else if (how == LOSS_BF16)
         loss_launch_bf16(ctx, mode, a);
-    else
+    else if (how == LOSS_F16)
         loss_launch_f16(ctx, mode, a);
+    else
+        loss_launch_f32_wide(ctx, mode, a);
 }
 
 static void loss_common(fae_ctx *ctx, const fae_softmax_loss *l, const LossShape &s, loss_args *a)
@@ -326,7 +399,7 @@ static void loss_common(fae_ctx *ctx, const fae_softmax_loss *l, const LossShape
 static int32_t loss_forward(fae_ctx *ctx, const fae_softmax_loss *l, const void *x, int64_t x_stride, const void *w, int64_t w_stride, float *loss,
                             float *lse, float *mean, void *ws, size_t ws_bytes)
 {
-    const LossShape s = loss_shape(l, l->n_rows, l->n_classes);
+    const LossShape s = loss_shape(l, mean ? LOSS_MEAN : LOSS_STATS);
     fae_carver cv(ws, ws_bytes);
     loss_args a;
     loss_common(ctx, l, s, &a);
@@ -336,14 +409,23 @@ static int32_t loss_forward(fae_ctx *ctx, const fae_softmax_loss *l, const void 
     a.own_stride = x_stride;
     a.n_st = (int32_t)l->n_classes;
     a.n_own = (int32_t)l->n_rows;
+    float *most = cv.take<float>(LOSS_MOSTS);
     a.stat = cv.take<float>(s.splits * l->n_rows * 2);
     a.zt = cv.take<float>(l->n_rows);
     a.part = mean ? cv.take<float>(s.splits * l->n_rows * s.pitch) : nullptr;
     if (!cv.ok)
         return fae_fail(ctx, FAE_ENOSPC, "softmax loss: workspace too small");
+    if (s.how == LOSS_F32_WIDE) {
+        fae_ktimer kt(ctx, FAE_K_LOSS_JOIN);
+        const int64_t groups = (l->n_classes + 63) / 64;
+        a.st_most = most;
+        a.n_most = (int32_t)(groups < LOSS_MOSTS ? groups : LOSS_MOSTS);
+        FAE_LAUNCH(ctx, loss_most_kernel, dim3(a.n_most), dim3(256), 0, ctx->stream, (const float *)w, w_stride, l->n_classes, l->width, most);
+        FAE_LAUNCH_CHECK(ctx);
+    }
     {
         fae_ktimer kt(ctx, FAE_K_LOSS);
-        loss_run(ctx, l->type, mean ? LOSS_MEAN : LOSS_STATS, a);
+        loss_run(ctx, s.how, mean ? LOSS_MEAN : LOSS_STATS, a);
         FAE_LAUNCH_CHECK(ctx);
     }
     LossJoin j;
@@ -428,7 +510,7 @@ extern "C" int32_t fae_softmax_loss_bwd(fae_ctx *ctx, const fae_softmax_loss *wh
         return rc;
     FAE_HIP(ctx, hipSetDevice(ctx->device));
     fae_carver cv(ws, ws_bytes);
-    uint32_t *g_most = cv.take<uint32_t>(1);
+    float *g_most = cv.take<float>(LOSS_MOSTS), *x_most = cv.take<float>(LOSS_MOSTS);
     LossRows r;
     memset(&r, 0, sizeof(r));
     r.nlse = cv.take<float>(n);
@@ -439,11 +521,8 @@ extern "C" int32_t fae_softmax_loss_bwd(fae_ctx *ctx, const fae_softmax_loss *wh
         return fae_fail(ctx, FAE_ENOSPC, "%s: workspace too small", who);
     void *rest = cv.base + cv.used;
     const size_t rest_bytes = cv.cap - cv.used;
-    if (what->type == FAE_F16) {
-        rc = fae_fill_u32(ctx, g_most, 1, 0);
-        if (rc != FAE_OK)
-            return rc;
-    }
+    const int64_t row_groups = (n + 3) / 4;
+    const int32_t n_most = (int32_t)(row_groups < LOSS_MOSTS ? row_groups : LOSS_MOSTS);
     if (n > 0) {
         if (gx && !mean) {
             rc = loss_forward(ctx, what, x, x_row_stride, w, w_row_stride, nullptr, nullptr, own_mean, rest, rest_bytes);
@@ -463,14 +542,16 @@ extern "C" int32_t fae_softmax_loss_bwd(fae_ctx *ctx, const fae_softmax_loss *wh
         r.lse = lse;
         r.mean = mean;
         r.gloss = gloss;
-        r.g_most = what->type == FAE_F16 ? g_most : nullptr;
+        const bool grads = gw || gbias;
+        r.g_most = grads && what->type != FAE_BF16 ? g_most : nullptr;
+        r.x_most = grads && what->type == FAE_F32 ? x_most : nullptr;
         r.target_bits = what->target_bits;
         r.n_classes = (int32_t)v;
         r.width = (int32_t)d;
         r.scale = what->scale;
         r.status = ctx->d_block;
         fae_ktimer kt(ctx, FAE_K_LOSS_JOIN);
-        const dim3 grid((uint32_t)((n + 3) / 4)), block(256);
+        const dim3 grid(n_most), block(256);
         if (what->type == FAE_F32)
             FAE_LAUNCH(ctx, loss_rows_kernel<float>, grid, block, 0, ctx->stream, r);
         else if (what->type == FAE_BF16)
@@ -481,7 +562,7 @@ extern "C" int32_t fae_softmax_loss_bwd(fae_ctx *ctx, const fae_softmax_loss *wh
     }
     if (!gw && !gbias)
         return FAE_OK;
-    const LossShape s = loss_shape(what, v, n);
+    const LossShape s = loss_shape(what, LOSS_GRAD);
     loss_args a;
     loss_common(ctx, what, s, &a);
     a.st = x;
@@ -494,6 +575,8 @@ extern "C" int32_t fae_softmax_loss_bwd(fae_ctx *ctx, const fae_softmax_loss *wh
     a.g = r.g;
     a.t = r.t;
     a.g_most = g_most;
+    a.st_most = x_most;
+    a.n_most = n_most;
     if (s.splits > 1) {
         fae_carver more(rest, rest_bytes);
         a.psum = gbias ? more.take<float>(s.splits * v) : nullptr;
@@ -507,7 +590,7 @@ extern "C" int32_t fae_softmax_loss_bwd(fae_ctx *ctx, const fae_softmax_loss *wh
     }
     {
         fae_ktimer kt(ctx, FAE_K_LOSS_BWD);
-        loss_run(ctx, what->type, LOSS_GRAD, a);
+        loss_run(ctx, s.how, LOSS_GRAD, a);
         FAE_LAUNCH_CHECK(ctx);
     }
     if (s.splits > 1) {

@@ -2,4 +2,4 @@
 #define LOSS_KERNELS
 #include "fae_loss.h"
 
-void loss_launch_f16(fae_ctx *ctx, int mode, const loss_args &a) { loss_launch<fae_f16>(ctx, mode, a); }
+void loss_launch_f16(fae_ctx *ctx, int mode, const loss_args &a) { loss_launch<LOSS_F16>(ctx, mode, a); }

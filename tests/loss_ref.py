@@ -1,16 +1,18 @@
 """Softmax cross entropy over a table's rows from its definition in 64 bits, with a bound for what the kernels' arithmetic may add.
 
-Bounds (u = 2^-24; h = half a step of the type, finfo.eps / 2; N = 1 product per pair of 16-bit values, 6 per pair of fp32 values, which are
-three bf16 numbers each).  A matrix instruction adds 16 products to a sum with at most 16 roundings, so a product of `width` values
-errs by at most u (N width + 8) A with A = sum |x w| (the 8: what the six products leave out, 2^-23 A, and the factor), a score by
-  dz = u (|scale| (N width + 8) A + 4 |z| + 2 |bias|),
+Bounds (u = 2^-24; h = half a step of the type, finfo.eps / 2; N products per pair of values: 1 of 16 bits, up to 6 of fp32, whose values
+are three bf16 numbers or, after a power of two that brings the largest of all to 2^14 .. 2^15, two fp16 numbers).  Of fp32's
+products at most 2^-22 for each operand and 2^-22 for what is not multiplied is left out, 12 u, and of values 2^-18 below
+the largest half a step of fp16, 2^-25 where the largest is 2^14: m = 2^-38 of it.  A matrix instruction adds 16 products
+to a sum with at most 16 roundings, so a product of `width` values errs by at most u (N width + 16) A + m's with A = sum |x w|, a score by
+  dz = u (|scale| (N width + 16) A + 4 |z| + 2 |bias|) + |scale| (m_w sum |x| + m_x sum |w|),
 lse by the probabilities' mean of dz, by its sum over the classes (two additions per 32 classes and lane, 64 to join lanes and parts), by
 two units of 2^z and by the rounding of z - reference, which is below |z - lse| + 1:
   dlse = sum p dz + u (V / 16 + 64 + sum p (8 + 2 |z - lse|) + 4 |lse|).
 A probability's relative error is e = dz + dlse + u (8 + 2 |z - lse|) (as a factor, exp(e) - 1).  Entering a product it is
-rounded to the type, by h of itself (fp32: by 2^-24, as three bf16 numbers); sums of M such terms take at most N M + 64 roundings of the
-sum of their absolute values.  A 16-bit result is off by half a step more.  fp16 probabilities have a smallest step: they
-are multiplied by 2^12 at least 1 / 2 of the largest, so each is off by 2^-36 of that at most.  Of the other types, 2^z and the parts of a
+rounded to the type, by h of itself (fp32: 16 u as above); sums of M such terms take at most N M + 64 roundings of the
+sum of their absolute values.  A 16-bit result is off by half a step more.  fp16 probabilities have a smallest step: the
+largest is at least 2^9, and half a step is 2^-25: each is off by 2^-34 of the largest at most.  Of bf16 numbers, 2^z and the parts of a
 probability below fp32's smallest normal number, 2^-126, are lost: each is off by 2^-125 at most.
 
 Beside this worst case, fp32 results are held to what independent roundings add up to: one of at most 2 units per
@@ -33,8 +35,8 @@ class LossRef:
     def __init__(self, x, w, targets, bias=None, scale=1.0):
         self.dtype = x.dtype
         self.N = 6 if x.dtype == torch.float32 else 1
-        self.h = U if x.dtype == torch.float32 else torch.finfo(x.dtype).eps / 2
-        self.tiny = 2.0 ** -36 if x.dtype == torch.float16 else 2.0 ** -125
+        self.h = 16 * U if x.dtype == torch.float32 else torch.finfo(x.dtype).eps / 2
+        self.tiny = 2.0 ** -125 if x.dtype == torch.bfloat16 else 2.0 ** -34
         self.x, self.w = x.double(), w.double()
         self.scale = float(np.float32(scale))
         self.n, self.v, self.d = x.shape[0], w.shape[0], x.shape[1]
@@ -44,10 +46,14 @@ class LossRef:
         z = self.scale * (self.x @ self.w.t().contiguous())
         A = self.x.abs() @ self.w.abs().t().contiguous()
         b = torch.zeros(self.v, dtype=F, device=x.device) if bias is None else bias.double()
+        wide = x.dtype == torch.float32
+        self.mx = 2.0 ** -38 * float(torch.nan_to_num(self.x, posinf=0, neginf=0).abs().max()) if wide and self.n else 0.0
+        self.mw = 2.0 ** -38 * float(torch.nan_to_num(self.w, posinf=0, neginf=0).abs().max()) if wide else 0.0
+        off = self.mw * self.x.abs().sum(1)[:, None] + self.mx * self.w.abs().sum(1)
         self.bias = bias
         self.z = z + b
         fine = torch.isfinite(self.z)
-        self.dz = torch.where(fine, U * (abs(self.scale) * (self.N * self.d + 8) * A + 4 * z.abs() + 2 * torch.nan_to_num(b, neginf=0).abs()), torch.zeros((), dtype=F, device=x.device))
+        self.dz = torch.where(fine, U * (abs(self.scale) * (self.N * self.d + 16) * A + 4 * z.abs() + 2 * torch.nan_to_num(b, neginf=0).abs()) + abs(self.scale) * off, torch.zeros((), dtype=F, device=x.device))
         self.empty = ~fine.any(1) if self.n else self.known
         self.lse = torch.logsumexp(self.z, 1)
         off = torch.where(fine, self.z - self.lse[:, None], torch.full((), -float("inf"), dtype=F, device=x.device))
@@ -70,7 +76,7 @@ class LossRef:
     def mean(self):
         others = self.p * (1 - self.hot * self.known[:, None])
         ref = others @ self.w
-        err = (others * (self.e + self.h)) @ self.w.abs() + U * (self.N * self.v + 64) * (others @ self.w.abs()) + self.tiny * self.w.abs().sum(0)
+        err = (others * (self.e + self.h)) @ self.w.abs() + U * (self.N * self.v + 64) * (others @ self.w.abs()) + self.tiny * self.w.abs().sum(0) + self.mw
         return ref, err
 
     def backward(self, gloss, out_dtype=None):
@@ -85,13 +91,13 @@ class LossRef:
         dq = p * e + U * self.hot * 8 + q.abs() * (self.h + 4 * U)  # of p - (v == target), as it enters a product
         gx = self.scale * (G @ self.w)
         tx = s * (G.abs() @ self.w.abs())
-        dx = s * ((g.abs() * dq) @ self.w.abs()) + U * (self.N * self.v + 80) * tx + s * g.abs() * self.tiny * self.w.abs().sum(0)
+        dx = s * ((g.abs() * dq) @ self.w.abs()) + U * (self.N * self.v + 80) * tx + s * g.abs() * (self.tiny * self.w.abs().sum(0) + 2 * self.mw)
         gw = self.scale * (G.t().contiguous() @ x)
         tw = s * (G.abs().t().contiguous() @ x.abs())
         both = g.abs() * (p + self.hot)
         rx, rw = s * (both @ self.w.abs()), s * (both.t().contiguous() @ x.abs())
         most = g.abs().max() if self.n else 0.0
-        dw = s * ((g.abs() * dq).t().contiguous() @ x.abs()) + U * (self.N * self.n + 80) * tw + s * most * self.tiny * x.abs().sum(0)
+        dw = s * ((g.abs() * dq).t().contiguous() @ x.abs()) + U * (self.N * self.n + 80) * tw + s * (most * self.tiny * x.abs().sum(0) + self.mx * G.abs().sum(0)[:, None])
         gb = G.sum(0)
         db = (g.abs() * dq).sum(0) + U * (self.n + 80) * G.abs().sum(0) + most * self.tiny * self.n
         if out_dtype != torch.float32:
