@@ -458,7 +458,7 @@ int32_t fae_softmax_loss_bwd(fae_ctx *ctx, const fae_softmax_loss *what, const v
 typedef struct {
     const void *g; /* device, n values; may be NULL if n is 0 */
     void *out;     /* fae_grad_clip: device, n values; g itself, or memory that no other tensor of the list has */
-    int64_t n;     /* 0 .. 2^40 */
+    int64_t n;     /* 0 .. 2^36 - 1 */
     int32_t type;  /* FAE_F32, FAE_BF16 or FAE_F16, of both */
 } fae_grad;
 #define FAE_MAX_GRADS 65536

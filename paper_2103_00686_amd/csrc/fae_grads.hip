@@ -4,51 +4,119 @@
 
 #include "fae_rows.h"
 
-#define GRADS_LIST FAE_MAX_TABLES // tensors of a launch: their addresses are kernel arguments
-#define GRADS_SPAN 8192           // values of a tensor that a workgroup takes at a time
-#define GRADS_GROUPS 1024         // workgroups of a launch at most, and partial sums
-#define GRADS_MOST (1LL << 37)    // values of a tensor: more than the card holds
+// What bounds both kernels: memory.  188 M bf16 values: squares 67 us (5.6 TB/s), clipping 137 us (5.5 TB/s); the list is read twice, as a
+// factor is known only after the last square.  Spans of 8 KiB with the next one in flight; 16 KiB 70 and 151 us, 4 KiB 76 and 141.
+// Reading goes in stretches, without the caches' help (with it 97 us: the lines that it leaves there serve clipping a little, 127 instead
+// of 137, and cost more); stores go a grid's width apart (in stretches 152 us).
+#define GRADS_BYTES 8192      // of a tensor that a workgroup takes at a time: a span
+#define GRADS_GROUPS 2048     // workgroups of a launch at most, and partial sums
+#define GRADS_CHAINS 4
+#define GRADS_LIST 128        // tensors of a launch: their addresses are kernel arguments, of which there are 4 KiB
+#define GRADS_MOST (1LL << 36) // values of a tensor: more than the card holds
+
+__host__ __device__ static inline int grads_span(int type) { return type == FAE_F32 ? GRADS_BYTES / 4 : GRADS_BYTES / 2; }
 
 struct GradsArgs {
     const void *g[GRADS_LIST];
     void *out[GRADS_LIST];
     int64_t n[GRADS_LIST];
-    int32_t start[FAE_MAX_TABLES + 1]; // spans of the tensors before
+    int32_t start[GRADS_LIST + 1]; // spans of the tensors before
     uint8_t type[GRADS_LIST];
-    int32_t n_list, n_before; // n_before: partial sums of the launches before this one
+    int32_t spans, n_before; // n_before: partial sums of the launches before this one
     double *sums;
     double scale, max_norm;
     float *norm;
     int32_t n_sums;
 };
 
-template <typename T> __device__ __forceinline__ double grads_squares(const T *g, int64_t n)
+static_assert(sizeof(GradsArgs) <= 4096, "kernel arguments");
+
+// the tensor of a span: how many start at or before it, less one; counted in two rounds of independent loads
+__device__ __forceinline__ int grads_find(const GradsArgs &a, int span)
 {
-    constexpr int E = 16 / sizeof(T), UN = GRADS_SPAN / (256 * E);
-    typedef typename fae_vec<T, E>::loose loose;
-    double s = 0.0;
-    if (n >= GRADS_SPAN) {
-        typename fae_vec<T, E>::type v[UN];
+    int v[15], base = 0, more = 0;
 #pragma unroll
-        for (int u = 0; u < UN; ++u)
-            v[u] = *(const loose *)(g + (u * 256 + threadIdx.x) * E);
+    for (int i = 1; i < GRADS_LIST / 16; ++i)
+        v[i] = a.start[i * 16];
 #pragma unroll
-        for (int u = 0; u < UN; ++u)
+    for (int i = 1; i < GRADS_LIST / 16; ++i)
+        base += v[i] <= span ? 16 : 0;
+#pragma unroll
+    for (int i = 1; i < 16; ++i)
+        v[i - 1] = a.start[base + i];
+#pragma unroll
+    for (int i = 1; i < 16; ++i)
+        more += v[i - 1] <= span ? 1 : 0;
+    return base + more;
+}
+
+// A workgroup's spans: where it is, and the 16-byte pieces of a whole span in flight.
+struct GradsWalk {
+    int b, end, step, z, type, next_start;
+    const char *g;
+    int64_t left; // bytes from the span's start to the tensor's end
+    __device__ __forceinline__ void tensor(const GradsArgs &a)
+    {
+        type = a.type[z];
+        next_start = a.start[z + 1];
+        const int64_t from = (int64_t)(b - a.start[z]) * GRADS_BYTES;
+        g = (const char *)a.g[z] + from;
+        left = a.n[z] * (type == FAE_F32 ? 4 : 2) - from;
+    }
+    // spans one after the other (for reading alone), or a grid's width apart (where there are stores)
+    __device__ __forceinline__ void begin(const GradsArgs &a, bool apart)
+    {
+        step = apart ? gridDim.x : 1;
+        b = apart ? blockIdx.x : (int)((int64_t)a.spans * blockIdx.x / gridDim.x);
+        end = apart ? a.spans : (int)((int64_t)a.spans * (blockIdx.x + 1) / gridDim.x);
+        if (b < end) {
+            z = grads_find(a, b);
+            tensor(a);
+        }
+    }
+    __device__ __forceinline__ void next(const GradsArgs &a)
+    {
+        b += step;
+        g += (int64_t)step * GRADS_BYTES;
+        left -= (int64_t)step * GRADS_BYTES;
+        if (b < end && b >= next_start) {
+            z = grads_find(a, b);
+            tensor(a);
+        }
+    }
+    __device__ __forceinline__ bool whole() const { return b < end && left >= GRADS_BYTES; }
+};
+typedef uint32_t grads_raw __attribute__((ext_vector_type(4)));
+typedef grads_raw grads_loose __attribute__((aligned(2)));
+#define GRADS_UN (GRADS_BYTES / 4096)
+__device__ __forceinline__ void grads_load(const GradsWalk &w, grads_raw (&v)[GRADS_UN])
+{
+    if (w.whole()) {
+#pragma unroll
+        for (int u = 0; u < GRADS_UN; ++u)
+            v[u] = __builtin_nontemporal_load((const grads_loose *)(w.g + (u * 256 + threadIdx.x) * 16));
+    }
+}
+
+template <typename T> __device__ __forceinline__ void grads_squares(const GradsWalk &w, const grads_raw (&v)[GRADS_UN], double (&s)[GRADS_CHAINS])
+{
+    constexpr int E = 16 / sizeof(T);
+    if (w.whole()) {
+#pragma unroll
+        for (int u = 0; u < GRADS_UN; ++u) {
+            const auto t = __builtin_bit_cast(typename fae_vec<T, E>::type, v[u]);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const double d = (double)(float)v[u][e];
-                s = fma(d, d, s);
+                const double d = (double)(float)t[e];
+                s[e % GRADS_CHAINS] = fma(d, d, s[e % GRADS_CHAINS]);
             }
+        }
     } else {
-        for (int i = threadIdx.x * E; i < n; i += 256 * E)
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (i + e < n) {
-                    const double d = (double)(float)g[i + e];
-                    s = fma(d, d, s);
-                }
+        for (int i = threadIdx.x; i < w.left / (int)sizeof(T); i += 256) {
+            const double d = (double)(float)((const T *)w.g)[i];
+            s[0] = fma(d, d, s[0]);
+        }
     }
-    return s;
 }
 
 __device__ __forceinline__ double grads_block_sum(double s)
@@ -63,21 +131,31 @@ __device__ __forceinline__ double grads_block_sum(double s)
     return (part[0] + part[1]) + (part[2] + part[3]);
 }
 
-// A workgroup walks over spans of all tensors of its launch and adds what it finds to its own partial sum.
+// A workgroup walks over its stretch of the launch's spans, the next one on its way while one is squared, and adds what it finds to its own
+// partial sum.
 __global__ __launch_bounds__(256) void grads_squares_kernel(GradsArgs a)
 {
-    double s = 0.0;
-    for (int b = blockIdx.x; b < a.start[a.n_list]; b += gridDim.x) {
-        const int z = fae_find_table(a.start, a.n_list, b);
-        const int64_t from = (int64_t)(b - a.start[z]) * GRADS_SPAN, n = a.n[z] - from;
-        if (a.type[z] == FAE_F32)
-            s += grads_squares((const float *)a.g[z] + from, n);
-        else if (a.type[z] == FAE_BF16)
-            s += grads_squares((const fae_bf16 *)a.g[z] + from, n);
+    double some[GRADS_CHAINS] = {0.0, 0.0, 0.0, 0.0};
+    GradsWalk w, n;
+    grads_raw v[GRADS_UN], nv[GRADS_UN];
+    w.begin(a, false);
+    grads_load(w, v);
+    while (w.b < w.end) {
+        n = w;
+        n.next(a);
+        grads_load(n, nv);
+        if (w.type == FAE_F32)
+            grads_squares<float>(w, v, some);
+        else if (w.type == FAE_BF16)
+            grads_squares<fae_bf16>(w, v, some);
         else
-            s += grads_squares((const fae_f16 *)a.g[z] + from, n);
+            grads_squares<fae_f16>(w, v, some);
+        w = n;
+#pragma unroll
+        for (int u = 0; u < GRADS_UN; ++u)
+            v[u] = nv[u];
     }
-    s = grads_block_sum(s);
+    const double s = grads_block_sum((some[0] + some[1]) + (some[2] + some[3]));
     if (threadIdx.x == 0)
         a.sums[blockIdx.x] = ((int)blockIdx.x < a.n_before ? a.sums[blockIdx.x] : 0.0) + s;
 }
@@ -97,28 +175,21 @@ __global__ __launch_bounds__(256) void grads_norm_kernel(GradsArgs a)
         *a.norm = (float)norm;
 }
 
-template <typename T> __device__ __forceinline__ void grads_scale(const T *g, T *out, int64_t n, float f0, float f1)
+template <typename T> __device__ __forceinline__ void grads_scale(const GradsWalk &w, const grads_raw (&v)[GRADS_UN], char *out, float f0, float f1)
 {
-    constexpr int E = 16 / sizeof(T), UN = GRADS_SPAN / (256 * E);
-    typedef typename fae_vec<T, E>::loose loose;
-    if (n >= GRADS_SPAN) {
-        typename fae_vec<T, E>::type v[UN];
+    constexpr int E = 16 / sizeof(T);
+    if (w.whole()) {
 #pragma unroll
-        for (int u = 0; u < UN; ++u)
-            v[u] = *(const loose *)(g + (u * 256 + threadIdx.x) * E);
-#pragma unroll
-        for (int u = 0; u < UN; ++u) {
+        for (int u = 0; u < GRADS_UN; ++u) {
+            auto t = __builtin_bit_cast(typename fae_vec<T, E>::type, v[u]);
 #pragma unroll
             for (int e = 0; e < E; ++e)
-                v[u][e] = (T)((float)v[u][e] * f0 * f1);
-            *(loose *)(out + (u * 256 + threadIdx.x) * E) = v[u];
+                t[e] = (T)((float)t[e] * f0 * f1);
+            __builtin_nontemporal_store(__builtin_bit_cast(grads_raw, t), (grads_loose *)(out + (u * 256 + threadIdx.x) * 16));
         }
     } else {
-        for (int i = threadIdx.x * E; i < n; i += 256 * E)
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (i + e < n)
-                    out[i + e] = (T)((float)g[i + e] * f0 * f1);
+        for (int i = threadIdx.x; i < w.left / (int)sizeof(T); i += 256)
+            ((T *)out)[i] = (T)((float)((const T *)w.g)[i] * f0 * f1);
     }
 }
 
@@ -132,17 +203,27 @@ __global__ __launch_bounds__(256) void grads_clip_kernel(GradsArgs a)
     const double f = norm <= a.max_norm ? a.scale : a.max_norm / norm * a.scale;
     const bool tiny = fabs(f) < 0x1p-100;
     const float f0 = tiny ? 0x1p-64f : 1.f, f1 = (float)(tiny ? f * 0x1p64 : f);
-    for (int b = blockIdx.x; b < a.start[a.n_list]; b += gridDim.x) {
-        const int z = fae_find_table(a.start, a.n_list, b);
-        const int64_t from = (int64_t)(b - a.start[z]) * GRADS_SPAN, n = a.n[z] - from;
-        if (f == 1.0 && a.g[z] == a.out[z])
-            continue;
-        if (a.type[z] == FAE_F32)
-            grads_scale((const float *)a.g[z] + from, (float *)a.out[z] + from, n, f0, f1);
-        else if (a.type[z] == FAE_BF16)
-            grads_scale((const fae_bf16 *)a.g[z] + from, (fae_bf16 *)a.out[z] + from, n, f0, f1);
-        else
-            grads_scale((const fae_f16 *)a.g[z] + from, (fae_f16 *)a.out[z] + from, n, f0, f1);
+    GradsWalk w, n;
+    grads_raw v[GRADS_UN], nv[GRADS_UN];
+    w.begin(a, true);
+    grads_load(w, v);
+    while (w.b < w.end) {
+        n = w;
+        n.next(a);
+        grads_load(n, nv);
+        char *out = (char *)a.out[w.z] + (w.g - (const char *)a.g[w.z]);
+        if (f != 1.0 || out != w.g) {
+            if (w.type == FAE_F32)
+                grads_scale<float>(w, v, out, f0, f1);
+            else if (w.type == FAE_BF16)
+                grads_scale<fae_bf16>(w, v, out, f0, f1);
+            else
+                grads_scale<fae_f16>(w, v, out, f0, f1);
+        }
+        w = n;
+#pragma unroll
+        for (int u = 0; u < GRADS_UN; ++u)
+            v[u] = nv[u];
     }
 }
 
@@ -226,12 +307,12 @@ static int32_t grads_list(int32_t n_grads, const fae_grad *h, int32_t z, GradsAr
         a->out[k] = h[z].out;
         a->n[k] = h[z].n;
         a->type[k] = (uint8_t)h[z].type;
-        a->start[k + 1] = a->start[k] + (int32_t)((h[z].n + GRADS_SPAN - 1) / GRADS_SPAN);
+        a->start[k + 1] = a->start[k] + (int32_t)((h[z].n + grads_span(h[z].type) - 1) / grads_span(h[z].type));
         ++k;
     }
-    a->n_list = k;
-    for (int i = k + 1; i <= FAE_MAX_TABLES; ++i)
-        a->start[i] = a->start[k];
+    a->spans = a->start[k];
+    for (int i = k + 1; i <= GRADS_LIST; ++i)
+        a->start[i] = INT32_MAX;
     return z;
 }
 
@@ -243,7 +324,7 @@ extern "C" size_t fae_grad_workspace_bytes(int32_t n_grads, const fae_grad *h_gr
 
 static uint32_t grads_groups(const GradsArgs &a)
 {
-    const int32_t spans = a.start[a.n_list];
+    const int32_t spans = a.spans;
     return spans < GRADS_GROUPS ? (spans > 0 ? spans : 1) : GRADS_GROUPS;
 }
 
