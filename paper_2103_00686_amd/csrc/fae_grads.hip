@@ -303,11 +303,14 @@ static int32_t grads_list(int32_t n_grads, const fae_grad *h, int32_t z, GradsAr
     for (; z < n_grads && k < GRADS_LIST; ++z) {
         if (h[z].n == 0)
             continue;
+        const int64_t spans = (h[z].n + grads_span(h[z].type) - 1) / grads_span(h[z].type);
+        if (a->start[k] + spans >= 1LL << 30)
+            break;
         a->g[k] = h[z].g;
         a->out[k] = h[z].out;
         a->n[k] = h[z].n;
         a->type[k] = (uint8_t)h[z].type;
-        a->start[k + 1] = a->start[k] + (int32_t)((h[z].n + grads_span(h[z].type) - 1) / grads_span(h[z].type));
+        a->start[k + 1] = a->start[k] + (int32_t)spans;
         ++k;
     }
     a->spans = a->start[k];

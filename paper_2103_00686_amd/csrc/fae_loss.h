@@ -9,7 +9,8 @@
 //   LOSS_MEAN   the same, and O = the sum of 2^(Z - reference) w of all classes but the target
 //   LOSS_GRAD   held: w, streamed: x; P = gloss (2^(Z - lse) - (class is the target)), O = the sum of P x, and the sum of P (bias)
 // Z is in units of log 2 throughout.
-enum { LOSS_STATS, LOSS_MEAN, LOSS_GRAD };
+//   LOSS_FEW    what LOSS_STATS finds, for few rows
+enum { LOSS_STATS, LOSS_MEAN, LOSS_GRAD, LOSS_FEW };
 
 struct loss_args {
     const void *st, *own; // streamed rows, held rows
@@ -42,27 +43,28 @@ struct loss_args {
 enum { LOSS_F32, LOSS_BF16, LOSS_F16, LOSS_F32_WIDE };
 constexpr int loss_planes_of(int how) { return how == LOSS_F32 ? 3 : how == LOSS_F32_WIDE ? 2 : 1; }
 static inline int loss_padded(int32_t width) { return width <= 32 ? 32 : width <= 64 ? 64 : width <= 96 ? 96 : width <= 128 ? 128 : width <= 192 ? 192 : 256; }
-constexpr int loss_tile(int how, int dp) { return how == LOSS_F32 && dp > 128 ? 32 : 64; }
+constexpr int loss_tile(int how, int dp) { return dp > 128 && loss_planes_of(how) > 1 ? 32 : 64; }
 // held rows of a wave, in blocks of 32: two where their registers leave room for two waves on a SIMD
-#ifdef TRY_NB
-constexpr int loss_blocks(int how, int dp, int mode) { return TRY_NB; }
-#else
+// held rows of a wave, in blocks of 32: two where their registers leave room for two waves on a SIMD
 constexpr int loss_blocks(int how, int dp, int mode)
 {
     return loss_planes_of(how) > 1 ? (dp <= 32 ? 2 : 1) : (dp <= (mode == LOSS_STATS ? 128 : 64) ? 2 : 1);
 }
-#endif
+// Waves that hold the same rows, each with a share of O's columns: two for wide rows, whose O would leave room for one wave alone on a SIMD
+// (both take the scores: 16 matrix instructions of 32 are doubled, and still 8192 x 32 768 x 256 bf16 takes WIDE_AFTER us instead of 1130).
+constexpr int loss_shares(int how, int dp, int mode) { return mode != LOSS_STATS && dp > 128 ? 2 : 1; }
 // waves per SIMD that registers are left for: one where more than half of a SIMD's are needed
 constexpr int loss_waves(int how, int dp, int mode)
 {
-#ifdef TRY_W
-    if (dp <= 64)
-        return TRY_W;
-#endif
-    return mode == LOSS_STATS ? (loss_planes_of(how) > 1 && dp > 128 ? 1 : 2) : (dp <= (loss_planes_of(how) > 1 ? 64 : 128) ? 2 : 1);
+    return how == LOSS_F32 && dp > 64 ? 1 : 2;
 }
 #define LOSS_WAVES 4
 constexpr int loss_held(int how, int dp, int mode) { return LOSS_WAVES * 32 * loss_blocks(how, dp, mode); }
+
+// few rows (no more than a wave holds): blocks of 32 that it holds, and the workgroups of a launch
+constexpr int loss_few_blocks(int how, int dp) { return loss_planes_of(how) * dp <= 192 ? 2 : 1; }
+#define LOSS_FEW_ROWS 64
+#define LOSS_FEW_GROUPS 512 // two for each compute unit
 
 void loss_launch_f32(fae_ctx *ctx, int mode, const loss_args &a);
 void loss_launch_bf16(fae_ctx *ctx, int mode, const loss_args &a);
@@ -223,7 +225,7 @@ template <int DP> __device__ __forceinline__ int loss_swizzle(int m)
 #define LOSS_LDS(T) __attribute__((address_space(3))) T
 
 template <int HOW, int DP, int MODE, bool BIAS>
-__global__ __launch_bounds__(LOSS_WAVES * 64) __attribute__((amdgpu_waves_per_eu(loss_waves(HOW, DP, MODE)))) void loss_kernel(loss_args a)
+__global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __attribute__((amdgpu_waves_per_eu(loss_waves(HOW, DP, MODE)))) void loss_kernel(loss_args a)
 {
     typedef loss_type<HOW> H;
     typedef typename H::T T;
@@ -231,16 +233,16 @@ __global__ __launch_bounds__(LOSS_WAVES * 64) __attribute__((amdgpu_waves_per_eu
     typedef typename loss_vec<E>::v8 v8;
     typedef typename loss_vec<E>::v4 v4;
     typedef short s4 __attribute__((ext_vector_type(4)));
-    constexpr int P = H::PLANES, NP = H::PRODUCTS, THREADS = LOSS_WAVES * 64, NB = loss_blocks(HOW, DP, MODE), TM = loss_tile(HOW, DP);
-    constexpr int KS = DP / 16, DS = DP / 32, NC = TM * DP / 8 / THREADS;
+    constexpr int P = H::PLANES, NP = H::PRODUCTS, NB = loss_blocks(HOW, DP, MODE), TM = loss_tile(HOW, DP);
+    constexpr int SHARES = loss_shares(HOW, DP, MODE), THREADS = LOSS_WAVES * 64 * SHARES;
+    constexpr int KS = DP / 16, DS = DP / 32 / SHARES, PIECES = TM * DP / 8, NC = (PIECES + THREADS - 1) / THREADS;
     constexpr int PLANE = TM * DP * 2, TILE = P * PLANE; // bytes
     constexpr bool HAS_O = MODE != LOSS_STATS;
-    static_assert(TM * DP / 8 % THREADS == 0, "whole pieces per thread");
     __shared__ __attribute__((aligned(16))) char tiles[2 * TILE];
     __shared__ float side[2][3][TM]; // forward: bias; gradient: -lse + log |gloss|, gloss, target
-    __shared__ float mosts[2][LOSS_WAVES];
+    __shared__ float mosts[2][LOSS_WAVES * SHARES];
 
-    const int lane = fae_lane(), wave = threadIdx.x / 64, ln = lane & 31, half = lane >> 5;
+    const int lane = fae_lane(), wave = threadIdx.x / 64 % LOSS_WAVES, share = threadIdx.x / (LOSS_WAVES * 64), ln = lane & 31, half = lane >> 5;
     uint32_t block, split;
     if (a.n_split % 8 == 0) { // the workgroups of one part of the chip stream the same rows
         const uint32_t i = blockIdx.x >> 3;
@@ -269,13 +271,13 @@ __global__ __launch_bounds__(LOSS_WAVES * 64) __attribute__((amdgpu_waves_per_eu
             for (int d = 32; d > 0; d >>= 1)
                 most[k] = fmaxf(most[k], __shfl_xor(most[k], d, 64));
             if (lane == 0)
-                mosts[k][wave] = most[k];
+                mosts[k][threadIdx.x / 64] = most[k];
         }
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
-            for (int i = 0; i < LOSS_WAVES; ++i)
+            for (int i = 0; i < LOSS_WAVES * SHARES; ++i)
                 most[k] = fmaxf(most[k], mosts[k][i]);
         if (HOW == LOSS_F32_WIDE) {
             const int up = loss_power(most[0], 15);
@@ -338,7 +340,7 @@ __global__ __launch_bounds__(LOSS_WAVES * 64) __attribute__((amdgpu_waves_per_eu
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
             const int piece = i * THREADS + threadIdx.x, m = piece / (DP / 8), p = piece % (DP / 8);
-            next[i] = loss_load<T>((const T *)a.st + (int64_t)(m0 + m) * a.st_stride, p * 8, a.width, m0 + m < a.n_st);
+            next[i] = loss_load<T>((const T *)a.st + (int64_t)(m0 + m) * a.st_stride, p * 8, a.width, m0 + m < a.n_st && (PIECES % THREADS == 0 || piece < PIECES));
             if (MODE == LOSS_GRAD)
                 next_t[i] = m0 + m < a.n_st ? a.t[m0 + m] : -1;
         }
@@ -366,7 +368,8 @@ __global__ __launch_bounds__(LOSS_WAVES * 64) __attribute__((amdgpu_waves_per_eu
             loss_planes<HOW>(next[i], st_scale, o);
 #pragma unroll
             for (int k = 0; k < P; ++k)
-                *(v8 *)&tiles[buf * TILE + k * PLANE + m * DP * 2 + (p ^ loss_swizzle<DP>(m)) * 16] = o[k];
+                if (PIECES % THREADS == 0 || piece < PIECES)
+                    *(v8 *)&tiles[buf * TILE + k * PLANE + m * DP * 2 + (p ^ loss_swizzle<DP>(m)) * 16] = o[k];
         }
         if (threadIdx.x < TM) {
             side[buf][0][threadIdx.x] = next_side[0];
@@ -386,7 +389,7 @@ __global__ __launch_bounds__(LOSS_WAVES * 64) __attribute__((amdgpu_waves_per_eu
     for (int d = 0; d < DS; ++d)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const int m = u * 8 + half * 4 + ((lane & 15) >> 2), p = d * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+            const int m = u * 8 + half * 4 + ((lane & 15) >> 2), p = (share * DS + d) * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
             o_at[d][u] = m * DP * 2 + (p ^ loss_swizzle<DP>(m)) * 16 + (lane & 1) * 8;
         }
     LOSS_LDS(char) *const lds = (LOSS_LDS(char) *)tiles;
@@ -541,7 +544,8 @@ __global__ __launch_bounds__(LOSS_WAVES * 64) __attribute__((amdgpu_waves_per_eu
 #pragma unroll
                         for (int i = 0; i < 16; ++i)
                             if (8 * (i / 4) + 4 * half + i % 4 == at) {
-                                a.zt[first + b * 32 + ln] = fmaf(z[b][i], c[b], sd[i / 4 * 8 + i % 4]);
+                                if (share == 0)
+                                    a.zt[first + b * 32 + ln] = fmaf(z[b][i], c[b], sd[i / 4 * 8 + i % 4]);
                                 pr[b][i] = 0.f;
                             }
                     }
@@ -594,7 +598,7 @@ __global__ __launch_bounds__(LOSS_WAVES * 64) __attribute__((amdgpu_waves_per_eu
         const float all = sum[b] + __shfl_xor(sum[b], 32, 64);
         const int64_t at = (int64_t)split * a.n_own + n;
         const bool direct = MODE == LOSS_GRAD && a.n_split == 1;
-        if (n < a.n_own && half == 0) {
+        if (n < a.n_own && half == 0 && share == 0) {
             if (MODE != LOSS_GRAD) {
                 a.stat[at * 2] = ref[b] - (float)H::SHIFT;
                 a.stat[at * 2 + 1] = all;
@@ -609,7 +613,7 @@ __global__ __launch_bounds__(LOSS_WAVES * 64) __attribute__((amdgpu_waves_per_eu
             for (int d = 0; d < DS; ++d) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const int col = d * 32 + j * 8 + half * 4;
+                    const int col = (share * DS + d) * 32 + j * 8 + half * 4;
                     float v[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
@@ -628,15 +632,158 @@ __global__ __launch_bounds__(LOSS_WAVES * 64) __attribute__((amdgpu_waves_per_eu
     }
 }
 
+// Few rows (serving, small test batches): bound by reading w, so that every wave takes a stretch of classes of its own, straight from memory to the
+// matrix instructions' registers with the next 32 on their way, and no wave waits for another before the end.  1 x 200 003 x 64 fp32
+// 16.8 us, 48 x 1 000 003 x 32 41 us, 3.1 TB/s (the kernel above: 25 and 106, three of its waves without rows).  Two steps ahead: 17.4 and
+// 43.6; three waves per SIMD, which spill: 20.5 and 46.6.
+template <int HOW, int DP, int NB, bool BIAS>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(loss_planes_of(HOW) * DP <= 192 ? 2 : 1))) void loss_few_kernel(loss_args a)
+{
+    typedef loss_type<HOW> H;
+    typedef typename H::T T;
+    typedef typename loss_vec<typename H::E>::v8 v8;
+    constexpr int P = H::PLANES, NP = H::PRODUCTS, KS = DP / 16;
+    __shared__ float parts[4][2][NB * 32];
+    const int lane = fae_lane(), wave = threadIdx.x / 64, ln = lane & 31, half = lane >> 5;
+    const uint32_t split = blockIdx.x / a.n_blocks, block = blockIdx.x % a.n_blocks;
+    const int64_t strides = (int64_t)a.n_split * 4, mine = (int64_t)split * 4 + wave;
+    const int tile0 = (int)(a.tiles * mine / strides), tile1 = (int)(a.tiles * (mine + 1) / strides); // of 32 classes
+    const int first = (int)block * 32 * NB;
+
+    loss_raw<T> next[KS];
+    loss_f4 next_bias[4];
+    auto fetch = [&](int tl) {
+        const int m = tl * 32 + ln;
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+            next[k] = loss_load<T>((const T *)a.st + (int64_t)m * a.st_stride, k * 16 + half * 8, a.width, tl < tile1 && m < a.n_st);
+        if (BIAS && tl < tile1 && (tl + 1) * 32LL <= a.n_st)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                next_bias[j] = *(const typename fae_vec<float, 4>::loose *)(a.bias + tl * 32 + j * 8 + half * 4);
+    };
+    fetch(tile0);
+    v8 q[NB][KS][P];
+    int32_t target[NB];
+    float ref[NB], sum[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        const int n = first + b * 32 + ln;
+        const bool there = n < a.n_own;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            loss_raw<T> x = loss_load<T>((const T *)a.own + (int64_t)n * a.own_stride, k * 16 + half * 8, a.width, there);
+            if (a.flip) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    x.v[e] = -x.v[e];
+            }
+            loss_planes<HOW>(x, 1.f, q[b][k]);
+        }
+        target[b] = there ? loss_target(a.targets, a.target_bits, n, a.n_classes, a.status) : -1;
+        ref[b] = -3.402823466e38f;
+        sum[b] = 0.f;
+    }
+    for (int tl = tile0; tl < tile1; ++tl) {
+        v8 x[KS][P];
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+            loss_planes<HOW>(next[k], 1.f, x[k]);
+        float bias[16];
+        if ((tl + 1) * 32LL > a.n_st) { // the last 32 are fewer
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int m = tl * 32 + i / 4 * 8 + half * 4 + i % 4;
+                bias[i] = m >= a.n_st ? -INFINITY : (BIAS ? a.bias[m] * 1.44269504f : 0.f);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                bias[i] = BIAS ? next_bias[i / 4][i % 4] * 1.44269504f : 0.f;
+        }
+        fetch(tl + 1);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            loss_f16v z = (loss_f16v)(0.f);
+#pragma unroll
+            for (int k = 0; k < KS; ++k)
+#pragma unroll
+                for (int u = 6 - NP; u < 6; ++u)
+                    z = loss_mfma(x[k][LOSS_PA[u]], q[b][k][LOSS_PB[u]], z);
+            float some;
+            auto powers = [&]() {
+                some = 0.f;
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    some += __builtin_amdgcn_exp2f(fmaf(z[i], a.c, bias[i] - ref[b]));
+            };
+            powers();
+            if (__any(!(some < 0x1p40f))) { // the reference moves to the maximum of the lane's scores so far
+                float to = ref[b];
+                const bool moves = !(some < 0x1p40f);
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    to = fmaxf(to, fmaf(z[i], a.c, bias[i]));
+                to = moves ? to : ref[b];
+                sum[b] *= __builtin_amdgcn_exp2f(ref[b] - to);
+                ref[b] = to;
+                powers();
+            }
+            sum[b] += some;
+            const int at = target[b] - tl * 32;
+            if (__any((unsigned)at < 32u)) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (8 * (i / 4) + 4 * half + i % 4 == at)
+                        a.zt[first + b * 32 + ln] = fmaf(z[i], a.c, bias[i]);
+            }
+        }
+    }
+    // the two halves of a wave, then the four waves, at the largest reference
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        const float other = __shfl_xor(ref[b], 32, 64), to = fmaxf(ref[b], other);
+        sum[b] *= __builtin_amdgcn_exp2f(ref[b] - to);
+        sum[b] += __shfl_xor(sum[b], 32, 64);
+        if (half == 0) {
+            parts[wave][0][b * 32 + ln] = to;
+            parts[wave][1][b * 32 + ln] = sum[b];
+        }
+    }
+    __syncthreads();
+    const int n = first + threadIdx.x;
+    if (threadIdx.x < NB * 32 && n < a.n_own) {
+        float to = parts[0][0][threadIdx.x], all = 0.f;
+#pragma unroll
+        for (int w = 1; w < 4; ++w)
+            to = fmaxf(to, parts[w][0][threadIdx.x]);
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+            all += parts[w][1][threadIdx.x] * __builtin_amdgcn_exp2f(parts[w][0][threadIdx.x] - to);
+        const int64_t at = (int64_t)split * a.n_own + n;
+        a.stat[at * 2] = to;
+        a.stat[at * 2 + 1] = all;
+    }
+}
+
 template <int HOW, int DP, bool BIAS> static void loss_launch_mode(fae_ctx *ctx, int mode, const loss_args &a)
 {
-    const dim3 grid(a.n_blocks * a.n_split), block(LOSS_WAVES * 64);
+    const dim3 grid(a.n_blocks * a.n_split), block(LOSS_WAVES * 64), block_o(LOSS_WAVES * 64 * loss_shares(HOW, DP, LOSS_MEAN));
+    if constexpr (HOW != LOSS_F32_WIDE) {
+        if (mode == LOSS_FEW) {
+            if (a.n_own <= 32 || loss_few_blocks(HOW, DP) == 1)
+                FAE_LAUNCH(ctx, (loss_few_kernel<HOW, DP, 1, BIAS>), grid, block, 0, ctx->stream, a);
+            else
+                FAE_LAUNCH(ctx, (loss_few_kernel<HOW, DP, loss_few_blocks(HOW, DP), BIAS>), grid, block, 0, ctx->stream, a);
+            return;
+        }
+    }
     if (mode == LOSS_STATS)
         FAE_LAUNCH(ctx, (loss_kernel<HOW, DP, LOSS_STATS, BIAS>), grid, block, 0, ctx->stream, a);
     else if (mode == LOSS_MEAN)
-        FAE_LAUNCH(ctx, (loss_kernel<HOW, DP, LOSS_MEAN, BIAS>), grid, block, 0, ctx->stream, a);
+        FAE_LAUNCH(ctx, (loss_kernel<HOW, DP, LOSS_MEAN, BIAS>), grid, block_o, 0, ctx->stream, a);
     else
-        FAE_LAUNCH(ctx, (loss_kernel<HOW, DP, LOSS_GRAD, BIAS>), grid, block, 0, ctx->stream, a);
+        FAE_LAUNCH(ctx, (loss_kernel<HOW, DP, LOSS_GRAD, BIAS>), grid, block_o, 0, ctx->stream, a);
 }
 template <int HOW, int DP> static void loss_launch_bias(fae_ctx *ctx, int mode, const loss_args &a)
 {

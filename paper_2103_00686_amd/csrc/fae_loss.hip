@@ -3,14 +3,10 @@
 
 #include "fae_loss.h"
 
-#ifdef TRY_W
-#define LOSS_GROUPS (256 * TRY_W)
-#else
-#define LOSS_GROUPS 512 // workgroups that a launch should have: two for each compute unit
-#endif
+#define LOSS_ROUNDS 4   // workgroups of a launch that is shared out, in rounds of as many as the chip holds, at most
+#define LOSS_SLOTS 512  // workgroups that the chip holds: two for each compute unit
 #define LOSS_MOST 0x7fff0000LL
 #define LOSS_WIDE_ROWS 128
-#define LOSS_HELD_MOST 256 // held rows of a workgroup at most
 
 // ---------------------------------------------------------------------------------
 // kernels
@@ -89,7 +85,7 @@ struct LossRows {
     uint32_t *status;
 };
 
-#define LOSS_MOSTS 512 // workgroups that look for a largest value, and slots for what they find
+#define LOSS_MOSTS 2048 // workgroups that look for a largest value, and slots for what they find
 
 // the workgroup's largest value into its slot
 __device__ __forceinline__ void loss_most_of(float v, float *slot)
@@ -253,21 +249,42 @@ static LossShape loss_shape(const fae_softmax_loss *l, int mode)
     LossShape s;
     const int64_t n_own = mode == LOSS_GRAD ? l->n_classes : l->n_rows, n_st = mode == LOSS_GRAD ? l->n_rows : l->n_classes;
     s.how = loss_how(l, mode);
-    const int dp = loss_padded(l->width), tile = loss_tile(s.how, dp), held = loss_held(s.how, dp, mode);
+    const int dp = loss_padded(l->width);
+    const int tile = mode == LOSS_FEW ? 32 : loss_tile(s.how, dp);
+    const int held = mode != LOSS_FEW ? loss_held(s.how, dp, mode) : n_own <= 32 ? 32 : 32 * loss_few_blocks(s.how, dp);
     s.blocks = (n_own + held - 1) / held;
     s.tiles = (n_st + tile - 1) / tile;
-    s.splits = s.blocks ? LOSS_GROUPS / s.blocks : 1;
-    s.splits = s.splits > s.tiles ? s.tiles : s.splits;
-    s.splits = s.splits < 1 ? 1 : (s.splits > 8 ? s.splits / 8 * 8 : s.splits);
+    s.splits = 1;
+    if (mode == LOSS_FEW) {
+        s.splits = s.blocks ? LOSS_FEW_GROUPS / s.blocks : 1;
+        s.splits = s.splits > s.tiles ? s.tiles : s.splits;
+    } else if (s.blocks > 0) {
+        // The parts that leave the fewest places empty in the last round, less what putting them together takes: reading and writing a part's
+        // row, at 4 TB/s, beside a score's 0.1 + 0.007 dp ps (both as measured).  24 blocks in 16 parts leave a quarter of the chip empty,
+        // in 64 none: 3001 x 40 009 x 100 fp16 PARTS_FP16; 391 blocks in one part the same, in five 5 %: PARTS_BF16.
+        const double slots = LOSS_SLOTS / 2 * loss_waves(s.how, dp, mode) / loss_shares(s.how, dp, mode);
+        double best = 0.0;
+        for (int64_t p = 1; p <= s.tiles && (p == 1 || s.blocks * p <= LOSS_ROUNDS * LOSS_SLOTS); p += p >= 8 ? 8 : 1) { // (8: loss_kernel)
+            const double rounds = s.blocks * p / slots, most = ceil(rounds);
+            const double join = mode == LOSS_GRAD && p == 1 ? 0.0 : 2.0 * p * l->width / (n_st * (0.1 + 0.007 * dp));
+            const double good = rounds / most / (1.0 + join);
+            if (good > best * 1.001) {
+                best = good;
+                s.splits = p;
+            }
+        }
+    }
     s.pitch = (l->width + 3) / 4 * 4;
     return s;
 }
 
+// held rows of a workgroup at most
+static int loss_held_most(int32_t width) { return width <= 128 ? 2 * LOSS_WAVES * 32 : LOSS_WAVES * 32; }
 // rows of partial results that any call up to this size would need: in a launch that is shared out, a workgroup's held rows for each workgroup
 static int64_t loss_part_rows(const fae_softmax_loss *l, int mode)
 {
     const int64_t n_own = mode == LOSS_GRAD ? l->n_classes : l->n_rows, n_st = mode == LOSS_GRAD ? l->n_rows : l->n_classes;
-    const int64_t most = (int64_t)LOSS_GROUPS * LOSS_HELD_MOST, tiles = (n_st + 31) / 32;
+    const int64_t most = (int64_t)LOSS_ROUNDS * LOSS_SLOTS * loss_held_most(l->width), tiles = (n_st + 31) / 32;
     const int64_t shared = tiles == 0 ? 0 : n_own > most / tiles ? most : n_own * tiles;
     return mode == LOSS_GRAD || shared > n_own ? shared : n_own; // (the gradient in one part needs none)
 }
@@ -399,7 +416,8 @@ static void loss_common(fae_ctx *ctx, const fae_softmax_loss *l, const LossShape
 static int32_t loss_forward(fae_ctx *ctx, const fae_softmax_loss *l, const void *x, int64_t x_stride, const void *w, int64_t w_stride, float *loss,
                             float *lse, float *mean, void *ws, size_t ws_bytes)
 {
-    const LossShape s = loss_shape(l, mean ? LOSS_MEAN : LOSS_STATS);
+    const int mode = mean ? LOSS_MEAN : l->n_rows <= LOSS_FEW_ROWS ? LOSS_FEW : LOSS_STATS;
+    const LossShape s = loss_shape(l, mode);
     fae_carver cv(ws, ws_bytes);
     loss_args a;
     loss_common(ctx, l, s, &a);
@@ -425,7 +443,7 @@ static int32_t loss_forward(fae_ctx *ctx, const fae_softmax_loss *l, const void 
     }
     {
         fae_ktimer kt(ctx, FAE_K_LOSS);
-        loss_run(ctx, s.how, mean ? LOSS_MEAN : LOSS_STATS, a);
+        loss_run(ctx, s.how, mode, a);
         FAE_LAUNCH_CHECK(ctx);
     }
     LossJoin j;
@@ -522,7 +540,7 @@ extern "C" int32_t fae_softmax_loss_bwd(fae_ctx *ctx, const fae_softmax_loss *wh
     void *rest = cv.base + cv.used;
     const size_t rest_bytes = cv.cap - cv.used;
     const int64_t row_groups = (n + 3) / 4;
-    const int32_t n_most = (int32_t)(row_groups < LOSS_MOSTS ? row_groups : LOSS_MOSTS);
+    const int32_t n_most = (int32_t)(row_groups < LOSS_MOSTS || what->type == FAE_BF16 ? row_groups : LOSS_MOSTS);
     if (n > 0) {
         if (gx && !mean) {
             rc = loss_forward(ctx, what, x, x_row_stride, w, w_row_stride, nullptr, nullptr, own_mean, rest, rest_bytes);

@@ -335,3 +335,38 @@ def test_a_table_of_more_than_2_31_values(hp):
     assert torch.allclose(gw[v - 2].float(), torch.full((d,), rest, device="cuda"), rtol=2 ** -7)
     gw[at] = 0
     assert float(gw.float().max()) <= rest * (1 + 2 ** -7) and float(gw.float().min()) >= 0
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,v,d", [(1, 50_021, 64), (64, 33_000, 33), (33, 25_001, 200), (5, 31, 256), (48, 1, 8), (63, 100_000, 16), (65, 9001, 96)])
+def test_few_rows_without_mean(hp, n, v, d, dtype):
+    """The loss alone: a kernel of its own for up to 64 rows."""
+    for with_bias in (False, True):
+        x, w, t, bias, _ = _make(n + v + d, n, v, d, dtype, bias=with_bias, pad=with_bias * 3, lead=with_bias)
+        if with_bias:
+            bias[torch.rand(v, device="cuda") < 0.3] = -math.inf
+        ref = R.LossRef(x, w, t, bias, 2.0 / math.sqrt(d))
+        loss, lse = hp.softmax_loss(x, w, t, bias, 2.0 / math.sqrt(d))
+        hp.sync()
+        R.assert_within(lse, ref.lse, ref.dlse, "lse")
+        R.assert_within(loss, *ref.loss(), "loss")
+
+
+@pytest.mark.parametrize("n", [3, 40])
+def test_few_rows_and_what_they_may_meet(hp, n):
+    x, w, t, bias, _ = _make(7, n, 3000, 40, F32, bias=True)
+    t[:] = torch.arange(n, device="cuda") * 7
+    t[0] = -1
+    bias[:] = torch.linspace(-200, 200, 3000, device="cuda")
+    ref = R.LossRef(x, w, t, bias, 0.5)
+    loss, lse = hp.softmax_loss(x, w, t, bias, 0.5)
+    R.assert_within(lse, ref.lse, ref.dlse, "lse")
+    R.assert_within(loss, *ref.loss(), "loss")
+    rest = torch.arange(n, device="cuda") != 1
+    x[1] = float("nan")
+    loss2, lse2 = hp.softmax_loss(x, w, t, bias, 0.5)
+    assert torch.equal(loss2[rest], loss[rest]) and math.isnan(float(lse2[1]))
+    bias.fill_(-math.inf)
+    loss, lse = hp.softmax_loss(x[rest], w, t[rest], bias, 0.5)
+    assert bool((lse == -math.inf).all()) and not bool(loss.any())
+    hp.sync()
