@@ -37,6 +37,7 @@ struct loss_args {
     float scale;
     int32_t pitch, tiles; // tiles: of streamed rows
     uint32_t n_blocks, n_split;
+    int32_t spread; // forward: all waves hold the same rows (there are no more than one holds), and take the streamed blocks of 32 in turn
 };
 
 // What a kernel is built for: the types, and fp32 in two ways (loss_type says how).
@@ -51,7 +52,8 @@ constexpr int loss_blocks(int how, int dp, int mode)
     return loss_planes_of(how) > 1 ? (dp <= 32 ? 2 : 1) : (dp <= (mode == LOSS_STATS ? 128 : 64) ? 2 : 1);
 }
 // Waves that hold the same rows, each with a share of O's columns: two for wide rows, whose O would leave room for one wave alone on a SIMD
-// (both take the scores: 16 matrix instructions of 32 are doubled, and still 8192 x 32 768 x 256 bf16 takes WIDE_AFTER us instead of 1130).
+// (both take the scores: half of the matrix instructions are doubled, and still a step of 8192 x 32 768 x 256 bf16 takes 900 us instead of
+// 1130).
 constexpr int loss_shares(int how, int dp, int mode) { return mode != LOSS_STATS && dp > 128 ? 2 : 1; }
 // waves per SIMD that registers are left for: one where more than half of a SIMD's are needed
 constexpr int loss_waves(int how, int dp, int mode)
@@ -222,6 +224,16 @@ template <int DP> __device__ __forceinline__ int loss_swizzle(int m)
     return u == 0 ? ((m & 3) << 2) | ((m >> 2) & 3) : u == 8 ? ((m & 2) << 1) | ((m >> 2) & 3) : (m >> 2) & 3;
 }
 
+// (in pairs: a chain of 16 additions would wait for each of them)
+__device__ __forceinline__ float loss_sum(const float (&v)[16])
+{
+    float s[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        s[i] = v[i] + v[i + 8];
+    return ((s[0] + s[4]) + (s[2] + s[6])) + ((s[1] + s[5]) + (s[3] + s[7]));
+}
+
 #define LOSS_LDS(T) __attribute__((address_space(3))) T
 
 template <int HOW, int DP, int MODE, bool BIAS>
@@ -253,7 +265,7 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
         block = blockIdx.x % a.n_blocks;
     }
     const int tile0 = (int)((int64_t)a.tiles * split / a.n_split), tile1 = (int)((int64_t)a.tiles * (split + 1) / a.n_split);
-    const int first = (int)(block * (LOSS_WAVES * 32 * NB)) + wave * 32 * NB; // the wave's held rows; this lane's are first + ln + 32 b (they may lie behind the last)
+    const int first = (int)(block * (LOSS_WAVES * 32 * NB)) + (MODE != LOSS_GRAD && a.spread ? 0 : wave * 32 * NB); // the wave's held rows; this lane's are first + ln + 32 b (they may lie behind the last)
 
     // What was found before: the largest streamed value and gradient.  fp16 numbers of both are brought to a range that keeps them.
     float st_scale = 1.f, g_scale = 1.f, g_log = 0.f, c_all = a.c, back = 1.f;
@@ -418,6 +430,8 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
         const bool biased = BIAS || (tl + 1) * (int64_t)TM > a.n_st; // forward: also where the last tile has fewer rows
 #pragma unroll 1
         for (int sb = 0; sb < TM / 32; ++sb) {
+            if (MODE != LOSS_GRAD && a.spread && ((tl * (TM / 32) + sb) & (LOSS_WAVES - 1)) != wave)
+                continue;
             // Z: element i is streamed row 8 (i / 4) + 4 half + i % 4 and held row ln.  One held block after the other: a matrix instruction that
             // waits for the one before leaves the vector unit to the SIMD's other waves, one that waits for the matrix unit does not
             // (24 of them beside 200 vector instructions: 503 ns in one chain, 577 in two).
@@ -469,13 +483,8 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
                     }
                 }
 #pragma unroll
-                for (int b = 0; b < NB; ++b) {
-                    float some = 0.f;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        some += pr[b][i];
-                    sum[b] += some;
-                }
+                for (int b = 0; b < NB; ++b)
+                    sum[b] += loss_sum(pr[b]);
             } else {
                 float some[NB];
                 auto powers = [&](int b) {
@@ -596,7 +605,7 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
     for (int b = 0; b < NB; ++b) {
         const int n = first + b * 32 + ln;
         const float all = sum[b] + __shfl_xor(sum[b], 32, 64);
-        const int64_t at = (int64_t)split * a.n_own + n;
+        const int64_t at = (int64_t)(MODE != LOSS_GRAD && a.spread ? split * LOSS_WAVES + wave : split) * a.n_own + n;
         const bool direct = MODE == LOSS_GRAD && a.n_split == 1;
         if (n < a.n_own && half == 0 && share == 0) {
             if (MODE != LOSS_GRAD) {

@@ -7,6 +7,8 @@
 #define LOSS_SLOTS 512  // workgroups that the chip holds: two for each compute unit
 #define LOSS_MOST 0x7fff0000LL
 #define LOSS_WIDE_ROWS 128
+#define LOSS_WIDE_SCORES (1LL << 24)
+#define LOSS_WIDE_VALUES (1LL << 22)
 
 // ---------------------------------------------------------------------------------
 // kernels
@@ -21,27 +23,43 @@ struct LossJoin {
     uint32_t *status;
 };
 
-// A wave per row: the parts' sums at one reference, loss and lse, and the weighted sum of the parts' means.
-__global__ __launch_bounds__(256) void loss_join_kernel(LossJoin a)
+// W waves per row: the parts' sums at one reference, loss and lse, and the weighted sum of the parts' means.  One wave is a chain of as many
+// loads as there are parts: 12 rows in 1024 parts take 180 us with one wave each,
+// 15 with 16.
+template <int W> __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void loss_join_kernel(LossJoin a)
 {
-    const int lane = fae_lane();
-    const int64_t r = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
-    if (r >= a.n_rows)
+    __shared__ float part[W][64 * 4];
+    const int lane = fae_lane(), wave = W == 1 ? 0 : threadIdx.x / 64;
+    const int64_t r = W == 1 ? (int64_t)blockIdx.x * 4 + threadIdx.x / 64 : blockIdx.x;
+    if (W == 1 && r >= a.n_rows)
         return;
+    auto over_waves = [&](float v, bool most) {
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) {
+            const float o = __shfl_xor(v, d, 64);
+            v = most ? fmaxf(v, o) : v + o;
+        }
+        if (W > 1) {
+            __syncthreads();
+            if (lane == 0)
+                part[wave][0] = v;
+            __syncthreads();
+            v = part[0][0];
+            for (int w = 1; w < W; ++w)
+                v = most ? fmaxf(v, part[w][0]) : v + part[w][0];
+        }
+        return v;
+    };
     float most = -INFINITY;
-    for (uint32_t i = lane; i < a.n_split; i += 64)
+    for (uint32_t i = wave * 64 + lane; i < a.n_split; i += W * 64)
         most = fmaxf(most, a.stat[(i * a.n_rows + r) * 2]);
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1)
-        most = fmaxf(most, __shfl_xor(most, d, 64));
+    most = over_waves(most, true);
     float sum = 0.f;
-    for (uint32_t i = lane; i < a.n_split; i += 64)
+    for (uint32_t i = wave * 64 + lane; i < a.n_split; i += W * 64)
         sum += a.stat[(i * a.n_rows + r) * 2 + 1] * __builtin_amdgcn_exp2f(a.stat[(i * a.n_rows + r) * 2] - most);
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1)
-        sum += __shfl_xor(sum, d, 64);
+    sum = over_waves(sum, false);
     const float l2 = most + __log2f(sum);
-    if (lane == 0) {
+    if (lane == 0 && wave == 0) {
         const int32_t t = loss_target(a.targets, a.target_bits, r, a.n_classes, a.status);
         if (a.lse)
             a.lse[r] = l2 * 0.693147181f;
@@ -53,7 +71,7 @@ __global__ __launch_bounds__(256) void loss_join_kernel(LossJoin a)
     const int col = (lane % a.lanes) * 4;
     float v[4] = {0.f, 0.f, 0.f, 0.f};
     if (col < a.pitch)
-        for (uint32_t i = lane / a.lanes; i < a.n_split; i += 64 / a.lanes) {
+        for (uint32_t i = lane / a.lanes + wave * (64 / a.lanes); i < a.n_split; i += 64 / a.lanes * W) {
             const float f = __builtin_amdgcn_exp2f(a.stat[(i * a.n_rows + r) * 2] - most);
             const float4 p = *(const float4 *)(a.part + (i * a.n_rows + r) * a.pitch + col);
             v[0] += f * p.x;
@@ -65,7 +83,18 @@ __global__ __launch_bounds__(256) void loss_join_kernel(LossJoin a)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             v[e] += __shfl_xor(v[e], d, 64);
-    if (lane < (int)a.lanes)
+    if (W > 1) {
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            part[wave][lane * 4 + e] = v[e];
+        __syncthreads();
+        for (int w = 1; w < W; ++w)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[e] = (w == 1 ? part[0][lane * 4 + e] : v[e]) + part[w][lane * 4 + e];
+    }
+    if (lane < (int)a.lanes && wave == 0)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             if (col + e < a.width)
@@ -232,17 +261,23 @@ static bool loss_sizes_fit(const fae_softmax_loss *l)
            l->width <= FAE_LOSS_MAX_WIDTH && l->type >= FAE_F32 && l->type <= FAE_F16;
 }
 
-// fp32 as two fp16 numbers or three bf16: the first take a look at all streamed rows before, which a forward of few rows does not pay for
+// fp32 as two fp16 numbers or three bf16: the first take half the matrix instructions and fewer registers, and a look at all streamed rows
+// before (5 us and reading them).  Steps in us, two fp16 numbers and three bf16: 40 x 300 000 x 100 216 and 269, 1 x 1 000 000 x 32 equal,
+// 300 x 5003 x 16 41 and 39, 2048 x 1 000 000 x 32 1730 and 2860.
 static int loss_how(const fae_softmax_loss *l, int mode)
 {
-    return l->type == FAE_BF16 ? LOSS_BF16 : l->type == FAE_F16 ? LOSS_F16 : mode == LOSS_GRAD || l->n_rows >= LOSS_WIDE_ROWS ? LOSS_F32_WIDE : LOSS_F32;
+    if (l->type != FAE_F32)
+        return l->type == FAE_BF16 ? LOSS_BF16 : LOSS_F16;
+    const bool pays = (l->n_rows >= LOSS_WIDE_ROWS && l->n_rows * l->n_classes >= LOSS_WIDE_SCORES) ||
+                      (mode == LOSS_MEAN && l->width > 64 && l->n_classes * l->width >= LOSS_WIDE_VALUES);
+    return mode == LOSS_GRAD || pays ? LOSS_F32_WIDE : LOSS_F32;
 }
 
 // n_own held rows in workgroups of some, n_st streamed rows shared out among as many of them as fill the chip
 struct LossShape {
     int how;
     int64_t blocks, tiles, splits;
-    int32_t pitch;
+    int32_t pitch, held;
 };
 static LossShape loss_shape(const fae_softmax_loss *l, int mode)
 {
@@ -252,6 +287,7 @@ static LossShape loss_shape(const fae_softmax_loss *l, int mode)
     const int dp = loss_padded(l->width);
     const int tile = mode == LOSS_FEW ? 32 : loss_tile(s.how, dp);
     const int held = mode != LOSS_FEW ? loss_held(s.how, dp, mode) : n_own <= 32 ? 32 : 32 * loss_few_blocks(s.how, dp);
+    s.held = held;
     s.blocks = (n_own + held - 1) / held;
     s.tiles = (n_st + tile - 1) / tile;
     s.splits = 1;
@@ -261,7 +297,8 @@ static LossShape loss_shape(const fae_softmax_loss *l, int mode)
     } else if (s.blocks > 0) {
         // The parts that leave the fewest places empty in the last round, less what putting them together takes: reading and writing a part's
         // row, at 4 TB/s, beside a score's 0.1 + 0.007 dp ps (both as measured).  24 blocks in 16 parts leave a quarter of the chip empty,
-        // in 64 none: 3001 x 40 009 x 100 fp16 PARTS_FP16; 391 blocks in one part the same, in five 5 %: PARTS_BF16.
+        // in 40 6 %: 3001 x 40 009 x 100 fp16 forward 137 and 116 us; 391 blocks in one part the same, in five 5 %: the gradient
+        // of 16 384 x 100 003 x 64 bf16 666 and 577 us.
         const double slots = LOSS_SLOTS / 2 * loss_waves(s.how, dp, mode) / loss_shares(s.how, dp, mode);
         double best = 0.0;
         for (int64_t p = 1; p <= s.tiles && (p == 1 || s.blocks * p <= LOSS_ROUNDS * LOSS_SLOTS); p += p >= 8 ? 8 : 1) { // (8: loss_kernel)
@@ -284,7 +321,8 @@ static int loss_held_most(int32_t width) { return width <= 128 ? 2 * LOSS_WAVES 
 static int64_t loss_part_rows(const fae_softmax_loss *l, int mode)
 {
     const int64_t n_own = mode == LOSS_GRAD ? l->n_classes : l->n_rows, n_st = mode == LOSS_GRAD ? l->n_rows : l->n_classes;
-    const int64_t most = (int64_t)LOSS_ROUNDS * LOSS_SLOTS * loss_held_most(l->width), tiles = (n_st + 31) / 32;
+    const int64_t most = (int64_t)LOSS_ROUNDS * LOSS_SLOTS * loss_held_most(l->width);
+    const int64_t tiles = (n_st + 31) / 32 * (mode == LOSS_GRAD ? 1 : LOSS_WAVES); // (forward: also a part for each wave)
     const int64_t shared = tiles == 0 ? 0 : n_own > most / tiles ? most : n_own * tiles;
     return mode == LOSS_GRAD || shared > n_own ? shared : n_own; // (the gradient in one part needs none)
 }
@@ -428,9 +466,12 @@ static int32_t loss_forward(fae_ctx *ctx, const fae_softmax_loss *l, const void 
     a.n_st = (int32_t)l->n_classes;
     a.n_own = (int32_t)l->n_rows;
     float *most = cv.take<float>(LOSS_MOSTS);
-    a.stat = cv.take<float>(s.splits * l->n_rows * 2);
+    // one wave's rows: the four share the streamed rows out among themselves, and leave a part each
+    a.spread = mode == LOSS_MEAN && l->n_rows <= s.held / LOSS_WAVES;
+    const int64_t parts = a.spread ? s.splits * LOSS_WAVES : s.splits;
+    a.stat = cv.take<float>(parts * l->n_rows * 2);
     a.zt = cv.take<float>(l->n_rows);
-    a.part = mean ? cv.take<float>(s.splits * l->n_rows * s.pitch) : nullptr;
+    a.part = mean ? cv.take<float>(parts * l->n_rows * s.pitch) : nullptr;
     if (!cv.ok)
         return fae_fail(ctx, FAE_ENOSPC, "softmax loss: workspace too small");
     if (s.how == LOSS_F32_WIDE) {
@@ -460,13 +501,18 @@ static int32_t loss_forward(fae_ctx *ctx, const fae_softmax_loss *l, const void 
     j.width = l->width;
     j.pitch = s.pitch;
     j.n_rows = l->n_rows;
-    j.n_split = a.n_split;
+    j.n_split = (uint32_t)parts;
     j.lanes = 1;
     while ((int)j.lanes * 4 < s.pitch)
         j.lanes *= 2;
     j.status = ctx->d_block;
     fae_ktimer kt(ctx, FAE_K_LOSS_JOIN);
-    FAE_LAUNCH(ctx, loss_join_kernel, dim3((uint32_t)((l->n_rows + 3) / 4)), dim3(256), 0, ctx->stream, j);
+    if (parts >= 64 && l->n_rows <= 2048)
+        FAE_LAUNCH(ctx, (loss_join_kernel<16>), dim3((uint32_t)l->n_rows), dim3(1024), 0, ctx->stream, j);
+    else if (parts >= 16)
+        FAE_LAUNCH(ctx, (loss_join_kernel<4>), dim3((uint32_t)l->n_rows), dim3(256), 0, ctx->stream, j);
+    else
+        FAE_LAUNCH(ctx, (loss_join_kernel<1>), dim3((uint32_t)((l->n_rows + 3) / 4)), dim3(256), 0, ctx->stream, j);
     FAE_LAUNCH_CHECK(ctx);
     return FAE_OK;
 }
