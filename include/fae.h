@@ -411,16 +411,16 @@ int32_t fae_dropout_bwd(fae_ctx *ctx, const fae_drop *drop, int64_t n_rows, int3
  * their values.  Products of 16-bit values are exact and their sums fp32.  An fp32 value is taken as the sum of two fp16 numbers, after a power
  * of two that brings the largest value of its row, or of all rows, to 2^14 .. 2^15 (calls with few rows: as three bf16 numbers, without one);
  * of a product at most 2^-20 is lost, and a value below 2^-18 of that largest is kept to 2^-39 of it.  Probabilities enter the gradients'
- * sums rounded to the type (fp32: as two or three numbers again).  x and w have to be finite; in the gradients, rows
- * without a target may hold anything.
+ * sums rounded to the type (fp32: as two or three numbers again).  x and w have to be finite; but rows without a
+ * target may hold anything in the gradients, and classes that are not offered anything anywhere unless they are a target.
  *   targets: int32 or int64 (target_bits), one per row.  A negative one is a row without a target (a cold row, padding):
  *     its loss is 0, its gradients are 0 and it adds nothing to gw and gbias.  One of n_classes or more is treated so too,
  *     and reported as FAE_ERANGE by the next synchronising call.
- *   bias: may be -infinity (a class that is not offered: probability 0).  A row for which no class is offered has
+ *   bias: may be -infinity, or anything below -2.3e38 (a class that is not offered: probability 0).  A row for which no class is offered has
  *     lse = -infinity, loss 0 and no gradients; one whose target is not offered has loss +infinity and finite gradients. */
 typedef struct {
-    int64_t n_rows;    /* 0 .. 2^31 - 1 */
-    int64_t n_classes; /* 1 .. 2^31 - 1 */
+    int64_t n_rows;    /* 0 .. 2^31 - 2^16 - 1 */
+    int64_t n_classes; /* 1 .. 2^31 - 2^16 - 1 */
     int32_t width;     /* 1 .. FAE_LOSS_MAX_WIDTH */
     int32_t type;      /* of x, w and their gradients */
     float scale;       /* finite */

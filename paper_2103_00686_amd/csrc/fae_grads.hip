@@ -240,7 +240,7 @@ static int grads_by_start(const void *a, const void *b)
 }
 
 // no output on another tensor's memory (its own gradient's, whole, is allowed), on the norm or the workspace
-static int32_t grads_check_overlap(fae_ctx *ctx, const char *who, int32_t n, const fae_grad *h, const float *norm, const void *ws, size_t ws_bytes)
+static int32_t grads_check_overlap(fae_ctx *ctx, const char *who, int32_t n, const fae_grad *h, bool clip, const float *norm, const void *ws, size_t ws_bytes)
 {
     GradsSpan *s = (GradsSpan *)malloc(sizeof(GradsSpan) * (2 * (size_t)n + 2));
     if (!s)
@@ -253,8 +253,9 @@ static int32_t grads_check_overlap(fae_ctx *ctx, const char *who, int32_t n, con
         const int64_t bytes = h[z].n * fae_type_size(h[z].type);
         if (bytes == 0)
             continue;
-        s[k++] = {(uintptr_t)h[z].out, (uintptr_t)h[z].out + bytes, z, true};
-        if (h[z].g != h[z].out)
+        if (clip)
+            s[k++] = {(uintptr_t)h[z].out, (uintptr_t)h[z].out + bytes, z, true};
+        if (!clip || h[z].g != h[z].out)
             s[k++] = {(uintptr_t)h[z].g, (uintptr_t)h[z].g + bytes, z, false};
     }
     qsort(s, k, sizeof(*s), grads_by_start);
@@ -348,7 +349,10 @@ static int32_t grads_sums(fae_ctx *ctx, int32_t n_grads, const fae_grad *h, Grad
 
 extern "C" int32_t fae_grad_norm(fae_ctx *ctx, int32_t n_grads, const fae_grad *h_grads, float scale, float *norm, void *ws, size_t ws_bytes)
 {
-    int32_t rc = grads_check(ctx, "fae_grad_norm", n_grads, h_grads, scale, norm, ws, ws_bytes, false);
+    const char *who = "fae_grad_norm";
+    int32_t rc = grads_check(ctx, who, n_grads, h_grads, scale, norm, ws, ws_bytes, false);
+    if (rc == FAE_OK)
+        rc = grads_check_overlap(ctx, who, n_grads, h_grads, false, norm, ws, fae_grad_workspace_bytes(n_grads, h_grads));
     if (rc != FAE_OK)
         return rc;
     FAE_HIP(ctx, hipSetDevice(ctx->device));
@@ -375,7 +379,7 @@ extern "C" int32_t fae_grad_clip(fae_ctx *ctx, int32_t n_grads, const fae_grad *
         return rc;
     if (!(max_norm >= 0.f))
         return fae_fail(ctx, FAE_EINVAL, "%s: max_norm=%g", who, max_norm);
-    rc = grads_check_overlap(ctx, who, n_grads, h_grads, norm, ws, fae_grad_workspace_bytes(n_grads, h_grads));
+    rc = grads_check_overlap(ctx, who, n_grads, h_grads, true, norm, ws, fae_grad_workspace_bytes(n_grads, h_grads));
     if (rc != FAE_OK)
         return rc;
     FAE_HIP(ctx, hipSetDevice(ctx->device));

@@ -102,7 +102,7 @@ template <int HOW> struct loss_type;
 template <> struct loss_type<LOSS_BF16> {
     typedef fae_bf16 T, E;
     static constexpr int PLANES = 1, PRODUCTS = 1, SHIFT = 0;
-    static constexpr float MOST = 0x1p40f;
+    static constexpr float MOST = 0x1p24f;
 };
 template <> struct loss_type<LOSS_F16> {
     typedef fae_f16 T, E;
@@ -113,7 +113,7 @@ template <> struct loss_type<LOSS_F32> {
     typedef float T;
     typedef fae_bf16 E;
     static constexpr int PLANES = 3, PRODUCTS = 6, SHIFT = 0;
-    static constexpr float MOST = 0x1p40f;
+    static constexpr float MOST = 0x1p24f;
 };
 template <> struct loss_type<LOSS_F32_WIDE> {
     typedef float T;
@@ -297,8 +297,8 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
             back = __builtin_amdgcn_ldexpf(1.f, -up);
             c_all *= back;
         }
-        if (MODE == LOSS_GRAD) { // the largest P is 2^12
-            const int up = loss_power(most[1], 12);
+        if (MODE == LOSS_GRAD) { // the largest P is below 2^15: of a probability of 2^-20, fp32 keeps 20 bits still
+            const int up = loss_power(most[1], 15);
             g_scale = __builtin_amdgcn_ldexpf(1.f, up);
             g_log = (float)up;
         }
@@ -311,7 +311,8 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
         const int n = first + b * 32 + ln;
-        const bool there = n < a.n_own;
+        own_bias[b] = MODE == LOSS_GRAD && BIAS && n < a.n_own ? a.bias[n] * 1.44269504f : 0.f;
+        const bool there = n < a.n_own && own_bias[b] != -INFINITY;
         const T *row = (const T *)a.own + (int64_t)n * a.own_stride;
         float scale = a.flip ? -1.f : 1.f;
         c[b] = c_all;
@@ -340,7 +341,6 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
             loss_planes<HOW>(x, scale, q[b][k]);
         }
         target[b] = MODE != LOSS_GRAD && there ? loss_target(a.targets, a.target_bits, n, a.n_classes, a.status) : -1;
-        own_bias[b] = MODE == LOSS_GRAD && BIAS && there ? a.bias[n] * 1.44269504f : 0.f;
     }
 
     // the next tile on its way from memory to LDS
@@ -355,6 +355,8 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
             next[i] = loss_load<T>((const T *)a.st + (int64_t)(m0 + m) * a.st_stride, p * 8, a.width, m0 + m < a.n_st && (PIECES % THREADS == 0 || piece < PIECES));
             if (MODE == LOSS_GRAD)
                 next_t[i] = m0 + m < a.n_st ? a.t[m0 + m] : -1;
+            else if (BIAS)
+                next_t[i] = m0 + m < a.n_st && a.bias[m0 + m] * 1.44269504f == -INFINITY ? -1 : 0;
         }
         if (threadIdx.x < TM) {
             const int m = m0 + threadIdx.x;
@@ -372,7 +374,7 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
         for (int i = 0; i < NC; ++i) {
             const int piece = i * THREADS + threadIdx.x, m = piece / (DP / 8), p = piece % (DP / 8);
             v8 o[P];
-            if (MODE == LOSS_GRAD) { // a row without a target may hold anything, and 0 times that is not always 0
+            if (MODE == LOSS_GRAD || BIAS) { // a row without a target, or a class that is not offered, may hold anything, and 0 times that is not always 0
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
                     next[i].v[e] = next_t[i] < 0 ? (T)0.f : next[i].v[e];
@@ -661,11 +663,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(loss_planes
 
     loss_raw<T> next[KS];
     loss_f4 next_bias[4];
+    bool next_gone = false;
     auto fetch = [&](int tl) {
         const int m = tl * 32 + ln;
 #pragma unroll
         for (int k = 0; k < KS; ++k)
             next[k] = loss_load<T>((const T *)a.st + (int64_t)m * a.st_stride, k * 16 + half * 8, a.width, tl < tile1 && m < a.n_st);
+        next_gone = BIAS && tl < tile1 && m < a.n_st && a.bias[m] * 1.44269504f == -INFINITY; // such a class may hold anything
         if (BIAS && tl < tile1 && (tl + 1) * 32LL <= a.n_st)
 #pragma unroll
             for (int j = 0; j < 4; ++j)
@@ -696,8 +700,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(loss_planes
     for (int tl = tile0; tl < tile1; ++tl) {
         v8 x[KS][P];
 #pragma unroll
-        for (int k = 0; k < KS; ++k)
+        for (int k = 0; k < KS; ++k) {
+            if (BIAS) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    next[k].v[e] = next_gone ? (T)0.f : next[k].v[e];
+            }
             loss_planes<HOW>(next[k], 1.f, x[k]);
+        }
         float bias[16];
         if ((tl + 1) * 32LL > a.n_st) { // the last 32 are fewer
 #pragma unroll
@@ -727,9 +737,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(loss_planes
                     some += __builtin_amdgcn_exp2f(fmaf(z[i], a.c, bias[i] - ref[b]));
             };
             powers();
-            if (__any(!(some < 0x1p40f))) { // the reference moves to the maximum of the lane's scores so far
+            if (__any(!(some < loss_type<HOW>::MOST))) { // the reference moves to the maximum of the lane's scores so far
                 float to = ref[b];
-                const bool moves = !(some < 0x1p40f);
+                const bool moves = !(some < loss_type<HOW>::MOST);
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
                     to = fmaxf(to, fmaf(z[i], a.c, bias[i]));

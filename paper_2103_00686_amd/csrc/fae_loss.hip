@@ -6,6 +6,7 @@
 #define LOSS_ROUNDS 4   // workgroups of a launch that is shared out, in rounds of as many as the chip holds, at most
 #define LOSS_SLOTS 512  // workgroups that the chip holds: two for each compute unit
 #define LOSS_MOST 0x7fff0000LL
+#define LOSS_GRID (1 << 20) // workgroups of a kernel over rows at most: a grid holds fewer than 2^32 threads
 #define LOSS_WIDE_ROWS 128
 #define LOSS_WIDE_SCORES (1LL << 24)
 #define LOSS_WIDE_VALUES (1LL << 22)
@@ -30,9 +31,6 @@ template <int W> __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void loss_j
 {
     __shared__ float part[W][64 * 4];
     const int lane = fae_lane(), wave = W == 1 ? 0 : threadIdx.x / 64;
-    const int64_t r = W == 1 ? (int64_t)blockIdx.x * 4 + threadIdx.x / 64 : blockIdx.x;
-    if (W == 1 && r >= a.n_rows)
-        return;
     auto over_waves = [&](float v, bool most) {
 #pragma unroll
         for (int d = 32; d > 0; d >>= 1) {
@@ -50,55 +48,57 @@ template <int W> __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void loss_j
         }
         return v;
     };
-    float most = -INFINITY;
-    for (uint32_t i = wave * 64 + lane; i < a.n_split; i += W * 64)
-        most = fmaxf(most, a.stat[(i * a.n_rows + r) * 2]);
-    most = over_waves(most, true);
-    float sum = 0.f;
-    for (uint32_t i = wave * 64 + lane; i < a.n_split; i += W * 64)
-        sum += a.stat[(i * a.n_rows + r) * 2 + 1] * __builtin_amdgcn_exp2f(a.stat[(i * a.n_rows + r) * 2] - most);
-    sum = over_waves(sum, false);
-    const float l2 = most + __log2f(sum);
-    if (lane == 0 && wave == 0) {
-        const int32_t t = loss_target(a.targets, a.target_bits, r, a.n_classes, a.status);
-        if (a.lse)
-            a.lse[r] = l2 * 0.693147181f;
-        if (a.loss)
-            a.loss[r] = t < 0 || sum == 0.f ? 0.f : (l2 - a.zt[r]) * 0.693147181f;
-    }
-    if (!a.mean)
-        return;
-    const int col = (lane % a.lanes) * 4;
-    float v[4] = {0.f, 0.f, 0.f, 0.f};
-    if (col < a.pitch)
-        for (uint32_t i = lane / a.lanes + wave * (64 / a.lanes); i < a.n_split; i += 64 / a.lanes * W) {
-            const float f = __builtin_amdgcn_exp2f(a.stat[(i * a.n_rows + r) * 2] - most);
-            const float4 p = *(const float4 *)(a.part + (i * a.n_rows + r) * a.pitch + col);
-            v[0] += f * p.x;
-            v[1] += f * p.y;
-            v[2] += f * p.z;
-            v[3] += f * p.w;
+    for (int64_t r = W == 1 ? (int64_t)blockIdx.x * 4 + threadIdx.x / 64 : blockIdx.x; r < a.n_rows; r += (int64_t)gridDim.x * (W == 1 ? 4 : 1)) {
+        float most = -INFINITY;
+        for (uint32_t i = wave * 64 + lane; i < a.n_split; i += W * 64)
+            most = fmaxf(most, a.stat[(i * a.n_rows + r) * 2]);
+        most = over_waves(most, true);
+        float sum = 0.f;
+        for (uint32_t i = wave * 64 + lane; i < a.n_split; i += W * 64)
+            sum += a.stat[(i * a.n_rows + r) * 2 + 1] * __builtin_amdgcn_exp2f(a.stat[(i * a.n_rows + r) * 2] - most);
+        sum = over_waves(sum, false);
+        const float l2 = most + __log2f(sum);
+        if (lane == 0 && wave == 0) {
+            const int32_t t = loss_target(a.targets, a.target_bits, r, a.n_classes, a.status);
+            if (a.lse)
+                a.lse[r] = l2 * 0.693147181f;
+            if (a.loss)
+                a.loss[r] = t < 0 || sum == 0.f ? 0.f : (l2 - a.zt[r]) * 0.693147181f;
         }
-    for (uint32_t d = a.lanes; d < 64; d <<= 1)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            v[e] += __shfl_xor(v[e], d, 64);
-    if (W > 1) {
-        __syncthreads();
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            part[wave][lane * 4 + e] = v[e];
-        __syncthreads();
-        for (int w = 1; w < W; ++w)
+        if (!a.mean)
+            continue;
+        const int col = (lane % a.lanes) * 4;
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        if (col < a.pitch)
+            for (uint32_t i = lane / a.lanes + wave * (64 / a.lanes); i < a.n_split; i += 64 / a.lanes * W) {
+                const float f = __builtin_amdgcn_exp2f(a.stat[(i * a.n_rows + r) * 2] - most);
+                const float4 p = *(const float4 *)(a.part + (i * a.n_rows + r) * a.pitch + col);
+                v[0] += f * p.x;
+                v[1] += f * p.y;
+                v[2] += f * p.z;
+                v[3] += f * p.w;
+            }
+        for (uint32_t d = a.lanes; d < 64; d <<= 1)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                v[e] = (w == 1 ? part[0][lane * 4 + e] : v[e]) + part[w][lane * 4 + e];
-    }
-    if (lane < (int)a.lanes && wave == 0)
+                v[e] += __shfl_xor(v[e], d, 64);
+        if (W > 1) {
+            __syncthreads();
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (col + e < a.width)
-                a.mean[r * a.width + col + e] = sum == 0.f ? 0.f : v[e] / sum;
+            for (int e = 0; e < 4; ++e)
+                part[wave][lane * 4 + e] = v[e];
+            __syncthreads();
+            for (int w = 1; w < W; ++w)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    v[e] = (w == 1 ? part[0][lane * 4 + e] : v[e]) + part[w][lane * 4 + e];
+        }
+        if (lane < (int)a.lanes && wave == 0)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (col + e < a.width)
+                    a.mean[r * a.width + col + e] = sum == 0.f ? 0.f : v[e] / sum;
+    }
 }
 
 struct LossRows {
@@ -137,8 +137,8 @@ __device__ __forceinline__ float loss_most(float most, float v)
     return v < INFINITY ? fmaxf(most, v) : most;
 }
 
-// The largest value of all rows of fp32.  Bound by memory.
-__global__ __launch_bounds__(256) void loss_most_kernel(const float *w, int64_t stride, int64_t n, int32_t width, float *slots)
+// The largest value of all rows of fp32 (of classes that are offered).  Bound by memory.
+__global__ __launch_bounds__(256) void loss_most_kernel(const float *w, int64_t stride, int64_t n, int32_t width, const float *bias, float *slots)
 {
     float most = 0.f;
     const uint32_t per = ((uint32_t)width + 3) / 4, lanes = per <= 1 ? 1 : 1u << (32 - __clz(per - 1)); // lanes of a row, 4 values each
@@ -146,6 +146,8 @@ __global__ __launch_bounds__(256) void loss_most_kernel(const float *w, int64_t 
     fae_place<4> at;
     at.set((threadIdx.x % lanes) * 4, width);
     for (int64_t r = (int64_t)blockIdx.x * rows + threadIdx.x / lanes; r < n; r += (int64_t)gridDim.x * rows) {
+        if (bias && bias[r] * 1.44269504f == -INFINITY)
+            continue;
         const float *row = w + r * stride;
         if (width >= 4) {
             const auto v = *(const typename fae_vec<float, 4>::loose *)(row + at.from);
@@ -479,7 +481,7 @@ static int32_t loss_forward(fae_ctx *ctx, const fae_softmax_loss *l, const void 
         const int64_t groups = (l->n_classes + 63) / 64;
         a.st_most = most;
         a.n_most = (int32_t)(groups < LOSS_MOSTS ? groups : LOSS_MOSTS);
-        FAE_LAUNCH(ctx, loss_most_kernel, dim3(a.n_most), dim3(256), 0, ctx->stream, (const float *)w, w_stride, l->n_classes, l->width, most);
+        FAE_LAUNCH(ctx, loss_most_kernel, dim3(a.n_most), dim3(256), 0, ctx->stream, (const float *)w, w_stride, l->n_classes, l->width, l->bias, most);
         FAE_LAUNCH_CHECK(ctx);
     }
     {
@@ -512,7 +514,7 @@ static int32_t loss_forward(fae_ctx *ctx, const fae_softmax_loss *l, const void 
     else if (parts >= 16)
         FAE_LAUNCH(ctx, (loss_join_kernel<4>), dim3((uint32_t)l->n_rows), dim3(256), 0, ctx->stream, j);
     else
-        FAE_LAUNCH(ctx, (loss_join_kernel<1>), dim3((uint32_t)((l->n_rows + 3) / 4)), dim3(256), 0, ctx->stream, j);
+        FAE_LAUNCH(ctx, (loss_join_kernel<1>), dim3((uint32_t)((l->n_rows + 3) / 4 < LOSS_GRID ? (l->n_rows + 3) / 4 : LOSS_GRID)), dim3(256), 0, ctx->stream, j);
     FAE_LAUNCH_CHECK(ctx);
     return FAE_OK;
 }
@@ -586,7 +588,7 @@ extern "C" int32_t fae_softmax_loss_bwd(fae_ctx *ctx, const fae_softmax_loss *wh
     void *rest = cv.base + cv.used;
     const size_t rest_bytes = cv.cap - cv.used;
     const int64_t row_groups = (n + 3) / 4;
-    const int32_t n_most = (int32_t)(row_groups < LOSS_MOSTS || what->type == FAE_BF16 ? row_groups : LOSS_MOSTS);
+    const int32_t n_most = (int32_t)(row_groups < LOSS_MOSTS ? row_groups : what->type != FAE_BF16 ? LOSS_MOSTS : row_groups < LOSS_GRID ? row_groups : LOSS_GRID);
     if (n > 0) {
         if (gx && !mean) {
             rc = loss_forward(ctx, what, x, x_row_stride, w, w_row_stride, nullptr, nullptr, own_mean, rest, rest_bytes);

@@ -12,7 +12,7 @@ two units of 2^z and by the rounding of z - reference, which is below |z - lse| 
 A probability's relative error is e = dz + dlse + u (8 + 2 |z - lse|) (as a factor, exp(e) - 1).  Entering a product it is
 rounded to the type, by h of itself (fp32: 16 u as above); sums of M such terms take at most N M + 64 roundings of the
 sum of their absolute values.  A 16-bit result is off by half a step more.  fp16 probabilities have a smallest step: the
-largest is at least 2^9, and half a step is 2^-25: each is off by 2^-34 of the largest at most.  Of bf16 numbers, 2^z and the parts of a
+largest is at least 2^9 (with the gradients 2^14), and half a step is 2^-25: each is off by 2^-34 of the largest at most.  Of bf16 numbers, 2^z and the parts of a
 probability below fp32's smallest normal number, 2^-126, are lost: each is off by 2^-125 at most.
 
 Beside this worst case, fp32 results are held to what independent roundings add up to: one of at most 2 units per

@@ -370,3 +370,68 @@ def test_few_rows_and_what_they_may_meet(hp, n):
     loss, lse = hp.softmax_loss(x[rest], w, t[rest], bias, 0.5)
     assert bool((lse == -math.inf).all()) and not bool(loss.any())
     hp.sync()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n,with_mean", [(20, False), (20, True), (300, False), (300, True), (7000, True)])
+def test_classes_that_are_not_offered_may_hold_anything(hp, n, with_mean, dtype):
+    """Infinities, NaN and the type's largest value in masked places; a mask of fp32's lowest value is as good as one of infinity."""
+    v, d = 3000, 40
+    x, w, t, bias, g = _make(n, n, v, d, dtype, bias=True)
+    gone = torch.rand(v, device="cuda") < 0.3
+    gone[t.clamp(min=0).long()] = False
+    clean = w.clone()
+    clean[gone] = 0
+    bias[gone] = -math.inf
+
+    def calls(w, bias):
+        out = hp.softmax_loss(x, w, t, bias, 0.2, keep=with_mean)
+        return [*out, *hp.softmax_loss_backward(x, w, t, out[1], g, out[2] if with_mean else None, bias, 0.2)]
+    want = calls(clean, bias)
+    for fill in (math.nan, math.inf, torch.finfo(dtype).max):
+        w[gone] = fill
+        assert all(torch.equal(a, b) for a, b in zip(calls(w, bias), want))
+    assert all(torch.equal(a, b) for a, b in zip(calls(w, bias.clamp(min=torch.finfo(F32).min)), want))
+    hp.sync()
+
+
+def test_more_rows_than_threads_of_a_grid(hp):
+    """2^26 rows and more: kernels with a wave per row walk."""
+    n = (1 << 26) + 1000
+    x = torch.ones((n, 1), dtype=BF16, device="cuda")
+    x[-3:] = 2.0
+    w = torch.tensor([[0.5], [1.0], [-1.0]], dtype=BF16, device="cuda")
+    t = torch.zeros(n, dtype=torch.int32, device="cuda")
+    loss, lse, mean = hp.softmax_loss(x, w, t, keep=True)
+    gx, gw = hp.softmax_loss_backward(x, w, t, lse, torch.ones(n, device="cuda"), mean)
+    hp.sync()
+    for part, value in ((slice(0, n - 3), 1.0), (slice(n - 3, n), 2.0)):
+        z = [0.5 * value, value, -value]
+        total = math.log(sum(map(math.exp, z)))
+        p = [math.exp(s - total) for s in z]
+        for got, want, rel in ((lse, total, 1e-5), (loss, total - z[0], 1e-5), (gx, p[0] * 0.5 + p[1] - p[2] - 0.5, 2 ** -6)):
+            assert float((got[part].float() - want).abs().max()) <= rel * abs(want)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("size", [1e-30, 1e-3, 1e4, 1e18])
+def test_large_and_small_values(hp, size, dtype):
+    """Rows of any size whose scores are of the usual one: x size, w 1 / size."""
+    if dtype == F16 and not 1e-4 < size < 1e5:
+        pytest.skip("no numbers of fp16")
+    for n in (40, 200):
+        x, w, t, bias, g = _make(6, n, 100_000 if n == 200 else 500, 48, F32, bias=True)
+        x, w = (x * (size if dtype != F16 else 1.0)).to(dtype), (w / size if dtype != F16 else w * size / 100).to(dtype)
+        scale = 0.2 if dtype != F16 else 0.2 * 100 / size
+        ref = R.LossRef(x, w, t, bias, scale)
+        g = g * 1e-3
+        _check(hp, x, w, t, bias, g, scale, ref=ref)
+
+
+def test_values_of_different_sizes(hp):
+    """Some rows of the table 2^14 times the others, some columns 2^-12: what is far below the largest keeps its digits."""
+    x, w, t, bias, g = _make(9, 256, 70_000, 64, F32)
+    w[::7] *= 2.0 ** -14
+    w[:, 5] *= 2.0 ** -12
+    x[:, 9] *= 2.0 ** -10
+    _check(hp, x, w, t, None, g, 0.1)

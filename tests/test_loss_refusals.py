@@ -133,6 +133,7 @@ def test_gradients_arguments():
         assert call(fine, ws=0) == B.FAE_ENOSPC and call(fine, n=8) == B.FAE_ENOSPC
         assert call(fine, count=-1) == B.FAE_EINVAL and call(fine, count=B.FAE_MAX_GRADS + 1) == B.FAE_EINVAL
     assert _norm(fine, norm=0) == B.FAE_EINVAL
+    assert _norm(fine, norm=X + 8) == B.FAE_EINVAL and _norm(fine, ws=X) == B.FAE_EINVAL
     assert _clip(fine, most=-1.0) == B.FAE_EINVAL and _clip(fine, most=float("nan")) == B.FAE_EINVAL
     assert _clip([(X, 0, 5, 0)]) == B.FAE_EINVAL and _clip([(X, W + 2, 5, 0)]) == B.FAE_EINVAL
 
