@@ -173,24 +173,69 @@ template <int HOW> __device__ __forceinline__ void loss_split(const float (&v)[8
 template <typename T> struct loss_raw {
     T v[8];
 };
-template <typename T> __device__ __forceinline__ loss_raw<T> loss_load(const T *row, int col, int width, bool there)
+template <typename T> __device__ __forceinline__ loss_raw<T> loss_load_whole(const T *at)
 {
+    typedef typename fae_vec<T, 16 / sizeof(T)>::loose loose;
     loss_raw<T> o;
-    if (there && col + 8 <= width) {
-        typedef typename fae_vec<T, 16 / sizeof(T)>::loose loose;
 #pragma unroll
-        for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
-            const auto x = *(const loose *)(row + col + h * (16 / sizeof(T)));
+    for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
+        const auto x = *(const loose *)(at + h * (16 / sizeof(T)));
 #pragma unroll
-            for (int e = 0; e < (int)(16 / sizeof(T)); ++e)
-                o.v[h * (16 / sizeof(T)) + e] = x[e];
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            o.v[e] = there && col + e < width ? row[col + e] : (T)0.f;
+        for (int e = 0; e < (int)(16 / sizeof(T)); ++e)
+            o.v[h * (16 / sizeof(T)) + e] = x[e];
     }
     return o;
+}
+template <typename T> __device__ __forceinline__ loss_raw<T> loss_load(const T *row, int col, int width, bool there)
+{
+    if (there && col + 8 <= width)
+        return loss_load_whole(row + col);
+    loss_raw<T> o;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        o.v[e] = there && col + e < width ? row[col + e] : (T)0.f;
+    return o;
+}
+// the same with a row's end by four values first: for where few rows are missing
+template <typename T> __device__ __forceinline__ loss_raw<T> loss_load_ends(const T *row, int col, int width, bool there)
+{
+    if (there && col + 8 <= width)
+        return loss_load_whole(row + col);
+    loss_raw<T> o;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        o.v[e] = (T)0.f;
+    if (there && col < width) { // a row's end
+        const int left = width - col;
+        int done = 0;
+        if (left >= 4) {
+            const auto x = *(const typename fae_vec<T, 4>::loose *)(row + col);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                o.v[e] = x[e];
+            done = 4;
+        }
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (done + e < left) {
+                const T x = row[col + done + e];
+                if (done)
+                    o.v[4 + e] = x;
+                else
+                    o.v[e] = x;
+            }
+    }
+    return o;
+}
+// zeros instead, by whole words
+template <typename T> __device__ __forceinline__ loss_raw<T> loss_clear(const loss_raw<T> &x, bool clear)
+{
+    typedef uint32_t words __attribute__((ext_vector_type(sizeof(x) / 4)));
+    words w = __builtin_bit_cast(words, x);
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(x) / 4; ++i)
+        w[i] = clear ? 0u : w[i];
+    return __builtin_bit_cast(loss_raw<T>, w);
 }
 template <int HOW>
 __device__ __forceinline__ void loss_planes(const loss_raw<typename loss_type<HOW>::T> &x, float scale,
@@ -375,9 +420,7 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
             const int piece = i * THREADS + threadIdx.x, m = piece / (DP / 8), p = piece % (DP / 8);
             v8 o[P];
             if (MODE == LOSS_GRAD || BIAS) { // a row without a target, or a class that is not offered, may hold anything, and 0 times that is not always 0
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    next[i].v[e] = next_t[i] < 0 ? (T)0.f : next[i].v[e];
+                next[i] = loss_clear(next[i], next_t[i] < 0);
             }
             loss_planes<HOW>(next[i], st_scale, o);
 #pragma unroll
@@ -668,7 +711,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(loss_planes
         const int m = tl * 32 + ln;
 #pragma unroll
         for (int k = 0; k < KS; ++k)
-            next[k] = loss_load<T>((const T *)a.st + (int64_t)m * a.st_stride, k * 16 + half * 8, a.width, tl < tile1 && m < a.n_st);
+            next[k] = loss_load_ends<T>((const T *)a.st + (int64_t)m * a.st_stride, k * 16 + half * 8, a.width, tl < tile1 && m < a.n_st);
         next_gone = BIAS && tl < tile1 && m < a.n_st && a.bias[m] * 1.44269504f == -INFINITY; // such a class may hold anything
         if (BIAS && tl < tile1 && (tl + 1) * 32LL <= a.n_st)
 #pragma unroll
@@ -701,11 +744,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(loss_planes
         v8 x[KS][P];
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
-            if (BIAS) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    next[k].v[e] = next_gone ? (T)0.f : next[k].v[e];
-            }
+            if (BIAS)
+                next[k] = loss_clear(next[k], next_gone);
             loss_planes<HOW>(next[k], 1.f, x[k]);
         }
         float bias[16];
