@@ -55,10 +55,15 @@ constexpr int loss_blocks(int how, int dp, int mode)
 // (both take the scores: half of the matrix instructions are doubled, and still a step of 8192 x 32 768 x 256 bf16 takes 900 us instead of
 // 1130).
 constexpr int loss_shares(int how, int dp, int mode) { return mode != LOSS_STATS && dp > 128 ? 2 : 1; }
-// waves per SIMD that registers are left for: one where more than half of a SIMD's are needed
+// Waves per SIMD that registers are left for: three where 168 of them do (a few less than the compiler would take), one where 256 do not.
+// Two and three: loss of 16 384 x 131 072 x 64 bf16 512 and 447 us, the gradient of 2048 x 100 000 x 64 fp32 218 and 203; but with
+// spills (fp32 means of width 32) 870 and 1120.
 constexpr int loss_waves(int how, int dp, int mode)
 {
-    return how == LOSS_F32 && dp > 64 ? 1 : 2;
+    if (how == LOSS_F32)
+        return dp > 64 ? 1 : 2;
+    const bool three = dp <= 32 ? mode != LOSS_MEAN || how != LOSS_F32_WIDE : dp <= 64 && (mode == LOSS_STATS || how == LOSS_F32_WIDE);
+    return three ? 3 : 2;
 }
 #define LOSS_WAVES 4
 constexpr int loss_held(int how, int dp, int mode) { return LOSS_WAVES * 32 * loss_blocks(how, dp, mode); }

@@ -4,7 +4,7 @@
 #include "fae_loss.h"
 
 #define LOSS_ROUNDS 4   // workgroups of a launch that is shared out, in rounds of as many as the chip holds, at most
-#define LOSS_SLOTS 512  // workgroups that the chip holds: two for each compute unit
+#define LOSS_SLOTS 512  // workgroups that the chip holds with two waves per SIMD
 #define LOSS_MOST 0x7fff0000LL
 #define LOSS_GRID (1 << 20) // workgroups of a kernel over rows at most: a grid holds fewer than 2^32 threads
 #define LOSS_WIDE_ROWS 128
@@ -509,9 +509,9 @@ static int32_t loss_forward(fae_ctx *ctx, const fae_softmax_loss *l, const void 
         j.lanes *= 2;
     j.status = ctx->d_block;
     fae_ktimer kt(ctx, FAE_K_LOSS_JOIN);
-    if (parts >= 64 && l->n_rows <= 2048)
+    if (parts >= 256 && l->n_rows <= 2048)
         FAE_LAUNCH(ctx, (loss_join_kernel<16>), dim3((uint32_t)l->n_rows), dim3(1024), 0, ctx->stream, j);
-    else if (parts >= 16)
+    else if (parts >= 16 && l->n_rows <= 8192)
         FAE_LAUNCH(ctx, (loss_join_kernel<4>), dim3((uint32_t)l->n_rows), dim3(256), 0, ctx->stream, j);
     else
         FAE_LAUNCH(ctx, (loss_join_kernel<1>), dim3((uint32_t)((l->n_rows + 3) / 4 < LOSS_GRID ? (l->n_rows + 3) / 4 : LOSS_GRID)), dim3(256), 0, ctx->stream, j);
