@@ -395,7 +395,12 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
 
     // the next tile on its way from memory to LDS
     loss_raw<T> next[NC];
-    int32_t next_t[NC];
+    // A row without a target, or a class that is not offered, may hold anything, and 0 times that is not always 0: it is staged as zeros.  Which
+    // rows these are every wave finds with one load (forward of 4096 x 60 000 x 128 bf16 166 us instead of 202), or in the gradient every
+    // piece with its own (2 to 5 % faster there, but for the widest fp32 rows, whose registers are all taken: 1146 us instead of 847).
+    constexpr bool BY_PIECE = MODE == LOSS_GRAD && !(HOW == LOSS_F32_WIDE && DP > 192), BY_WAVE = (MODE == LOSS_GRAD || BIAS) && !BY_PIECE;
+    int32_t next_t[BY_PIECE ? NC : 1];
+    bool next_gone = false; // of row `lane` of the tile
     float next_side[3];
     auto fetch = [&](int tl) {
         const int m0 = tl * TM;
@@ -403,10 +408,12 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
         for (int i = 0; i < NC; ++i) {
             const int piece = i * THREADS + threadIdx.x, m = piece / (DP / 8), p = piece % (DP / 8);
             next[i] = loss_load<T>((const T *)a.st + (int64_t)(m0 + m) * a.st_stride, p * 8, a.width, m0 + m < a.n_st && (PIECES % THREADS == 0 || piece < PIECES));
-            if (MODE == LOSS_GRAD)
-                next_t[i] = m0 + m < a.n_st ? a.t[m0 + m] : -1;
-            else if (BIAS)
-                next_t[i] = m0 + m < a.n_st && a.bias[m0 + m] * 1.44269504f == -INFINITY ? -1 : 0;
+            if (BY_PIECE)
+                next_t[BY_PIECE ? i : 0] = m0 + m < a.n_st ? a.t[m0 + m] : -1;
+        }
+        if (BY_WAVE) {
+            const int m = m0 + (lane & (TM - 1));
+            next_gone = m < a.n_st && (MODE == LOSS_GRAD ? a.t[m] < 0 : a.bias[m] * 1.44269504f == -INFINITY);
         }
         if (threadIdx.x < TM) {
             const int m = m0 + threadIdx.x;
@@ -420,13 +427,15 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
         }
     };
     auto place = [&](int buf) {
+        const uint64_t gone = BY_WAVE ? __ballot(next_gone) : 0; // (tiles of 32: both halves alike)
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
             const int piece = i * THREADS + threadIdx.x, m = piece / (DP / 8), p = piece % (DP / 8);
             v8 o[P];
-            if (MODE == LOSS_GRAD || BIAS) { // a row without a target, or a class that is not offered, may hold anything, and 0 times that is not always 0
-                next[i] = loss_clear(next[i], next_t[i] < 0);
-            }
+            if (BY_PIECE)
+                next[i] = loss_clear(next[i], next_t[BY_PIECE ? i : 0] < 0);
+            else if (gone != 0)
+                next[i] = loss_clear(next[i], (gone >> m) & 1);
             loss_planes<HOW>(next[i], st_scale, o);
 #pragma unroll
             for (int k = 0; k < P; ++k)
