@@ -431,7 +431,8 @@ typedef struct {
 #define FAE_LOSS_MAX_WIDTH 256
 /* loss and lse: device fp32[n_rows], either may be NULL.  mean: NULL, or device fp32[n_rows * width], what a training step keeps
  * for its backward:
- *   mean[r] = sum over the classes v other than r's target of exp(z[r][v] - lse[r]) * w[v].
+ *   mean[r] = sum over the classes v other than r's target of exp(z[r][v] - lse[r]) * (w[v] - w[target[r]])
+ * (w[v] alone in a row without a target).
  * No output may share memory with another or with an input.  ws is on 16 bytes; its size does not fall with
  * n_rows or n_classes (one for the largest call is enough for the others), and calls that may overlap need one each.  Sums
  * are taken in an order that depends on the sizes alone.  Asynchronous. */

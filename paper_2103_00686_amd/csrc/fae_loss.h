@@ -5,7 +5,7 @@
 
 // Both directions stream rows past rows that a wave holds: Z = (streamed rows) x (held rows)^T by matrix instructions, P = a function of Z in
 // registers, O += (streamed rows)^T x P by matrix instructions.
-//   LOSS_STATS  held: x, streamed: w; reference and sum of 2^(Z - reference) for every row of x, and the target's Z
+//   LOSS_STATS  held: x, streamed: w; reference and sum of 2^(Z - reference) of all classes but the target for every row of x, and the target's Z
 //   LOSS_MEAN   the same, and O = the sum of 2^(Z - reference) w of all classes but the target
 //   LOSS_GRAD   held: w, streamed: x; P = gloss (2^(Z - lse) - (class is the target)), O = the sum of P x, and the sum of P (bias)
 // Z is in units of log 2 throughout.
@@ -44,6 +44,7 @@ struct loss_args {
 enum { LOSS_F32, LOSS_BF16, LOSS_F16, LOSS_F32_WIDE };
 constexpr int loss_planes_of(int how) { return how == LOSS_F32 ? 3 : how == LOSS_F32_WIDE ? 2 : 1; }
 static inline int loss_padded(int32_t width) { return width <= 32 ? 32 : width <= 64 ? 64 : width <= 96 ? 96 : width <= 128 ? 128 : width <= 192 ? 192 : 256; }
+#define LOSS_F32_WIDTH 64 // LOSS_F32 for wider rows is for few rows alone
 constexpr int loss_tile(int how, int dp) { return dp > 128 && loss_planes_of(how) > 1 ? 32 : 64; }
 // held rows of a wave, in blocks of 32: two where their registers leave room for two waves on a SIMD
 // held rows of a wave, in blocks of 32: two where their registers leave room for two waves on a SIMD
@@ -55,13 +56,13 @@ constexpr int loss_blocks(int how, int dp, int mode)
 // (both take the scores: half of the matrix instructions are doubled, and still a step of 8192 x 32 768 x 256 bf16 takes 900 us instead of
 // 1130).
 constexpr int loss_shares(int how, int dp, int mode) { return mode != LOSS_STATS && dp > 128 ? 2 : 1; }
-// Waves per SIMD that registers are left for: three where 168 of them do (a few less than the compiler would take), one where 256 do not.
+// Waves per SIMD that registers are left for: three where 168 of them do (a few less than the compiler would take), else two.
 // Two and three: loss of 16 384 x 131 072 x 64 bf16 512 and 447 us, the gradient of 2048 x 100 000 x 64 fp32 218 and 203; but with
 // spills (fp32 means of width 32) 870 and 1120.
 constexpr int loss_waves(int how, int dp, int mode)
 {
     if (how == LOSS_F32)
-        return dp > 64 ? 1 : 2;
+        return 2;
     const bool three = dp <= 32 ? mode != LOSS_MEAN || how != LOSS_F32_WIDE : dp <= 64 && (mode == LOSS_STATS || how == LOSS_F32_WIDE);
     return three ? 3 : 2;
 }
@@ -141,6 +142,18 @@ __device__ __forceinline__ loss_f16v loss_mfma(loss_vec<fae_bf16>::v8 a, loss_ve
 __device__ __forceinline__ loss_f16v loss_mfma(loss_vec<fae_f16>::v8 a, loss_vec<fae_f16>::v8 b, loss_f16v c)
 {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+
+// A step of a score.  Wide fp32 rows: the small products of planes go to a sum of their own, so that the large one is rounded once per 16
+// values and not three or six times (an addition per score more; 3863 x 132 x 224 2e-6 off without, 6e-7 with).
+template <int HOW, int KS> constexpr bool loss_apart() { return loss_type<HOW>::PLANES > 1 && KS > 4; }
+template <int HOW, int KS, typename V, int P> __device__ __forceinline__ void loss_score(const V (&x)[P], const V (&q)[P], loss_f16v &z, loss_f16v &less)
+{
+#pragma unroll
+    for (int u = 6 - loss_type<HOW>::PRODUCTS; u < 6; ++u) {
+        loss_f16v &to = loss_apart<HOW, KS>() && u < 5 ? less : z;
+        to = loss_mfma(x[LOSS_PA[u]], q[LOSS_PB[u]], to);
+    }
 }
 
 // eight fp32 values as planes, each rounded to nearest so that what is left has either sign
@@ -503,16 +516,19 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
             v8 x[NB > 1 ? KS : 1][P];
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
+                loss_f16v less = (loss_f16v)(0.f);
                 z[b] = (loss_f16v)(0.f);
 #pragma unroll
                 for (int k = 0; k < KS; ++k) {
                     v8(&xk)[P] = x[NB > 1 ? k : 0];
                     if (b == 0)
                         streamed(k, xk);
-#pragma unroll
-                    for (int u = 6 - NP; u < 6; ++u)
-                        z[b] = loss_mfma(xk[LOSS_PA[u]], q[b][k][LOSS_PB[u]], z[b]);
+                    loss_score<HOW, KS>(xk, q[b][k], z[b], less);
                 }
+                if (loss_apart<HOW, KS>())
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        z[b][i] += less[i];
             }
             float pr[NB][16];
             const float *sd = &side[buf][0][sb * 32 + half * 4];
@@ -602,10 +618,9 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
                 bool hit = false;
 #pragma unroll
                 for (int b = 0; b < NB; ++b) {
-                    sum[b] += some[b];
                     hit = hit || (unsigned)(target[b] - tl * TM - sb * 32) < 32u;
                 }
-                if (__any(hit)) { // the target's score, and no part of it in the mean
+                if (__any(hit)) { // the target's score goes out by itself; it has no part in sum and mean
 #pragma unroll
                     for (int b = 0; b < NB; ++b) {
                         const int at = target[b] - tl * TM - sb * 32;
@@ -616,8 +631,15 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
                                     a.zt[first + b * 32 + ln] = fmaf(z[b][i], c[b], sd[i / 4 * 8 + i % 4]);
                                 pr[b][i] = 0.f;
                             }
+                        some[b] = 0.f;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            some[b] += pr[b][i];
                     }
                 }
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+                    sum[b] += some[b];
             }
             if (HAS_O) {
                 // eight streamed rows of a lane are the eight of an operand: rows 16 t + 4 half + {0..3, 8..11}
@@ -710,7 +732,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(loss_planes
     typedef loss_type<HOW> H;
     typedef typename H::T T;
     typedef typename loss_vec<typename H::E>::v8 v8;
-    constexpr int P = H::PLANES, NP = H::PRODUCTS, KS = DP / 16;
+    constexpr int P = H::PLANES, KS = DP / 16;
     __shared__ float parts[4][2][NB * 32];
     const int lane = fae_lane(), wave = threadIdx.x / 64, ln = lane & 31, half = lane >> 5;
     const uint32_t split = blockIdx.x / a.n_blocks, block = blockIdx.x % a.n_blocks;
@@ -777,12 +799,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(loss_planes
         fetch(tl + 1);
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-            loss_f16v z = (loss_f16v)(0.f);
+            loss_f16v z = (loss_f16v)(0.f), less = (loss_f16v)(0.f);
 #pragma unroll
             for (int k = 0; k < KS; ++k)
+                loss_score<HOW, KS>(x[k], q[b][k], z, less);
+            if (loss_apart<HOW, KS>())
 #pragma unroll
-                for (int u = 6 - NP; u < 6; ++u)
-                    z = loss_mfma(x[k][LOSS_PA[u]], q[b][k][LOSS_PB[u]], z);
+                for (int i = 0; i < 16; ++i)
+                    z[i] += less[i];
             float some;
             auto powers = [&]() {
                 some = 0.f;
@@ -802,14 +826,19 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(loss_planes
                 ref[b] = to;
                 powers();
             }
-            sum[b] += some;
             const int at = target[b] - tl * 32;
-            if (__any((unsigned)at < 32u)) {
+            if (__any((unsigned)at < 32u)) { // the target's score goes out by itself
+                some = 0.f;
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
+                for (int i = 0; i < 16; ++i) {
+                    const float v = fmaf(z[i], a.c, bias[i]);
                     if (8 * (i / 4) + 4 * half + i % 4 == at)
-                        a.zt[first + b * 32 + ln] = fmaf(z[i], a.c, bias[i]);
+                        a.zt[first + b * 32 + ln] = v;
+                    else
+                        some += __builtin_amdgcn_exp2f(fmaf(z[i], a.c, bias[i] - ref[b]));
+                }
             }
+            sum[b] += some;
         }
     }
     // the two halves of a wave, then the four waves, at the largest reference
@@ -851,12 +880,14 @@ template <int HOW, int DP, bool BIAS> static void loss_launch_mode(fae_ctx *ctx,
             return;
         }
     }
-    if (mode == LOSS_STATS)
-        FAE_LAUNCH(ctx, (loss_kernel<HOW, DP, LOSS_STATS, BIAS>), grid, block, 0, ctx->stream, a);
-    else if (mode == LOSS_MEAN)
-        FAE_LAUNCH(ctx, (loss_kernel<HOW, DP, LOSS_MEAN, BIAS>), grid, block_o, 0, ctx->stream, a);
-    else
-        FAE_LAUNCH(ctx, (loss_kernel<HOW, DP, LOSS_GRAD, BIAS>), grid, block_o, 0, ctx->stream, a);
+    if constexpr (HOW != LOSS_F32 || DP <= LOSS_F32_WIDTH) {
+        if (mode == LOSS_STATS)
+            FAE_LAUNCH(ctx, (loss_kernel<HOW, DP, LOSS_STATS, BIAS>), grid, block, 0, ctx->stream, a);
+        else if (mode == LOSS_MEAN)
+            FAE_LAUNCH(ctx, (loss_kernel<HOW, DP, LOSS_MEAN, BIAS>), grid, block_o, 0, ctx->stream, a);
+        else if constexpr (HOW != LOSS_F32)
+            FAE_LAUNCH(ctx, (loss_kernel<HOW, DP, LOSS_GRAD, BIAS>), grid, block_o, 0, ctx->stream, a);
+    }
 }
 template <int HOW, int DP> static void loss_launch_bias(fae_ctx *ctx, int mode, const loss_args &a)
 {

@@ -9,20 +9,26 @@
 #define LOSS_GRID (1 << 20) // workgroups of a kernel over rows at most: a grid holds fewer than 2^32 threads
 #define LOSS_WIDE_ROWS 128
 #define LOSS_WIDE_SCORES (1LL << 24)
-#define LOSS_WIDE_VALUES (1LL << 22)
 
 // ---------------------------------------------------------------------------------
 // kernels
 // ---------------------------------------------------------------------------------
 struct LossJoin {
     const float *stat, *zt, *part;
-    const void *targets;
+    const void *targets, *w;
+    int64_t w_stride;
+    int32_t type;
     float *loss, *lse, *mean;
     int32_t target_bits, n_classes, width, pitch;
     int64_t n_rows;
     uint32_t n_split, lanes; // lanes: of a part's row, a power of two
     uint32_t *status;
 };
+
+__device__ __forceinline__ float loss_value(const void *p, int32_t type, int64_t i)
+{
+    return type == FAE_F32 ? ((const float *)p)[i] : type == FAE_BF16 ? (float)((const fae_bf16 *)p)[i] : (float)((const fae_f16 *)p)[i];
+}
 
 // W waves per row: the parts' sums at one reference, loss and lse, and the weighted sum of the parts' means.  One wave is a chain of as many
 // loads as there are parts: 12 rows in 1024 parts take 180 us with one wave each,
@@ -57,13 +63,15 @@ template <int W> __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void loss_j
         for (uint32_t i = wave * 64 + lane; i < a.n_split; i += W * 64)
             sum += a.stat[(i * a.n_rows + r) * 2 + 1] * __builtin_amdgcn_exp2f(a.stat[(i * a.n_rows + r) * 2] - most);
         sum = over_waves(sum, false);
-        const float l2 = most + __log2f(sum);
+        // All classes but the target are in sum: what a confident row leaves to them keeps its digits.
+        const int32_t t = loss_target(a.targets, a.target_bits, r, a.n_classes, a.status);
+        const float zt = t < 0 ? -INFINITY : a.zt[r], pt = t < 0 ? 0.f : __builtin_amdgcn_exp2f(zt - most), all = sum + pt;
+        const float l2 = most + __log2f(all);
         if (lane == 0 && wave == 0) {
-            const int32_t t = loss_target(a.targets, a.target_bits, r, a.n_classes, a.status);
             if (a.lse)
                 a.lse[r] = l2 * 0.693147181f;
             if (a.loss)
-                a.loss[r] = t < 0 || sum == 0.f ? 0.f : (l2 - a.zt[r]) * 0.693147181f;
+                a.loss[r] = t < 0 || all == 0.f ? 0.f : sum < pt ? log1pf(sum / pt) : (l2 - zt) * 0.693147181f;
         }
         if (!a.mean)
             continue;
@@ -96,16 +104,18 @@ template <int W> __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void loss_j
         if (lane < (int)a.lanes && wave == 0)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                if (col + e < a.width)
-                    a.mean[r * a.width + col + e] = sum == 0.f ? 0.f : v[e] / sum;
+                if (col + e < a.width) {
+                    const float wt = t < 0 || sum == 0.f ? 0.f : loss_value(a.w, a.type, t * a.w_stride + col + e);
+                    a.mean[r * a.width + col + e] = all == 0.f ? 0.f : (v[e] - sum * wt) / all;
+                }
     }
 }
 
 struct LossRows {
-    const void *x, *w, *targets;
+    const void *x, *targets;
     void *gx;
-    int64_t x_stride, w_stride, gx_stride, n_rows;
-    const float *bias, *lse, *mean, *gloss;
+    int64_t x_stride, gx_stride, n_rows;
+    const float *lse, *mean, *gloss;
     float *nlse, *g;
     int32_t *t;
     float *g_most, *x_most; // a value for every workgroup
@@ -161,8 +171,7 @@ __global__ __launch_bounds__(256) void loss_most_kernel(const float *w, int64_t 
     loss_most_of(most, slots + blockIdx.x);
 }
 
-// A wave per row: gx from the mean of the other classes' rows and the target's own, whose share p - 1 is taken without the cancellation of a
-// confident row; and what the classes' gradient reads of every row.
+// A wave per row: gx from what the forward has kept, and what the classes' gradient reads of every row.
 template <typename T> __global__ __launch_bounds__(256) void loss_rows_kernel(LossRows a)
 {
     const int lane = fae_lane();
@@ -179,31 +188,11 @@ template <typename T> __global__ __launch_bounds__(256) void loss_rows_kernel(Lo
             a.g[r] = g;
             a.t[r] = t;
         }
-        if (!a.gx && !a.x_most)
-            continue;
-        const T *x = (const T *)a.x + r * a.x_stride, *w = (const T *)a.w + t * a.w_stride;
-        float wv[4], dot = 0.f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int c = lane + j * 64;
-            const bool in = t >= 0 && c < a.width;
-            const float xv = in ? (float)x[c] : 0.f;
-            wv[j] = in && a.gx ? (float)w[c] : 0.f;
-            x_most = loss_most(x_most, xv);
-            dot += wv[j] * xv;
-        }
-        if (!a.gx)
-            continue;
-        T *gx = (T *)a.gx + r * a.gx_stride;
-#pragma unroll
-        for (int d = 32; d > 0; d >>= 1)
-            dot += __shfl_xor(dot, d, 64);
-        const float share = t < 0 ? 0.f : expm1f(dot * a.scale + (a.bias ? a.bias[t] : 0.f) - lse);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int c = lane + j * 64;
-            if (c < a.width)
-                gx[c] = (T)(t < 0 ? 0.f : a.scale * g * (a.mean[r * a.width + c] + share * wv[j]));
+        for (int c = lane; c < a.width; c += 64) {
+            if (a.x_most && t >= 0)
+                x_most = loss_most(x_most, (float)((const T *)a.x)[r * a.x_stride + c]);
+            if (a.gx)
+                ((T *)a.gx)[r * a.gx_stride + c] = (T)(t < 0 ? 0.f : a.scale * g * a.mean[r * a.width + c]);
         }
     }
     if (a.g_most)
@@ -264,14 +253,15 @@ static bool loss_sizes_fit(const fae_softmax_loss *l)
 }
 
 // fp32 as two fp16 numbers or three bf16: the first take half the matrix instructions and fewer registers, and a look at all streamed rows
-// before (5 us and reading them).  Steps in us, two fp16 numbers and three bf16: 40 x 300 000 x 100 216 and 269, 1 x 1 000 000 x 32 equal,
-// 300 x 5003 x 16 41 and 39, 2048 x 1 000 000 x 32 1730 and 2860.
+// before (5 us and reading them), which few rows or scores of narrow rows do not pay for.  Steps in us, two fp16 numbers and three bf16:
+// 40 x 300 000 x 100 216 and 269, 1 x 1 000 000 x 32 equal, 300 x 5003 x 16 41 and 39, 2048 x 1 000 000 x 32 1730 and 2860.
 static int loss_how(const fae_softmax_loss *l, int mode)
 {
     if (l->type != FAE_F32)
         return l->type == FAE_BF16 ? LOSS_BF16 : LOSS_F16;
-    const bool pays = (l->n_rows >= LOSS_WIDE_ROWS && l->n_rows * l->n_classes >= LOSS_WIDE_SCORES) ||
-                      (mode == LOSS_MEAN && l->width > 64 && l->n_classes * l->width >= LOSS_WIDE_VALUES);
+    if (mode == LOSS_FEW)
+        return LOSS_F32;
+    const bool pays = l->width > LOSS_F32_WIDTH || (l->n_rows >= LOSS_WIDE_ROWS && l->n_rows * l->n_classes >= LOSS_WIDE_SCORES);
     return mode == LOSS_GRAD || pays ? LOSS_F32_WIDE : LOSS_F32;
 }
 
@@ -493,6 +483,9 @@ static int32_t loss_forward(fae_ctx *ctx, const fae_softmax_loss *l, const void 
     memset(&j, 0, sizeof(j));
     j.stat = a.stat;
     j.zt = a.zt;
+    j.w = w;
+    j.w_stride = w_stride;
+    j.type = l->type;
     j.part = a.part;
     j.targets = l->targets;
     j.loss = loss;
@@ -597,14 +590,11 @@ extern "C" int32_t fae_softmax_loss_bwd(fae_ctx *ctx, const fae_softmax_loss *wh
             mean = own_mean;
         }
         r.x = x;
-        r.w = w;
         r.targets = what->targets;
         r.gx = gx;
         r.x_stride = x_row_stride;
-        r.w_stride = w_row_stride;
         r.gx_stride = gx_row_stride;
         r.n_rows = n;
-        r.bias = what->bias;
         r.lse = lse;
         r.mean = mean;
         r.gloss = gloss;

@@ -75,9 +75,11 @@ class LossRef:
 
     def mean(self):
         others = self.p * (1 - self.hot * self.known[:, None])
-        ref = others @ self.w
-        err = (others * (self.e + self.h)) @ self.w.abs() + U * (self.N * self.v + 64) * (others @ self.w.abs()) + self.tiny * self.w.abs().sum(0) + self.mw
-        return ref, err
+        wt = self.w[self.t] * self.known[:, None]
+        ref = others @ self.w - others.sum(1)[:, None] * wt
+        both = others @ self.w.abs() + others.sum(1)[:, None] * wt.abs()
+        err = (others * (self.e + self.h)) @ self.w.abs() + (others * self.e).sum(1)[:, None] * wt.abs()
+        return ref, err + U * (self.N * self.v + 64) * both + self.tiny * (self.w.abs().sum(0) + self.v * wt.abs()) + self.mw
 
     def backward(self, gloss, out_dtype=None):
         """((gx, its bound, terms, instructions), the same of gw, (gbias, its bound))"""
