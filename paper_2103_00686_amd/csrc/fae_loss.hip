@@ -211,36 +211,63 @@ struct LossClasses {
     float scale;
 };
 
-// A thread per four values of a class: the sum of the parts, in their order.
-template <typename T> __global__ __launch_bounds__(256) void loss_classes_kernel(LossClasses a)
+// G threads per four values of a class, each with every G-th part: the sum of the parts.  One thread is a chain of as many loads as there are
+// parts: 300 classes of 64 in 188 parts take 55 us with one, 8 with 16.
+template <typename T, int G> __global__ __launch_bounds__(256) void loss_classes_kernel(LossClasses a)
 {
-    const int per = a.pitch / 4;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, n = i / per;
+    constexpr int OUT = 256 / G;
+    __shared__ float some[G][OUT][5];
+    const int per = a.pitch / 4, out = threadIdx.x % OUT, group = threadIdx.x / OUT;
+    const int64_t i = (int64_t)blockIdx.x * OUT + out, n = i / per;
     const int col = (int)(i - n * per) * 4;
+    float v[5] = {0.f, 0.f, 0.f, 0.f, 0.f}; // four values, and the bias's sum with the first of a class
+    if (n < a.n_classes) {
+        if (a.gw)
+#pragma unroll 4
+            for (uint32_t s = group; s < a.n_split; s += G) {
+                const float4 p = *(const float4 *)(a.part + (s * a.n_classes + n) * a.pitch + col);
+                v[0] += p.x;
+                v[1] += p.y;
+                v[2] += p.z;
+                v[3] += p.w;
+            }
+        if (a.gbias && col == 0)
+            for (uint32_t s = group; s < a.n_split; s += G)
+                v[4] += a.psum[s * a.n_classes + n];
+    }
+    if (G > 1) {
+#pragma unroll
+        for (int e = 0; e < 5; ++e)
+            some[group][out][e] = v[e];
+        __syncthreads();
+        if (group != 0)
+            return;
+        for (int g = 1; g < G; ++g)
+#pragma unroll
+            for (int e = 0; e < 5; ++e)
+                v[e] += some[g][out][e];
+    }
     if (n >= a.n_classes)
         return;
     if (a.gw) {
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
-        for (uint32_t s = 0; s < a.n_split; ++s) {
-            const float4 p = *(const float4 *)(a.part + (s * a.n_classes + n) * a.pitch + col);
-            v[0] += p.x;
-            v[1] += p.y;
-            v[2] += p.z;
-            v[3] += p.w;
-        }
+        float o[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            v[e] *= a.scale;
+            o[e] = v[e] * a.scale;
         fae_place<4> p;
         p.set(col, a.width);
-        fae_store<T, 4, FAE_ANY>((T *)a.gw + n * a.gw_stride, v, p);
+        fae_store<T, 4, FAE_ANY>((T *)a.gw + n * a.gw_stride, o, p);
     }
-    if (a.gbias && col == 0) {
-        float v = 0.f;
-        for (uint32_t s = 0; s < a.n_split; ++s)
-            v += a.psum[s * a.n_classes + n];
-        a.gbias[n] = v;
-    }
+    if (a.gbias && col == 0)
+        a.gbias[n] = v[4];
+}
+template <typename T> static void loss_classes(fae_ctx *ctx, const LossClasses &c)
+{
+    const int64_t n = c.n_classes * (c.pitch / 4);
+    if (c.n_split >= 32)
+        FAE_LAUNCH(ctx, (loss_classes_kernel<T, 16>), dim3((uint32_t)((n + 15) / 16)), dim3(256), 0, ctx->stream, c);
+    else
+        FAE_LAUNCH(ctx, (loss_classes_kernel<T, 1>), dim3((uint32_t)((n + 255) / 256)), dim3(256), 0, ctx->stream, c);
 }
 
 // ---------------------------------------------------------------------------------
@@ -663,13 +690,12 @@ extern "C" int32_t fae_softmax_loss_bwd(fae_ctx *ctx, const fae_softmax_loss *wh
         c.pitch = s.pitch;
         c.scale = what->scale;
         fae_ktimer kt(ctx, FAE_K_LOSS_JOIN);
-        const dim3 grid((uint32_t)((v * (s.pitch / 4) + 255) / 256)), block(256);
         if (what->type == FAE_F32)
-            FAE_LAUNCH(ctx, loss_classes_kernel<float>, grid, block, 0, ctx->stream, c);
+            loss_classes<float>(ctx, c);
         else if (what->type == FAE_BF16)
-            FAE_LAUNCH(ctx, loss_classes_kernel<fae_bf16>, grid, block, 0, ctx->stream, c);
+            loss_classes<fae_bf16>(ctx, c);
         else
-            FAE_LAUNCH(ctx, loss_classes_kernel<fae_f16>, grid, block, 0, ctx->stream, c);
+            loss_classes<fae_f16>(ctx, c);
         FAE_LAUNCH_CHECK(ctx);
     }
     return FAE_OK;
