@@ -506,7 +506,7 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
                 continue;
             // Z: element i is streamed row 8 (i / 4) + 4 half + i % 4 and held row ln.  One held block after the other: a matrix instruction that
             // waits for the one before leaves the vector unit to the SIMD's other waves, one that waits for the matrix unit does not
-            // (24 of them beside 200 vector instructions: 503 ns in one chain, 577 in two).
+            // (24 of them, then 200 vector instructions: 515 ns in one chain and 577 in two at two waves per SIMD, 503 and 544 at four).
             loss_f16v z[NB];
             auto streamed = [&](int k, v8 (&x)[P]) {
 #pragma unroll
@@ -724,8 +724,8 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
 
 // Few rows (serving, small test batches): bound by reading w, so that every wave takes a stretch of classes of its own, straight from memory to the
 // matrix instructions' registers with the next 32 on their way, and no wave waits for another before the end.  1 x 200 003 x 64 fp32
-// 16.8 us, 48 x 1 000 003 x 32 41 us, 3.1 TB/s (the kernel above: 25 and 106, three of its waves without rows).  Two steps ahead: 17.4 and
-// 43.6; three waves per SIMD, which spill: 20.5 and 46.6.
+// 14 to 16 us, 48 x 1 000 003 x 32 47 us, 2.7 TB/s.  When it was built it took 16.8 and 41 (the kernel above: 25 and 106, three of its waves
+// without rows; two steps ahead: 17.4 and 43.6; three waves per SIMD, which spill: 20.5 and 46.6).
 template <int HOW, int DP, int NB, bool BIAS>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(loss_planes_of(HOW) * DP <= 192 ? 2 : 1))) void loss_few_kernel(loss_args a)
 {

@@ -31,8 +31,7 @@ __device__ __forceinline__ float loss_value(const void *p, int32_t type, int64_t
 }
 
 // W waves per row: the parts' sums at one reference, loss and lse, and the weighted sum of the parts' means.  One wave is a chain of as many
-// loads as there are parts: 12 rows in 1024 parts take 180 us with one wave each,
-// 15 with 16.
+// loads as there are parts: the small kernels of a step of 12 x 100 000 x 64 bf16 take 191 us together with one, 22 with 16.
 template <int W> __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void loss_join_kernel(LossJoin a)
 {
     __shared__ float part[W][64 * 4];
@@ -212,7 +211,7 @@ struct LossClasses {
 };
 
 // G threads per four values of a class, each with every G-th part: the sum of the parts.  One thread is a chain of as many loads as there are
-// parts: 300 classes of 64 in 188 parts take 55 us with one, 8 with 16.
+// parts: the small kernels of a step of 12 000 x 300 x 64 bf16 take 66 us together with one, 22 with 16.
 template <typename T, int G> __global__ __launch_bounds__(256) void loss_classes_kernel(LossClasses a)
 {
     constexpr int OUT = 256 / G;
