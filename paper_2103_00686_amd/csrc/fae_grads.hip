@@ -200,7 +200,8 @@ __global__ __launch_bounds__(256) void grads_clip_kernel(GradsArgs a)
     if (a.norm && blockIdx.x == 0 && threadIdx.x == 0)
         *a.norm = (float)norm;
     // a factor below fp32's normal range (gradients of 1e38) would lose its digits: it is taken as two then
-    const double f = norm <= a.max_norm ? a.scale : a.max_norm / norm * a.scale;
+    // (an infinite norm is not below an infinite limit: 0, as under any other)
+    const double f = norm < INFINITY && norm <= a.max_norm ? a.scale : (norm == INFINITY ? 0.0 : a.max_norm / norm) * a.scale;
     const bool tiny = fabs(f) < 0x1p-100;
     const float f0 = tiny ? 0x1p-64f : 1.f, f1 = (float)(tiny ? f * 0x1p64 : f);
     GradsWalk w, n;
