@@ -6,6 +6,7 @@
 // Both directions stream rows past rows that a wave holds: Z = (streamed rows) x (held rows)^T by matrix instructions, P = a function of Z in
 // registers, O += (streamed rows)^T x P by matrix instructions.
 //   LOSS_STATS  held: x, streamed: w; reference and sum of 2^(Z - reference) of all classes but the target for every row of x, and the target's Z
+//               (the reference is one of the others too: the target's may lie far above)
 //   LOSS_MEAN   the same, and O = the sum of 2^(Z - reference) w of all classes but the target
 //   LOSS_GRAD   held: w, streamed: x; P = gloss (2^(Z - lse) - (class is the target)), O = the sum of P x, and the sum of P (bias)
 // Z is in units of log 2 throughout.
@@ -393,6 +394,7 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
             scale = __builtin_amdgcn_ldexpf(scale, up);
             c[b] = __builtin_amdgcn_ldexpf(c_all, -up);
         }
+        c[b] = fmaxf(c[b], 0x1p-149f); // a scale of 0: no score is off by more than 2^-21, and minus infinity stays what it is
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
             loss_raw<T> x = loss_load<T>(row, k * 16 + half * 8, a.width, there);
@@ -561,6 +563,26 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
                 for (int b = 0; b < NB; ++b)
                     sum[b] += loss_sum(pr[b]);
             } else {
+                // The target's score goes out by itself, and is minus infinity from here on (c is never 0).  It has no part in sum and mean, nor in
+                // the reference: 2^10 above the others' largest, as in a row that is sure of its target, it would leave their powers
+                // fewer fp16 bits, and none from 2^35 on.
+                bool hit = false;
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+                    hit = hit || (unsigned)(target[b] - tl * TM - sb * 32) < 32u;
+                if (__any(hit)) {
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) {
+                        const int at = target[b] - tl * TM - sb * 32;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (8 * (i / 4) + 4 * half + i % 4 == at) {
+                                if (share == 0)
+                                    a.zt[first + b * 32 + ln] = fmaf(z[b][i], c[b], sd[i / 4 * 8 + i % 4]);
+                                z[b][i] = -INFINITY;
+                            }
+                    }
+                }
                 float some[NB];
                 auto powers = [&](int b) {
                     const float off = ref[b] - (float)H::SHIFT;
@@ -613,28 +635,6 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
                                     o[b][d][i] *= f;
                         }
                         powers(b);
-                    }
-                }
-                bool hit = false;
-#pragma unroll
-                for (int b = 0; b < NB; ++b) {
-                    hit = hit || (unsigned)(target[b] - tl * TM - sb * 32) < 32u;
-                }
-                if (__any(hit)) { // the target's score goes out by itself; it has no part in sum and mean
-#pragma unroll
-                    for (int b = 0; b < NB; ++b) {
-                        const int at = target[b] - tl * TM - sb * 32;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            if (8 * (i / 4) + 4 * half + i % 4 == at) {
-                                if (share == 0)
-                                    a.zt[first + b * 32 + ln] = fmaf(z[b][i], c[b], sd[i / 4 * 8 + i % 4]);
-                                pr[b][i] = 0.f;
-                            }
-                        some[b] = 0.f;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            some[b] += pr[b][i];
                     }
                 }
 #pragma unroll

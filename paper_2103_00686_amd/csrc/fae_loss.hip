@@ -58,13 +58,15 @@ template <int W> __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void loss_j
         for (uint32_t i = wave * 64 + lane; i < a.n_split; i += W * 64)
             most = fmaxf(most, a.stat[(i * a.n_rows + r) * 2]);
         most = over_waves(most, true);
+        const int32_t t = loss_target(a.targets, a.target_bits, r, a.n_classes, a.status);
+        const float zt = t < 0 ? -INFINITY : a.zt[r];
+        most = fmaxf(most, zt); // the parts' references are the other classes'
         float sum = 0.f;
         for (uint32_t i = wave * 64 + lane; i < a.n_split; i += W * 64)
             sum += a.stat[(i * a.n_rows + r) * 2 + 1] * __builtin_amdgcn_exp2f(a.stat[(i * a.n_rows + r) * 2] - most);
         sum = over_waves(sum, false);
         // All classes but the target are in sum: what a confident row leaves to them keeps its digits.
-        const int32_t t = loss_target(a.targets, a.target_bits, r, a.n_classes, a.status);
-        const float zt = t < 0 ? -INFINITY : a.zt[r], pt = t < 0 ? 0.f : __builtin_amdgcn_exp2f(zt - most), all = sum + pt;
+        const float pt = t < 0 ? 0.f : __builtin_amdgcn_exp2f(zt - most), all = sum + pt;
         const float l2 = most + __log2f(all);
         if (lane == 0 && wave == 0) {
             if (a.lse)
