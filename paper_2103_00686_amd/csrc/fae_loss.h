@@ -7,7 +7,7 @@
 // registers, O += (streamed rows)^T x P by matrix instructions.
 //   LOSS_STATS  held: x, streamed: w; reference and sum of 2^(Z - reference) of all classes but the target for every row of x, and the target's Z
 //               (the reference is one of the others too: the target's may lie far above)
-//   LOSS_MEAN   the same, and O = the sum of 2^(Z - reference) w of all classes but the target
+//   LOSS_MEAN   the same, and O = the sum of 2^(Z - reference) w of all classes but the target; of 16-bit types also the sum of P as rounded for O
 //   LOSS_GRAD   held: w, streamed: x; P = gloss (2^(Z - lse) - (class is the target)), O = the sum of P x, and the sum of P (bias)
 // Z is in units of log 2 throughout.
 //   LOSS_FEW    what LOSS_STATS finds, for few rows
@@ -31,7 +31,7 @@ struct loss_args {
     float *stat; // forward: [n_split][n_own][2]: reference, sum of 2^(Z - reference)
     float *zt;   // forward: [n_own] Z of the target
     float *part; // [n_split][n_own][pitch] O
-    float *psum; // gradient: [n_split][n_own] sums of P, or NULL
+    float *psum; // [n_split][n_own]: gradient, sums of P, or NULL; means of 16-bit types, sums of P as it entered O
     void *out;   // gradient, one split: gw
     int64_t out_stride;
     float *out_sum; // ... and gbias or NULL
@@ -256,6 +256,24 @@ template <typename T> __device__ __forceinline__ loss_raw<T> loss_clear(const lo
         w[i] = clear ? 0u : w[i];
     return __builtin_bit_cast(loss_raw<T>, w);
 }
+// a sum, and eight probabilities as they enter a product
+__device__ __forceinline__ float loss_add(const loss_vec<fae_bf16>::v8 &p, float s)
+{
+    typedef fae_bf16 two __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int e = 0; e < 8; e += 2)
+        s = __builtin_amdgcn_fdot2_f32_bf16(two{p[e], p[e + 1]}, two{(fae_bf16)1.f, (fae_bf16)1.f}, s, false);
+    return s;
+}
+__device__ __forceinline__ float loss_add(const loss_vec<fae_f16>::v8 &p, float s)
+{
+    typedef fae_f16 two __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int e = 0; e < 8; e += 2)
+        s = __builtin_amdgcn_fdot2(two{p[e], p[e + 1]}, two{(fae_f16)1.f, (fae_f16)1.f}, s, false);
+    return s;
+}
+
 template <int HOW>
 __device__ __forceinline__ void loss_planes(const loss_raw<typename loss_type<HOW>::T> &x, float scale,
                                             typename loss_vec<typename loss_type<HOW>::E>::v8 (&o)[loss_type<HOW>::PLANES])
@@ -313,7 +331,7 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
     constexpr int SHARES = loss_shares(HOW, DP, MODE), THREADS = LOSS_WAVES * 64 * SHARES;
     constexpr int KS = DP / 16, DS = DP / 32 / SHARES, PIECES = TM * DP / 8, NC = (PIECES + THREADS - 1) / THREADS;
     constexpr int PLANE = TM * DP * 2, TILE = P * PLANE; // bytes
-    constexpr bool HAS_O = MODE != LOSS_STATS;
+    constexpr bool HAS_O = MODE != LOSS_STATS, ROUNDED = MODE == LOSS_MEAN && P == 1;
     __shared__ __attribute__((aligned(16))) char tiles[2 * TILE];
     __shared__ float side[2][3][TM]; // forward: bias; gradient: -lse + log |gloss|, gloss, target
     __shared__ float mosts[2][LOSS_WAVES * SHARES];
@@ -482,14 +500,14 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
 
     loss_f16v o[NB][HAS_O ? DS : 1];
     // Forward: 2^(Z - ref) is what is summed.  Gradient: sum is that of P.
-    float ref[NB], sum[NB];
+    float ref[NB], sum[NB], rounded[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
 #pragma unroll
         for (int d = 0; d < (HAS_O ? DS : 1); ++d)
             o[b][d] = (loss_f16v)(0.f);
         ref[b] = -3.402823466e38f;
-        sum[b] = 0.f;
+        sum[b] = rounded[b] = 0.f;
     }
     if (tile0 < tile1) {
         fetch(tile0);
@@ -627,6 +645,7 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
                         const float f = __builtin_amdgcn_exp2f(ref[b] - to);
                         ref[b] = to;
                         sum[b] *= f;
+                        rounded[b] *= f;
                         if (HAS_O) {
 #pragma unroll
                             for (int d = 0; d < DS; ++d)
@@ -654,6 +673,15 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
                             v[e] = pr[b][t * 8 + e];
                         loss_split<HOW>(v, pb[b][t]);
                     }
+                // P loses up to half a step of its type here: O is then divided by the sum of what P has become, so that what all rows have in common
+                // stays (dot products with ones: 30 us of the 1130 of a step of 16 384 x 100 003 x 64 bf16).
+                if constexpr (ROUNDED) {
+                    if (share == 0) {
+#pragma unroll
+                        for (int b = 0; b < NB; ++b)
+                            rounded[b] += loss_add(pb[b][1][0], loss_add(pb[b][0][0], 0.f));
+                    }
+                }
 #pragma unroll
                 for (int d = 0; d < DS; ++d) {
 #pragma unroll
@@ -685,13 +713,15 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
         const int n = first + b * 32 + ln;
-        const float all = sum[b] + __shfl_xor(sum[b], 32, 64);
+        const float all = sum[b] + __shfl_xor(sum[b], 32, 64), all_rounded = ROUNDED ? rounded[b] + __shfl_xor(rounded[b], 32, 64) : 0.f;
         const int64_t at = (int64_t)(MODE != LOSS_GRAD && a.spread ? split * LOSS_WAVES + wave : split) * a.n_own + n;
         const bool direct = MODE == LOSS_GRAD && a.n_split == 1;
         if (n < a.n_own && half == 0 && share == 0) {
             if (MODE != LOSS_GRAD) {
                 a.stat[at * 2] = ref[b] - (float)H::SHIFT;
                 a.stat[at * 2 + 1] = all;
+                if (ROUNDED)
+                    a.psum[at] = all_rounded;
             } else if (!direct && a.psum)
                 a.psum[at] = all / g_scale;
             else if (direct && a.out_sum)

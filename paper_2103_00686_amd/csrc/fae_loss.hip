@@ -14,7 +14,7 @@
 // kernels
 // ---------------------------------------------------------------------------------
 struct LossJoin {
-    const float *stat, *zt, *part;
+    const float *stat, *zt, *part, *psum; // psum: NULL where it is what stat has
     const void *targets, *w;
     int64_t w_stride;
     int32_t type;
@@ -76,6 +76,16 @@ template <int W> __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void loss_j
         }
         if (!a.mean)
             continue;
+        // The parts' means over the sum of the same rounded powers are the other classes' mean row, and what all rows have in common is in it once,
+        // however the powers were rounded: their errors count by how far a row is from that mean.
+        float even = 1.f;
+        if (a.psum) {
+            float rest = 0.f;
+            for (uint32_t i = wave * 64 + lane; i < a.n_split; i += W * 64)
+                rest += a.psum[i * a.n_rows + r] * __builtin_amdgcn_exp2f(a.stat[(i * a.n_rows + r) * 2] - most);
+            rest = over_waves(rest, false);
+            even = rest > 0.f ? sum / rest : 1.f;
+        }
         const int col = (lane % a.lanes) * 4;
         float v[4] = {0.f, 0.f, 0.f, 0.f};
         if (col < a.pitch)
@@ -107,7 +117,7 @@ template <int W> __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void loss_j
             for (int e = 0; e < 4; ++e)
                 if (col + e < a.width) {
                     const float wt = t < 0 || sum == 0.f ? 0.f : loss_value(a.w, a.type, t * a.w_stride + col + e);
-                    a.mean[r * a.width + col + e] = all == 0.f ? 0.f : (v[e] - sum * wt) / all;
+                    a.mean[r * a.width + col + e] = all == 0.f ? 0.f : (v[e] * even - sum * wt) / all;
                 }
     }
 }
@@ -346,11 +356,11 @@ static int64_t loss_part_rows(const fae_softmax_loss *l, int mode)
     const int64_t shared = tiles == 0 ? 0 : n_own > most / tiles ? most : n_own * tiles;
     return mode == LOSS_GRAD || shared > n_own ? shared : n_own; // (the gradient in one part needs none)
 }
-// what the forward takes: the largest values, per part and row reference and sum, per row the target's score, and the parts' means
+// what the forward takes: the largest values, per part and row reference and two sums, per row the target's score, and the parts' means
 static size_t loss_fwd_bytes(const fae_softmax_loss *l)
 {
     const int64_t rows = loss_part_rows(l, LOSS_MEAN), pitch = (l->width + 3) / 4 * 4;
-    return fae_align_up(LOSS_MOSTS * 4, 256) + fae_align_up(rows * 8, 256) + fae_align_up(l->n_rows * 4, 256) + fae_align_up(rows * pitch * 4, 256);
+    return fae_align_up(LOSS_MOSTS * 4, 256) + fae_align_up(rows * 8, 256) + fae_align_up(rows * 4, 256) + fae_align_up(l->n_rows * 4, 256) + fae_align_up(rows * pitch * 4, 256);
 }
 static size_t loss_grad_bytes(const fae_softmax_loss *l)
 {
@@ -492,6 +502,7 @@ static int32_t loss_forward(fae_ctx *ctx, const fae_softmax_loss *l, const void 
     a.stat = cv.take<float>(parts * l->n_rows * 2);
     a.zt = cv.take<float>(l->n_rows);
     a.part = mean ? cv.take<float>(parts * l->n_rows * s.pitch) : nullptr;
+    a.psum = mean && loss_planes_of(s.how) == 1 ? cv.take<float>(parts * l->n_rows) : nullptr;
     if (!cv.ok)
         return fae_fail(ctx, FAE_ENOSPC, "softmax loss: workspace too small");
     if (s.how == LOSS_F32_WIDE) {
@@ -515,6 +526,7 @@ static int32_t loss_forward(fae_ctx *ctx, const fae_softmax_loss *l, const void 
     j.w_stride = w_stride;
     j.type = l->type;
     j.part = a.part;
+    j.psum = a.psum;
     j.targets = l->targets;
     j.loss = loss;
     j.lse = lse;

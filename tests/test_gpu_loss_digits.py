@@ -92,3 +92,30 @@ def test_rows_whose_target_is_beyond_all_powers(hp, n, v, dtype):
                 R.assert_within(loss, *ref.loss(), "loss")
                 if keep:
                     R.assert_within(mean[0], *ref.mean(), "mean")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("n,v,d", [(300, 50, 64), (20, 400, 64), (500, 900, 200), (200, 300, 33)])
+def test_what_all_classes_have_in_common_is_in_no_gradient(hp, n, v, d, dtype):
+    """Rows of the table that differ by a few steps of their type around 1: the mean is held to their differences, not to the rows."""
+    rand = _rand(v)
+    step = torch.finfo(dtype).eps
+    w = (1 + step * (rand(v, d) * 2).round().clamp(-6, 6)).to(dtype)
+    x = rand(n, d).to(dtype)
+    t = (4 + torch.arange(n, device="cuda") * 7 % (v - 4)).to(torch.int32)
+    scale = 0.15 / (2 * step * math.sqrt(d))
+    bias = 0.5 * rand(v)
+    bias[:3] += 6.0  # most of what the target leaves goes to few classes: their roundings do not average out
+    loss, lse, mean = hp.softmax_loss(x, w, t, bias, scale, keep=True)
+    hp.sync()
+    ref = R.LossRef(x, w, t, bias, scale)
+    p, left = _others(ref)
+    wt = ref.w[ref.t]
+    want = p @ ref.w - left * wt
+    middle = p @ ref.w / left  # P's roundings count by how far a row is from the others' mean, the scores' by how far from the target's
+    apart = torch.stack([pe @ (ref.w - wr).abs() + ref.h * (pr @ (ref.w - mr).abs()) for pe, pr, wr, mr in zip(p * ref.e, p, wt, middle)])
+    size = p @ ref.w.abs() + left * wt.abs()
+    err = apart + _at_random(v / 16) * size
+    if dtype == F16:
+        err += 2.0 ** -34 * p.max(1).values[:, None] * (ref.w.abs().sum(0) + v * wt.abs())
+    R.assert_within(mean, want, err, "mean")
