@@ -448,6 +448,13 @@ size_t fae_softmax_loss_bwd_workspace_bytes(const fae_softmax_loss *what);
 int32_t fae_softmax_loss_bwd(fae_ctx *ctx, const fae_softmax_loss *what, const void *x, int64_t x_row_stride, const void *w,
                              int64_t w_row_stride, const float *lse, const float *mean, const float *gloss, void *gx,
                              int64_t gx_row_stride, void *gw, int64_t gw_row_stride, float *gbias, void *ws, size_t ws_bytes);
+/* The same with the forward's losses (device fp32[n_rows], or NULL: the plain call).  What gw and gbias of a row's target take is gloss * (p - 1).
+ * From the loss that keeps its digits however sure of its target the row is; the plain call takes it from lse and the target's
+ * score, so that 1 - p is off by some 2^-22 of |lse| there (never below 0).  gx, from mean, keeps its digits in both. */
+int32_t fae_softmax_loss_bwd_kept(fae_ctx *ctx, const fae_softmax_loss *what, const void *x, int64_t x_row_stride, const void *w,
+                                  int64_t w_row_stride, const float *lse, const float *loss, const float *mean, const float *gloss,
+                                  void *gx, int64_t gx_row_stride, void *gw, int64_t gw_row_stride, float *gbias, void *ws,
+                                  size_t ws_bytes);
 
 /* ---- norm of all gradients together, and clipping by it --------------------------------
  * Over a list of tensors of any sizes and types:

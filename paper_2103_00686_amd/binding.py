@@ -40,6 +40,7 @@ EXPORTS = [
     "fae_layer_norm_fwd", "fae_layer_norm_bwd_workspace_bytes", "fae_layer_norm_bwd",
     "fae_dropout_fwd", "fae_dropout_bwd",
     "fae_softmax_loss_fwd_workspace_bytes", "fae_softmax_loss_fwd", "fae_softmax_loss_bwd_workspace_bytes", "fae_softmax_loss_bwd",
+    "fae_softmax_loss_bwd_kept",
     "fae_grad_workspace_bytes", "fae_grad_norm", "fae_grad_clip",
 ]
 
@@ -675,23 +676,24 @@ def fae_softmax_loss_bwd_workspace_bytes(what: SoftmaxLoss) -> int:
 
 def prepare_softmax_loss_bwd(ctx: Context, what: SoftmaxLoss, x: torch.Tensor, w: torch.Tensor, lse: torch.Tensor,
                              mean: Optional[torch.Tensor], gloss: torch.Tensor, gx: Optional[torch.Tensor], gw: Optional[torch.Tensor],
-                             gbias: Optional[torch.Tensor], ws: torch.Tensor):
-    """fae_softmax_loss_bwd of these tensors, marshalled once: a zero-argument callable."""
+                             gbias: Optional[torch.Tensor], ws: torch.Tensor, loss: Optional[torch.Tensor] = None):
+    """fae_softmax_loss_bwd_kept of these tensors (without loss: fae_softmax_loss_bwd), marshalled once: a zero-argument callable."""
     c, dev = what.c(ctx.device), ctx.device
     none = (None, C.c_int64(0))
-    return _prepare(ctx, load().fae_softmax_loss_bwd,
+    return _prepare(ctx, load().fae_softmax_loss_bwd_kept,
                     (ctx._h, C.byref(c), *_loss_rows(x, what.n_rows, what, dev), *_loss_rows(w, what.n_classes, what, dev),
-                     _loss_vector("lse", lse, what.n_rows, dev), _loss_vector("mean", mean, what.n_rows * what.width, dev),
-                     _loss_vector("gloss", gloss, what.n_rows, dev), *(none if gx is None else _loss_rows(gx, what.n_rows, what, dev)),
+                     _loss_vector("lse", lse, what.n_rows, dev), _loss_vector("loss", loss, what.n_rows, dev),
+                     _loss_vector("mean", mean, what.n_rows * what.width, dev), _loss_vector("gloss", gloss, what.n_rows, dev),
+                     *(none if gx is None else _loss_rows(gx, what.n_rows, what, dev)),
                      *(none if gw is None else _loss_rows(gw, what.n_classes, what, dev)), _loss_vector("gbias", gbias, what.n_classes, dev),
                      _ptr_on(ws, torch.uint8, dev), C.c_size_t(ws.numel())),
-                    (ctx, c, x, w, lse, mean, gloss, gx, gw, gbias, ws))
+                    (ctx, c, x, w, lse, loss, mean, gloss, gx, gw, gbias, ws))
 
 
 def fae_softmax_loss_bwd(ctx: Context, what: SoftmaxLoss, x: torch.Tensor, w: torch.Tensor, lse: torch.Tensor, mean: Optional[torch.Tensor],
                          gloss: torch.Tensor, gx: Optional[torch.Tensor], gw: Optional[torch.Tensor], gbias: Optional[torch.Tensor],
-                         ws: torch.Tensor):
-    prepare_softmax_loss_bwd(ctx, what, x, w, lse, mean, gloss, gx, gw, gbias, ws)()
+                         ws: torch.Tensor, loss: Optional[torch.Tensor] = None):
+    prepare_softmax_loss_bwd(ctx, what, x, w, lse, mean, gloss, gx, gw, gbias, ws, loss)()
 
 
 def _dense(t: torch.Tensor) -> bool:

@@ -8,7 +8,7 @@
 //   LOSS_STATS  held: x, streamed: w; reference and sum of 2^(Z - reference) of all classes but the target for every row of x, and the target's Z
 //               (the reference is one of the others too: the target's may lie far above)
 //   LOSS_MEAN   the same, and O = the sum of 2^(Z - reference) w of all classes but the target; of 16-bit types also the sum of P as rounded for O
-//   LOSS_GRAD   held: w, streamed: x; P = gloss (2^(Z - lse) - (class is the target)), O = the sum of P x, and the sum of P (bias)
+//   LOSS_GRAD   held: w, streamed: x; P = gloss 2^(Z - lse), or what the row leaves to its target, O = the sum of P x, and the sum of P (bias)
 // Z is in units of log 2 throughout.
 //   LOSS_FEW    what LOSS_STATS finds, for few rows
 enum { LOSS_STATS, LOSS_MEAN, LOSS_GRAD, LOSS_FEW };
@@ -25,7 +25,7 @@ struct loss_args {
     const float *st_most; // fp32 as fp16 numbers: n_most values, the largest of them is the largest streamed value
     const float *g_most;  // gradient with fp16 numbers: the same of |gloss|
     int32_t n_most;
-    const float *nlse, *g; // gradient, per streamed row: -lse * log2(e) + log2 |gloss|, gloss (-infinity and 0 without a target)
+    const float *nlse, *gt; // gradient, per streamed row: -lse * log2(e) + log2 |gloss|, P of its target (-infinity and -0 without one)
     const int32_t *t;      // ... and its target or -1
     uint32_t *status;
     float *stat; // forward: [n_split][n_own][2]: reference, sum of 2^(Z - reference)
@@ -333,7 +333,7 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
     constexpr int PLANE = TM * DP * 2, TILE = P * PLANE; // bytes
     constexpr bool HAS_O = MODE != LOSS_STATS, ROUNDED = MODE == LOSS_MEAN && P == 1;
     __shared__ __attribute__((aligned(16))) char tiles[2 * TILE];
-    __shared__ float side[2][3][TM]; // forward: bias; gradient: -lse + log |gloss|, gloss, target
+    __shared__ float side[2][3][TM]; // forward: bias; gradient: -lse + log |gloss|, P of the target, target
     __shared__ float mosts[2][LOSS_WAVES * SHARES];
 
     const int lane = fae_lane(), wave = threadIdx.x / 64 % LOSS_WAVES, share = threadIdx.x / (LOSS_WAVES * 64), ln = lane & 31, half = lane >> 5;
@@ -453,7 +453,7 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
             const bool in = m < a.n_st;
             if (MODE == LOSS_GRAD) {
                 next_side[0] = in ? a.nlse[m] + g_log : -INFINITY;
-                next_side[1] = in ? a.g[m] * g_scale : 0.f;
+                next_side[1] = in ? a.gt[m] * g_scale : -0.f;
                 next_side[2] = __int_as_float(in ? a.t[m] : -1);
             } else
                 next_side[0] = !in ? -INFINITY : (BIAS ? a.bias[m] * 1.44269504f : 0.f);
@@ -562,18 +562,19 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
                         for (int e = 0; e < 4; ++e)
                             pr[b][j * 4 + e] = __builtin_amdgcn_exp2f(fmaf(z[b][j * 4 + e], c[b], BIAS ? own_bias[b] + nl[e] : nl[e]));
                 }
-                // a target in this wave's classes, or a gradient below 0: seldom
+                // A target in this wave's classes, or a gradient below 0: seldom.  P of a target is gloss (p - 1), of the other sign than gloss also where it
+                // is 0; p - 1 has been found before, as the exponential here and 1 would leave nothing of it in a row that is sure of its target.
                 const int32_t mine = __float_as_int(side[buf][2][sb * 32 + ln]);
-                if (__any((mine >= first && mine < first + 32 * NB) || side[buf][1][sb * 32 + ln] < 0.f)) {
+                if (__any((mine >= first && mine < first + 32 * NB) || __float_as_int(side[buf][1][sb * 32 + ln]) >= 0)) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const loss_f4 g = *(const loss_f4 *)(sd + TM + j * 8), t = *(const loss_f4 *)(sd + 2 * TM + j * 8);
+                        const loss_f4 gt = *(const loss_f4 *)(sd + TM + j * 8), t = *(const loss_f4 *)(sd + 2 * TM + j * 8);
 #pragma unroll
                         for (int b = 0; b < NB; ++b)
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
                                 const float v = pr[b][j * 4 + e];
-                                pr[b][j * 4 + e] = (g[e] < 0.f ? -v : v) - (__float_as_int(t[e]) == first + b * 32 + ln ? g[e] : 0.f);
+                                pr[b][j * 4 + e] = __float_as_int(t[e]) == first + b * 32 + ln ? gt[e] : __float_as_int(gt[e]) >= 0 ? -v : v;
                             }
                     }
                 }

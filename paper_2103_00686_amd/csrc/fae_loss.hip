@@ -126,8 +126,10 @@ struct LossRows {
     const void *x, *targets;
     void *gx;
     int64_t x_stride, gx_stride, n_rows;
-    const float *lse, *mean, *gloss;
-    float *nlse, *g;
+    const float *lse, *loss, *mean, *gloss, *bias; // loss: NULL if the caller has not kept it
+    const void *w;
+    int64_t w_stride;
+    float *nlse, *gt; // NULL: gx alone
     int32_t *t;
     float *g_most, *x_most; // a value for every workgroup
     int32_t target_bits, n_classes, width;
@@ -194,10 +196,28 @@ template <typename T> __global__ __launch_bounds__(256) void loss_rows_kernel(Lo
             t = -1;
         const float g = t < 0 ? 0.f : a.gloss[r];
         g_most = loss_most(g_most, g);
-        if (lane == 0) {
-            a.nlse[r] = t < 0 ? -INFINITY : __log2f(fabsf(g)) - lse * 1.44269504f;
-            a.g[r] = g;
-            a.t[r] = t;
+        if (a.gt) {
+            // 1 - p of the target is 1 - exp(-loss); without the loss, from lse and the target's score, whose digits end at lse's
+            float loss = 0.f;
+            if (t >= 0) {
+                if (a.loss)
+                    loss = a.loss[r];
+                else {
+                    float z = 0.f;
+                    for (int c = lane; c < a.width; c += 64)
+                        z = fmaf((float)((const T *)a.x)[r * a.x_stride + c], (float)((const T *)a.w)[t * a.w_stride + c], z);
+#pragma unroll
+                    for (int d = 32; d > 0; d >>= 1)
+                        z += __shfl_xor(z, d, 64);
+                    loss = lse - (a.scale * z + (a.bias ? a.bias[t] : 0.f));
+                    loss = loss < 0.f ? 0.f : loss;
+                }
+            }
+            if (lane == 0) {
+                a.nlse[r] = t < 0 ? -INFINITY : __log2f(fabsf(g)) - lse * 1.44269504f;
+                a.gt[r] = t < 0 ? -0.f : copysignf(g * expm1f(-loss), -g); // (expm1f loses the sign of 0)
+                a.t[r] = t;
+            }
         }
         for (int c = lane; c < a.width; c += 64) {
             if (a.x_most && t >= 0)
@@ -577,18 +597,17 @@ extern "C" int32_t fae_softmax_loss_fwd(fae_ctx *ctx, const fae_softmax_loss *wh
     return loss_forward(ctx, what, x, x_row_stride, w, w_row_stride, loss, lse, mean, ws, ws_bytes);
 }
 
-extern "C" int32_t fae_softmax_loss_bwd(fae_ctx *ctx, const fae_softmax_loss *what, const void *x, int64_t x_row_stride, const void *w,
-                                        int64_t w_row_stride, const float *lse, const float *mean, const float *gloss, void *gx,
-                                        int64_t gx_row_stride, void *gw, int64_t gw_row_stride, float *gbias, void *ws, size_t ws_bytes)
+static int32_t loss_backward(fae_ctx *ctx, const char *who, const fae_softmax_loss *what, const void *x, int64_t x_row_stride, const void *w,
+                             int64_t w_row_stride, const float *lse, const float *loss, const float *mean, const float *gloss, void *gx,
+                             int64_t gx_row_stride, void *gw, int64_t gw_row_stride, float *gbias, void *ws, size_t ws_bytes)
 {
-    const char *who = "fae_softmax_loss_bwd";
     int32_t rc = loss_check(ctx, who, what, x, x_row_stride, w, w_row_stride);
     if (rc != FAE_OK)
         return rc;
     const int64_t n = what->n_rows, v = what->n_classes, d = what->width;
     const int size = fae_type_size(what->type);
-    if (((uintptr_t)lse | (uintptr_t)mean | (uintptr_t)gloss | (uintptr_t)gbias) % 4 != 0)
-        return fae_fail(ctx, FAE_EINVAL, "%s: lse, mean, gloss or gbias are not aligned to their values", who);
+    if (((uintptr_t)lse | (uintptr_t)loss | (uintptr_t)mean | (uintptr_t)gloss | (uintptr_t)gbias) % 4 != 0)
+        return fae_fail(ctx, FAE_EINVAL, "%s: lse, loss, mean, gloss or gbias are not aligned to their values", who);
     if (n > 0 && (!lse || !gloss))
         return fae_fail(ctx, FAE_EINVAL, "%s: null %s", who, lse ? "gloss" : "lse");
     if (gx && n > 0)
@@ -601,8 +620,8 @@ extern "C" int32_t fae_softmax_loss_bwd(fae_ctx *ctx, const fae_softmax_loss *wh
                             loss_span("workspace", ws, ws_bytes, ws_bytes, 1, 1)};
     const LossSpan in[] = {loss_span("x", x, x_row_stride, d, n, size), loss_span("w", w, w_row_stride, d, v, size), loss_span("bias", what->bias, 1, 1, v, 4),
                            loss_span("targets", what->targets, 1, 1, n, what->target_bits / 8), loss_span("lse", lse, 1, 1, n, 4),
-                           loss_span("mean", mean, d, d, n, 4), loss_span("gloss", gloss, 1, 1, n, 4)};
-    rc = loss_check_outputs(ctx, who, out, 4, in, 7);
+                           loss_span("mean", mean, d, d, n, 4), loss_span("gloss", gloss, 1, 1, n, 4), loss_span("loss", loss, 1, 1, n, 4)};
+    rc = loss_check_outputs(ctx, who, out, 4, in, 8);
     if (rc == FAE_OK)
         rc = loss_check_ws(ctx, who, ws, ws_bytes, fae_softmax_loss_bwd_workspace_bytes(what));
     if (rc != FAE_OK)
@@ -612,8 +631,7 @@ extern "C" int32_t fae_softmax_loss_bwd(fae_ctx *ctx, const fae_softmax_loss *wh
     float *g_most = cv.take<float>(LOSS_MOSTS), *x_most = cv.take<float>(LOSS_MOSTS);
     LossRows r;
     memset(&r, 0, sizeof(r));
-    r.nlse = cv.take<float>(n);
-    r.g = cv.take<float>(n);
+    float *nlse = cv.take<float>(n), *gt = cv.take<float>(n);
     r.t = cv.take<int32_t>(n);
     float *own_mean = cv.take<float>(n * d);
     if (!cv.ok)
@@ -636,9 +654,15 @@ extern "C" int32_t fae_softmax_loss_bwd(fae_ctx *ctx, const fae_softmax_loss *wh
         r.gx_stride = gx_row_stride;
         r.n_rows = n;
         r.lse = lse;
+        r.loss = loss;
         r.mean = mean;
         r.gloss = gloss;
+        r.bias = what->bias;
+        r.w = w;
+        r.w_stride = w_row_stride;
         const bool grads = gw || gbias;
+        r.nlse = nlse;
+        r.gt = grads ? gt : nullptr;
         r.g_most = grads && what->type != FAE_BF16 ? g_most : nullptr;
         r.x_most = grads && what->type == FAE_F32 ? x_most : nullptr;
         r.target_bits = what->target_bits;
@@ -667,8 +691,8 @@ extern "C" int32_t fae_softmax_loss_bwd(fae_ctx *ctx, const fae_softmax_loss *wh
     a.own_stride = w_row_stride;
     a.n_st = (int32_t)n;
     a.n_own = (int32_t)v;
-    a.nlse = r.nlse;
-    a.g = r.g;
+    a.nlse = nlse;
+    a.gt = gt;
     a.t = r.t;
     a.g_most = g_most;
     a.st_most = x_most;
@@ -712,4 +736,21 @@ extern "C" int32_t fae_softmax_loss_bwd(fae_ctx *ctx, const fae_softmax_loss *wh
         FAE_LAUNCH_CHECK(ctx);
     }
     return FAE_OK;
+}
+
+extern "C" int32_t fae_softmax_loss_bwd(fae_ctx *ctx, const fae_softmax_loss *what, const void *x, int64_t x_row_stride, const void *w,
+                                        int64_t w_row_stride, const float *lse, const float *mean, const float *gloss, void *gx,
+                                        int64_t gx_row_stride, void *gw, int64_t gw_row_stride, float *gbias, void *ws, size_t ws_bytes)
+{
+    return loss_backward(ctx, "fae_softmax_loss_bwd", what, x, x_row_stride, w, w_row_stride, lse, nullptr, mean, gloss, gx, gx_row_stride, gw, gw_row_stride, gbias,
+                         ws, ws_bytes);
+}
+
+extern "C" int32_t fae_softmax_loss_bwd_kept(fae_ctx *ctx, const fae_softmax_loss *what, const void *x, int64_t x_row_stride, const void *w,
+                                             int64_t w_row_stride, const float *lse, const float *loss, const float *mean, const float *gloss,
+                                             void *gx, int64_t gx_row_stride, void *gw, int64_t gw_row_stride, float *gbias, void *ws,
+                                             size_t ws_bytes)
+{
+    return loss_backward(ctx, "fae_softmax_loss_bwd_kept", what, x, x_row_stride, w, w_row_stride, lse, loss, mean, gloss, gx, gx_row_stride, gw, gw_row_stride,
+                         gbias, ws, ws_bytes);
 }

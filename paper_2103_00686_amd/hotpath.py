@@ -435,14 +435,17 @@ class HotPath:
         return (loss, lse, mean) if keep else (loss, lse)
 
     def softmax_loss_backward(self, x: torch.Tensor, w, targets: torch.Tensor, lse: torch.Tensor, gloss: torch.Tensor,
-                              mean: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, scale: float = 1.0):
-        """(gx, gw), or (gx, gw, gbias) with a bias, from the gradient gloss of every row's loss; lse and mean from ``softmax_loss``."""
+                              mean: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, scale: float = 1.0,
+                              loss: Optional[torch.Tensor] = None):
+        """(gx, gw), or (gx, gw, gbias) with a bias, from the gradient gloss of every row's loss; lse, mean and loss from ``softmax_loss``.
+        With the loss gw and gbias keep their digits also in rows that are sure of their target; without it 1 - p of a target is off by some 2^-22
+        of |lse|."""
         w = self._classes(w)
         what = B.SoftmaxLoss(x.shape[0], w.shape[0], x.shape[-1], targets, bias, scale, x.dtype)
         gx, gw = (torch.empty(tuple(t.shape), dtype=x.dtype, device=self.dev) for t in (x, w))
         gbias = torch.empty(w.shape[0], dtype=torch.float32, device=self.dev) if bias is not None else None
         B.fae_softmax_loss_bwd(self.ctx, what, x, w, lse, mean, gloss, gx, gw, gbias,
-                               self._call_workspace("loss", B.fae_softmax_loss_bwd_workspace_bytes(what)))
+                               self._call_workspace("loss", B.fae_softmax_loss_bwd_workspace_bytes(what)), loss)
         return (gx, gw) if bias is None else (gx, gw, gbias)
 
     # -- norm of all gradients together, and clipping by it ------------------------------------
@@ -470,9 +473,9 @@ class HotPath:
 
     def prepare_softmax_loss_backward(self, what: B.SoftmaxLoss, x: torch.Tensor, w: torch.Tensor, lse: torch.Tensor, gloss: torch.Tensor,
                                       gx: Optional[torch.Tensor], gw: Optional[torch.Tensor], gbias: Optional[torch.Tensor] = None,
-                                      mean: Optional[torch.Tensor] = None):
+                                      mean: Optional[torch.Tensor] = None, loss: Optional[torch.Tensor] = None):
         return B.prepare_softmax_loss_bwd(self.ctx, what, x, w, lse, mean, gloss, gx, gw, gbias,
-                                          self._own_workspace(B.fae_softmax_loss_bwd_workspace_bytes(what)))
+                                          self._own_workspace(B.fae_softmax_loss_bwd_workspace_bytes(what)), loss)
 
     def prepare_gradient_norm(self, grads: Sequence[torch.Tensor], norm: torch.Tensor, scale: float = 1.0):
         return B.prepare_grad_norm(self.ctx, grads, scale, norm, self._own_workspace(B.fae_grad_workspace_bytes(len(grads))))

@@ -119,3 +119,71 @@ def test_what_all_classes_have_in_common_is_in_no_gradient(hp, n, v, d, dtype):
     if dtype == F16:
         err += 2.0 ** -34 * p.max(1).values[:, None] * (ref.w.abs().sum(0) + v * wt.abs())
     R.assert_within(mean, want, err, "mean")
+
+
+def _sure(n, v, least, most, dtype, seed):
+    """Rows with targets of their own, `least` to `most` nats above all other classes."""
+    rand = _rand(seed)
+    d = n + 16
+    x, w = torch.zeros((n, d), device="cuda"), torch.zeros((v, d), device="cuda")
+    w[:, n:] = 0.5 + 0.3 * rand(v, 16)
+    x[:, n:] = 0.3 * rand(n, 16)
+    at = torch.arange(n, device="cuda")
+    t = at * (v // n) + 3
+    x[at, at] = torch.linspace(least, most, n, device="cuda")
+    w[t, at] = 1.0
+    return x.to(dtype), w.to(dtype), t.to(torch.int32), rand
+
+
+def _gradients(ref, g):
+    """(gw, gbias, bounds) with 1 - p of a target as the sum of the others' probabilities."""
+    p, left = _others(ref)
+    eo = (p * ref.e).sum(1)[:, None] / left + ref.dz.gather(1, ref.t[:, None]) + 16 * R.U  # of 1 - p
+    g = g.double()[:, None]
+    G, size = g * (p - ref.hot * left), g.abs() * (p + ref.hot * left)
+    dG = g.abs() * (p * ref.e + ref.hot * left * eo)
+    x, s = ref.x, abs(ref.scale)
+    n = ref.n
+    gw, tw = ref.scale * (G.t().contiguous() @ x), s * (size.t().contiguous() @ x.abs())
+    dw = s * ((dG + size * ref.h).t().contiguous() @ x.abs()) + _at_random(ref.N * n / 16) * tw
+    return gw, dw, tw, G.sum(0), dG.sum(0) + _at_random(n) * size.sum(0), size
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("v", [700, 40_000])
+def test_gradient_of_a_target_that_is_sure(hp, v, dtype):
+    """loss down to 1e-14: with the forward's loss, the target's gradient is that sum and no difference of two numbers next to 1."""
+    n = 48
+    x, w, t, rand = _sure(n, v, 14.0, 40.0, dtype, v)
+    bias = 0.1 * rand(v)
+    for g in (rand(n), rand(n).abs(), -rand(n).abs()):
+        loss, lse, mean = hp.softmax_loss(x, w, t, bias, keep=True)
+        gx, gw, gb = hp.softmax_loss_backward(x, w, t, lse, g, mean, bias, loss=loss)
+        hp.sync()
+        ref = R.LossRef(x, w, t, bias)
+        rw, dw, tw, rb, db, size = _gradients(ref, g)
+        live = size.sum(0) > 0
+        assert float((db / size.sum(0))[live].max()) < 0.02
+        R.assert_within(gb, rb, db, "gbias")
+        if dtype != BF16:  # fp16 numbers of all probabilities beside the largest gradient
+            dw = dw + 2.0 ** -38 * float(g.abs().max()) * ref.x.abs().sum(0)
+        if dtype != F32:
+            dw = dw + R.half_step(rw.abs() + dw, dtype)
+        R.assert_within(gw, rw, dw, "gw")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_gradient_of_a_target_without_the_loss(hp, dtype):
+    """From lse alone 1 - p is a difference whose digits end at lse's, but it has no wrong sign."""
+    n, v = 48, 700
+    x, w, t, rand = _sure(n, v, 20.0, 60.0, dtype, 5)
+    bias, g = 0.1 * rand(v), rand(n).abs()
+    loss, lse, mean = hp.softmax_loss(x, w, t, bias, keep=True)
+    gx, gw, gb = hp.softmax_loss_backward(x, w, t, lse, g, mean, bias)
+    hp.sync()
+    ref = R.LossRef(x, w, t, bias)
+    p, left = _others(ref)
+    from_others = (g.double()[:, None] * p).sum(0)
+    assert bool((gb.double() <= from_others * 1.01)[t.long()].all())
+    (_, _, _, _), (_, _, _, _), (rb, db) = ref.backward(g)
+    R.assert_within(gb, rb, db, "gbias")
