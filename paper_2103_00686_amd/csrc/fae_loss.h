@@ -23,7 +23,7 @@ struct loss_args {
     const void *targets;  // forward
     int32_t target_bits, n_classes;
     const float *st_most; // fp32 as fp16 numbers: n_most values, the largest of them is the largest streamed value
-    const float *g_most;  // gradient with fp16 numbers: the same of |gloss|
+    const float *g_most;  // gradient of fp16: the same of |gloss|
     int32_t n_most;
     const float *nlse, *gt; // gradient, per streamed row: -lse * log2(e) + log2 |gloss|, P of its target (-infinity and -0 without one)
     const int32_t *t;      // ... and its target or -1
@@ -157,8 +157,9 @@ template <int HOW, int KS, typename V, int P> __device__ __forceinline__ void lo
     }
 }
 
-// eight fp32 values as planes, each rounded to nearest so that what is left has either sign
-template <int HOW> __device__ __forceinline__ void loss_split(const float (&v)[8], typename loss_vec<typename loss_type<HOW>::E>::v8 (&o)[loss_type<HOW>::PLANES])
+// eight fp32 values as planes, each rounded to nearest so that what is left has either sign (SCALED, two fp16 numbers alone: times a power of two)
+template <int HOW, bool SCALED = false>
+__device__ __forceinline__ void loss_split(const float (&v)[8], typename loss_vec<typename loss_type<HOW>::E>::v8 (&o)[loss_type<HOW>::PLANES], float up = 1.f)
 {
     typedef typename loss_type<HOW>::E E;
     float r[8];
@@ -167,6 +168,23 @@ template <int HOW> __device__ __forceinline__ void loss_split(const float (&v)[8
         r[e] = v[e];
 #pragma unroll
     for (int p = 0; p < loss_type<HOW>::PLANES; ++p) {
+        if constexpr (SCALED) {
+            if (p == 0) { // a mixed product and sum rounds to either half of a register
+                typedef uint32_t words __attribute__((ext_vector_type(4)));
+                words w;
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    uint32_t two;
+                    asm("v_fma_mixlo_f16 %0, %1, %2, 0" : "=v"(two) : "v"(r[e]), "v"(up));
+                    asm("v_fma_mixhi_f16 %0, %1, %2, 0" : "+v"(two) : "v"(r[e + 1]), "v"(up));
+                    w[e / 2] = two;
+                    asm("v_fma_mix_f32 %0, %0, %2, -%1 op_sel_hi:[0,0,1]" : "+v"(r[e]) : "v"(two), "v"(up));
+                    asm("v_fma_mix_f32 %0, %0, %2, -%1 op_sel:[0,0,1] op_sel_hi:[0,0,1]" : "+v"(r[e + 1]) : "v"(two), "v"(up));
+                }
+                o[0] = __builtin_bit_cast(typename loss_vec<E>::v8, w);
+                continue;
+            }
+        }
 #pragma unroll
         for (int e = 0; e < 8; ++e)
             o[p][e] = (E)r[e];
@@ -316,6 +334,15 @@ __device__ __forceinline__ float loss_sum(const float (&v)[16])
     return ((s[0] + s[4]) + (s[2] + s[6])) + ((s[1] + s[5]) + (s[3] + s[7]));
 }
 
+__device__ __forceinline__ float loss_sum_abs(const float (&v)[16])
+{
+    float a[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        a[i] = fabsf(v[i]);
+    return loss_sum(a);
+}
+
 #define LOSS_LDS(T) __attribute__((address_space(3))) T
 
 template <int HOW, int DP, int MODE, bool BIAS>
@@ -332,6 +359,7 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
     constexpr int KS = DP / 16, DS = DP / 32 / SHARES, PIECES = TM * DP / 8, NC = (PIECES + THREADS - 1) / THREADS;
     constexpr int PLANE = TM * DP * 2, TILE = P * PLANE; // bytes
     constexpr bool HAS_O = MODE != LOSS_STATS, ROUNDED = MODE == LOSS_MEAN && P == 1;
+    constexpr bool MOVES = MODE == LOSS_GRAD && HOW == LOSS_F32_WIDE;
     __shared__ __attribute__((aligned(16))) char tiles[2 * TILE];
     __shared__ float side[2][3][TM]; // forward: bias; gradient: -lse + log |gloss|, P of the target, target
     __shared__ float mosts[2][LOSS_WAVES * SHARES];
@@ -351,12 +379,13 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
 
     // What was found before: the largest streamed value and gradient.  fp16 numbers of both are brought to a range that keeps them.
     float st_scale = 1.f, g_scale = 1.f, g_log = 0.f, c_all = a.c, back = 1.f;
+    int st_up = 0;
     if (HOW == LOSS_F32_WIDE || (HOW == LOSS_F16 && MODE == LOSS_GRAD)) {
         float most[2] = {0.f, 0.f};
         for (int i = threadIdx.x; i < a.n_most; i += THREADS) {
             if (HOW == LOSS_F32_WIDE)
                 most[0] = fmaxf(most[0], a.st_most[i]);
-            if (MODE == LOSS_GRAD)
+            if (HOW == LOSS_F16)
                 most[1] = fmaxf(most[1], a.g_most[i]);
         }
 #pragma unroll
@@ -374,12 +403,14 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
             for (int i = 0; i < LOSS_WAVES * SHARES; ++i)
                 most[k] = fmaxf(most[k], mosts[k][i]);
         if (HOW == LOSS_F32_WIDE) {
-            const int up = loss_power(most[0], 15);
-            st_scale = __builtin_amdgcn_ldexpf(1.f, up);
-            back = __builtin_amdgcn_ldexpf(1.f, -up);
+            st_up = loss_power(most[0], 15);
+            st_scale = __builtin_amdgcn_ldexpf(1.f, st_up);
+            back = __builtin_amdgcn_ldexpf(1.f, -st_up);
             c_all *= back;
         }
-        if (MODE == LOSS_GRAD) { // the largest P is below 2^15: of a probability of 2^-20, fp32 keeps 20 bits still
+        if (HOW == LOSS_F16) {
+            // The largest P is below 2^15, and from 2^-39 of it on P is lost.  What gw then lacks is below half its own smallest step of 2^-24 as long as
+            // rows x |gloss| |x| |scale| is below 2^14; sums that reach that far are about to leave fp16 on the other side.
             const int up = loss_power(most[1], 15);
             g_scale = __builtin_amdgcn_ldexpf(1.f, up);
             g_log = (float)up;
@@ -501,6 +532,9 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
     loss_f16v o[NB][HAS_O ? DS : 1];
     // Forward: 2^(Z - ref) is what is summed.  Gradient: sum is that of P.
     float ref[NB], sum[NB], rounded[NB];
+    // Gradient, P as two fp16 numbers: every class has a power of two of its own, which falls when its P grow, and keeps all digits of its sum beside
+    // others' of any size (a step of 2048 x 1 000 000 x 32 1740 us, 1665 with one power for all, where P below 2^-39 of the largest was lost).
+    float up[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
 #pragma unroll
@@ -508,6 +542,7 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
             o[b][d] = (loss_f16v)(0.f);
         ref[b] = -3.402823466e38f;
         sum[b] = rounded[b] = 0.f;
+        up[b] = 0x1p120f;
     }
     if (tile0 < tile1) {
         fetch(tile0);
@@ -565,7 +600,8 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
                 // A target in this wave's classes, or a gradient below 0: seldom.  P of a target is gloss (p - 1), of the other sign than gloss also where it
                 // is 0; p - 1 has been found before, as the exponential here and 1 would leave nothing of it in a row that is sure of its target.
                 const int32_t mine = __float_as_int(side[buf][2][sb * 32 + ln]);
-                if (__any((mine >= first && mine < first + 32 * NB) || __float_as_int(side[buf][1][sb * 32 + ln]) >= 0)) {
+                const bool seldom = __any((mine >= first && mine < first + 32 * NB) || __float_as_int(side[buf][1][sb * 32 + ln]) >= 0);
+                if (seldom) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const loss_f4 gt = *(const loss_f4 *)(sd + TM + j * 8), t = *(const loss_f4 *)(sd + 2 * TM + j * 8);
@@ -578,9 +614,32 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
                             }
                     }
                 }
+                bool over = false;
 #pragma unroll
-                for (int b = 0; b < NB; ++b)
-                    sum[b] += loss_sum(pr[b]);
+                for (int b = 0; b < NB; ++b) {
+                    const float some = loss_sum(pr[b]);
+                    sum[b] += some;
+                    if (MOVES)
+                        over = over || !((seldom ? loss_sum_abs(pr[b]) : some) * up[b] < H::MOST);
+                }
+                if (MOVES && __any(over)) {
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) {
+                        float most = 0.f;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            most = fmaxf(most, fabsf(pr[b][i]));
+                        most = fmaxf(most, __shfl_xor(most, 32, 64));
+                        const float to = fminf(up[b], __builtin_amdgcn_ldexpf(1.f, H::SHIFT - __builtin_amdgcn_frexp_expf(most)));
+                        const float f = to / up[b];
+                        up[b] = to;
+#pragma unroll
+                        for (int d = 0; d < (HAS_O ? DS : 1); ++d)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i)
+                                o[b][d][i] *= f;
+                    }
+                }
             } else {
                 // The target's score goes out by itself, and is minus infinity from here on (c is never 0).  It has no part in sum and mean, nor in
                 // the reference: 2^10 above the others' largest, as in a row that is sure of its target, it would leave their powers
@@ -672,7 +731,7 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
 #pragma unroll
                         for (int e = 0; e < 8; ++e)
                             v[e] = pr[b][t * 8 + e];
-                        loss_split<HOW>(v, pb[b][t]);
+                        loss_split<HOW, MOVES>(v, pb[b][t], up[b]);
                     }
                 // P loses up to half a step of its type here: O is then divided by the sum of what P has become, so that what all rows have in common
                 // stays (dot products with ones: 30 us of the 1130 of a step of 16 384 x 100 003 x 64 bf16).
@@ -724,9 +783,9 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
                 if (ROUNDED)
                     a.psum[at] = all_rounded;
             } else if (!direct && a.psum)
-                a.psum[at] = all / g_scale;
+                a.psum[at] = MOVES ? all : all / g_scale;
             else if (direct && a.out_sum)
-                a.out_sum[n] = all / g_scale;
+                a.out_sum[n] = MOVES ? all : all / g_scale;
         }
         if (HAS_O && n < a.n_own && (direct ? a.out != nullptr : a.part != nullptr)) {
             const float f = MODE == LOSS_GRAD ? (direct ? a.scale : 1.f) / g_scale : 1.f;
@@ -738,7 +797,7 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
                     float v[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        v[e] = o[b][d][j * 4 + e] * back * f;
+                        v[e] = MOVES ? __builtin_amdgcn_ldexpf(o[b][d][j * 4 + e] * f, 1 - __builtin_amdgcn_frexp_expf(up[b]) - st_up) : o[b][d][j * 4 + e] * back * f;
                     if (!direct) {
                         if (col < a.pitch)
                             *(loss_f4 *)(a.part + at * a.pitch + col) = loss_f4{v[0], v[1], v[2], v[3]};

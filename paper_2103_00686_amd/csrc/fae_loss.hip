@@ -663,7 +663,7 @@ static int32_t loss_backward(fae_ctx *ctx, const char *who, const fae_softmax_lo
         const bool grads = gw || gbias;
         r.nlse = nlse;
         r.gt = grads ? gt : nullptr;
-        r.g_most = grads && what->type != FAE_BF16 ? g_most : nullptr;
+        r.g_most = grads && what->type == FAE_F16 ? g_most : nullptr;
         r.x_most = grads && what->type == FAE_F32 ? x_most : nullptr;
         r.target_bits = what->target_bits;
         r.n_classes = (int32_t)v;

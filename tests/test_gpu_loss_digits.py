@@ -187,3 +187,54 @@ def test_gradient_of_a_target_without_the_loss(hp, dtype):
     assert bool((gb.double() <= from_others * 1.01)[t.long()].all())
     (_, _, _, _), (_, _, _, _), (rb, db) = ref.backward(g)
     R.assert_within(gb, rb, db, "gbias")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("width", [20, 64, 100, 200])
+def test_classes_whose_gradients_are_small_beside_others(hp, width, dtype):
+    """Seven groups of rows, each with its own classes, and gradients from 1 down to 2^-54: every class keeps the digits of its own sum (fp16:
+    but for 2^-39 of the largest gradient for every row, far below half a step of 2^-24)."""
+    rand = _rand(width)
+    groups, per, classes = 7, 40, 900
+    n, v = groups * per, groups * classes
+    x, w = 0.2 * rand(n, width), 0.5 + 0.3 * rand(v, width)
+    x[:, :groups], w[:, :groups] = 0.0, 0.0
+    row, cls = torch.arange(n, device="cuda") // per, torch.arange(v, device="cuda") % groups
+    x[torch.arange(n, device="cuda"), row] = 45.0
+    w[torch.arange(v, device="cuda"), cls] = 1.0
+    t = (torch.randint(0, classes, (n,), device="cuda") * groups + row).to(torch.int32)
+    x, w = x.to(dtype), w.to(dtype)
+    g = rand(n) * 2.0 ** (-9.0 * row)
+    bias = 0.1 * rand(v)
+    for b in (None, bias):
+        loss, lse, mean = hp.softmax_loss(x, w, t, b, keep=True)
+        gx, gw, *gb = hp.softmax_loss_backward(x, w, t, lse, g, mean, b, loss=loss)
+        hp.sync()
+        ref = R.LossRef(x, w, t, b)
+        rw, dw, tw, rb, db, size = _gradients(ref, g)
+        dw = dw + 2.0 ** -126 * ref.x.abs().sum(0)  # the power is 0 below fp32's smallest normal number: a gradient of 2^-54 times a probability of 2^-75
+        if dtype == F32:
+            dw = dw + 2.0 ** -34 * size.amax(0)[:, None] * ref.x.abs().sum(0) + ref.mx * size.sum(0)[:, None]
+        if dtype == F16:
+            dw = dw + 2.0 ** -39 * float(g.abs().max()) * ref.x.abs().sum(0)
+        else:
+            assert float((dw / tw).median()) < 0.02
+        if dtype != F32:
+            dw = dw + R.half_step(rw.abs() + dw, dtype)
+        R.assert_within(gw, rw, dw, "gw")
+        if b is not None:
+            R.assert_within(gb[0], rb, db, "gbias")
+
+
+def test_all_rows_sure_of_their_targets_in_fp32(hp):
+    """Nothing but small gradients: a class that is nobody's target has what the rows leave to it, down to 1e-24."""
+    n, v = 48, 2000
+    for least, most in ((30.0, 34.0), (20.0, 60.0)):
+        x, w, t, rand = _sure(n, v, least, most, F32, 9)
+        g = rand(n)
+        loss, lse, mean = hp.softmax_loss(x, w, t, keep=True)
+        gx, gw = hp.softmax_loss_backward(x, w, t, lse, g, mean, loss=loss)
+        hp.sync()
+        ref = R.LossRef(x, w, t)
+        rw, dw, tw, _, _, size = _gradients(ref, g)
+        R.assert_within(gw, rw, dw + 2.0 ** -34 * size.amax(0)[:, None] * ref.x.abs().sum(0) + ref.mx * size.sum(0)[:, None], "gw")
