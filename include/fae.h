@@ -435,6 +435,7 @@ typedef struct {
  * for its backward:
  *   mean[r] = sum over the classes v other than r's target of exp(z[r][v] - lse[r]) * (w[v] - w[target[r]])
  * (w[v] alone in a row without a target).
+ * With a width above 128, a mean needs n_rows, and gw or gbias n_classes, below 2^30 - 127.
  * No output may share memory with another or with an input.  ws is on 16 bytes; its size does not fall with
  * n_rows or n_classes (one for the largest call is enough for the others), and calls that may overlap need one each.  Sums
  * are taken in an order that depends on the sizes alone.  Asynchronous. */

@@ -6,6 +6,7 @@
 #define LOSS_ROUNDS 4   // workgroups of a launch that is shared out, in rounds of as many as the chip holds, at most
 #define LOSS_SLOTS 512  // workgroups that the chip holds with two waves per SIMD
 #define LOSS_MOST 0x7fff0000LL
+#define LOSS_MOST_SHARED ((1LL << 30) - 127) // of held rows whose columns two waves share: 512 threads for 128 of them, fewer than 2^32 in all
 #define LOSS_GRID (1 << 20) // workgroups of a kernel over rows at most: a grid holds fewer than 2^32 threads
 #define LOSS_WIDE_ROWS 128
 #define LOSS_WIDE_SCORES (1LL << 24)
@@ -471,6 +472,12 @@ static int32_t loss_check_ws(fae_ctx *ctx, const char *who, const void *ws, size
     return FAE_OK;
 }
 
+// a launch that sums O over columns shared by two waves (width above 128) holds half as many rows
+static int32_t loss_check_held(fae_ctx *ctx, const char *who, const char *what, int64_t n, int32_t width)
+{
+    return width > 128 && n >= LOSS_MOST_SHARED ? fae_fail(ctx, FAE_EINVAL, "%s: %s=%lld of width %d", who, what, (long long)n, width) : FAE_OK;
+}
+
 static void loss_run(fae_ctx *ctx, int how, int mode, const loss_args &a)
 {
     if (how == LOSS_F32)
@@ -588,6 +595,8 @@ extern "C" int32_t fae_softmax_loss_fwd(fae_ctx *ctx, const fae_softmax_loss *wh
     const LossSpan in[] = {loss_span("x", x, x_row_stride, d, n, size), loss_span("w", w, w_row_stride, d, v, size), loss_span("bias", what->bias, 1, 1, v, 4),
                            loss_span("targets", what->targets, 1, 1, n, what->target_bits / 8)};
     rc = loss_check_outputs(ctx, who, out, 4, in, 4);
+    if (rc == FAE_OK && mean)
+        rc = loss_check_held(ctx, who, "n_rows", n, what->width);
     if (rc != FAE_OK || n == 0)
         return rc;
     rc = loss_check_ws(ctx, who, ws, ws_bytes, fae_softmax_loss_fwd_workspace_bytes(what));
@@ -622,6 +631,10 @@ static int32_t loss_backward(fae_ctx *ctx, const char *who, const fae_softmax_lo
                            loss_span("targets", what->targets, 1, 1, n, what->target_bits / 8), loss_span("lse", lse, 1, 1, n, 4),
                            loss_span("mean", mean, d, d, n, 4), loss_span("gloss", gloss, 1, 1, n, 4), loss_span("loss", loss, 1, 1, n, 4)};
     rc = loss_check_outputs(ctx, who, out, 4, in, 8);
+    if (rc == FAE_OK && (gw || gbias))
+        rc = loss_check_held(ctx, who, "n_classes", v, what->width);
+    if (rc == FAE_OK && gx && !mean)
+        rc = loss_check_held(ctx, who, "n_rows", n, what->width);
     if (rc == FAE_OK)
         rc = loss_check_ws(ctx, who, ws, ws_bytes, fae_softmax_loss_bwd_workspace_bytes(what));
     if (rc != FAE_OK)
