@@ -48,18 +48,18 @@ static inline int loss_padded(int32_t width) { return width <= 32 ? 32 : width <
 #define LOSS_F32_WIDTH 64 // LOSS_F32 for wider rows is for few rows alone
 constexpr int loss_tile(int how, int dp) { return dp > 128 && loss_planes_of(how) > 1 ? 32 : 64; }
 // held rows of a wave, in blocks of 32: two where their registers leave room for two waves on a SIMD
-// held rows of a wave, in blocks of 32: two where their registers leave room for two waves on a SIMD
 constexpr int loss_blocks(int how, int dp, int mode)
 {
     return loss_planes_of(how) > 1 ? (dp <= 32 ? 2 : 1) : (dp <= (mode == LOSS_STATS ? 128 : 64) ? 2 : 1);
 }
 // Waves that hold the same rows, each with a share of O's columns: two for wide rows, whose O would leave room for one wave alone on a SIMD
-// (both take the scores: half of the matrix instructions are doubled, and still a step of 8192 x 32 768 x 256 bf16 takes 900 us instead of
-// 1130).
+// (both take all scores and powers: 48 matrix instructions for 32 x 32 scores where 32 are needed, and still a step of 8192 x 32 768 x 256 bf16
+// took 910 us instead of 1130 when this was chosen).
 constexpr int loss_shares(int how, int dp, int mode) { return mode != LOSS_STATS && dp > 128 ? 2 : 1; }
-// Waves per SIMD that registers are left for: three where 168 of them do (a few less than the compiler would take), else two.
-// Two and three: loss of 16 384 x 131 072 x 64 bf16 512 and 447 us, the gradient of 2048 x 100 000 x 64 fp32 218 and 203; but with
-// spills (fp32 means of width 32) 870 and 1120.
+// Waves per SIMD that registers are left for: three of 168 registers, else two of 256.
+// Two and three, when this was chosen: loss of 16 384 x 131 072 x 64 bf16 512 and 447 us, the gradient of 2048 x 100 000 x 64 fp32 218 and 203; but
+// with spills (fp32 means of width 32) 870 and 1120.  What the compiler spills all the same: means of 16-bit types of width 32, 42 registers
+// with a bias and 5 without; fp32 of width 64 to 192 up to 27, of 256 37 to 89 (9 for the loss with a bias).
 constexpr int loss_waves(int how, int dp, int mode)
 {
     if (how == LOSS_F32)
@@ -70,7 +70,9 @@ constexpr int loss_waves(int how, int dp, int mode)
 #define LOSS_WAVES 4
 constexpr int loss_held(int how, int dp, int mode) { return LOSS_WAVES * 32 * loss_blocks(how, dp, mode); }
 
-// few rows (no more than a wave holds): blocks of 32 that it holds, and the workgroups of a launch
+// few rows, LOSS_FEW_ROWS at most: blocks of 32 that a wave holds, and the workgroups of a launch.  Where a wave holds one block (fp32 padded to 96 and more, 16 bits
+// padded to 256), 33 to 64 rows are two of them, and the classes are read twice.  Spilled: 16 bits of width 129 to 192 in two blocks 163 registers
+// with a bias and 53 without, fp32 of width 193 to 256 65 and 43.
 constexpr int loss_few_blocks(int how, int dp) { return loss_planes_of(how) * dp <= 192 ? 2 : 1; }
 #define LOSS_FEW_ROWS 64
 #define LOSS_FEW_GROUPS 512 // two for each compute unit
@@ -103,7 +105,7 @@ typedef float loss_f4 __attribute__((ext_vector_type(4)));
 //                  first that brings the largest of a held row, or of all streamed rows, to 2^14 .. 2^15, where values down
 //                  to 2^-18 of it keep all their bits.  Costs a look at all streamed rows before.
 // SHIFT: probabilities are multiplied by 2^SHIFT (fp16 has nothing below 2^-24, and a million classes have probabilities of 2^-20).
-// MOST: the reference moves when a lane's sum of 16 of them reaches it.  They are then below fp16's 65504; the other types, with
+// MOST: the reference (in fp32's gradient, a class's power of two) moves when a lane's sum of 16 of them reaches it.  They are then below fp16's 65504; the other types, with
 // fp32's range, let the reference lag far behind the maximum, which costs no precision and spares them the search for it.
 template <int HOW> struct loss_type;
 template <> struct loss_type<LOSS_BF16> {
@@ -324,7 +326,7 @@ template <int DP> __device__ __forceinline__ int loss_swizzle(int m)
     return u == 0 ? ((m & 3) << 2) | ((m >> 2) & 3) : u == 8 ? ((m & 2) << 1) | ((m >> 2) & 3) : (m >> 2) & 3;
 }
 
-// (in pairs: a chain of 16 additions would wait for each of them)
+// (the gradient's, in pairs: a chain of 16 additions would wait for each of them; the forward's powers are added in a chain)
 __device__ __forceinline__ float loss_sum(const float (&v)[16])
 {
     float s[8];
@@ -377,7 +379,7 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
     const int tile0 = (int)((int64_t)a.tiles * split / a.n_split), tile1 = (int)((int64_t)a.tiles * (split + 1) / a.n_split);
     const int first = (int)(block * (LOSS_WAVES * 32 * NB)) + (MODE != LOSS_GRAD && a.spread ? 0 : wave * 32 * NB); // the wave's held rows; this lane's are first + ln + 32 b (they may lie behind the last)
 
-    // What was found before: the largest streamed value and gradient.  fp16 numbers of both are brought to a range that keeps them.
+    // What was found before: the largest streamed value (fp32) or gradient (fp16), to bring fp16 numbers to a range that keeps them.
     float st_scale = 1.f, g_scale = 1.f, g_log = 0.f, c_all = a.c, back = 1.f;
     int st_up = 0;
     if (HOW == LOSS_F32_WIDE || (HOW == LOSS_F16 && MODE == LOSS_GRAD)) {
@@ -721,7 +723,9 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
                     sum[b] += some[b];
             }
             if (HAS_O) {
-                // eight streamed rows of a lane are the eight of an operand: rows 16 t + 4 half + {0..3, 8..11}
+                // Eight streamed rows of a lane are the eight of an operand: rows 16 t + 4 half + {0..3, 8..11}.  P enters O as one number of the types of 16
+                // bits, off by up to half a step of itself: a second one would double O's matrix instructions.  gw of 16 384 x 100 003 x 64 bf16 is 2.4e-3
+                // off its definition in norm (1.65e-3 from its own rounding alone), of 3001 x 40 009 x 100 fp16 2.8e-4 (2.1e-4).
                 v8 pb[NB][2][P];
 #pragma unroll
                 for (int b = 0; b < NB; ++b)
@@ -812,7 +816,7 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
     }
 }
 
-// Few rows (serving, small test batches): bound by reading w, so that every wave takes a stretch of classes of its own, straight from memory to the
+// Few rows (serving, small test batches; sums in fp32 alone, so the target may move the reference here): bound by reading w, so that every wave takes a stretch of classes of its own, straight from memory to the
 // matrix instructions' registers with the next 32 on their way, and no wave waits for another before the end.  1 x 200 003 x 64 fp32
 // 14 to 16 us, 48 x 1 000 003 x 32 47 us, 2.7 TB/s.  When it was built it took 16.8 and 41 (the kernel above: 25 and 106, three of its waves
 // without rows; two steps ahead: 17.4 and 43.6; three waves per SIMD, which spill: 20.5 and 46.6).
