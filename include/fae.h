@@ -410,11 +410,13 @@ int32_t fae_dropout_bwd(fae_ctx *ctx, const fae_drop *drop, int64_t n_rows, int3
  * FAE_F32, FAE_BF16 or FAE_F16.  Values between rows are neither read nor written, buffers need the alignment of
  * their values.  Products of 16-bit values are exact and their sums fp32.  An fp32 value is taken as the sum of two fp16 numbers, after a power
  * of two that brings the largest value of its row, or of all rows, to 2^14 .. 2^15 (calls with few rows: as three bf16 numbers, without one);
- * of a product at most 2^-20 is lost, and a value below 2^-18 of that largest is kept to 2^-39 of it.  Probabilities enter the gradients'
- * sums rounded to the type (fp32: as two or three numbers again, of 22 bits and more; below 2^-34 of the largest that enters the same sum they may
- * vanish).  In fp16, gloss * p below 2^-39 of the largest |gloss| of all rows adds nothing to gw: less than half of fp16's smallest number
- * in all, unless n_rows * |gloss| * |x| * |scale| is beyond 2^14.  x and w have to be finite; but rows without a
- * target may hold anything in the gradients, and classes that are not offered anything anywhere unless they are a target.
+ * of a product at most 2^-20 is lost, and a value below 2^-18 of that largest is kept to 2^-39 of it.
+ * Probabilities enter the gradients' sums rounded to the type (a target's enters gw with twice the type's digits; fp32: as two or three numbers
+ * again, of 22 bits and more; below 2^-34 of the largest that enters the same sum they may vanish).  In fp16, gloss * p
+ * below 2^-39 of the largest |gloss| of all rows adds nothing to gw: less than half of fp16's smallest number in all,
+ * unless n_rows * |gloss| * |x| * |scale| is beyond 2^14.
+ * x and w have to be finite; but rows without a target may hold anything in the gradients, and classes that are not offered
+ * anything anywhere unless they are a target.
  *   targets: int32 or int64 (target_bits), one per row.  A negative one is a row without a target (a cold row, padding):
  *     its loss is 0, its gradients are 0 and it adds nothing to gw and gbias.  One of n_classes or more is treated so too,
  *     and reported as FAE_ERANGE by the next synchronising call.

@@ -588,6 +588,7 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
                         z[b][i] += less[i];
             }
             float pr[NB][16];
+            bool again = false;
             const float *sd = &side[buf][0][sb * 32 + half * 4];
             if (MODE == LOSS_GRAD) {
 #pragma unroll
@@ -602,8 +603,10 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
                 // A target in this wave's classes, or a gradient below 0: seldom.  P of a target is gloss (p - 1), of the other sign than gloss also where it
                 // is 0; p - 1 has been found before, as the exponential here and 1 would leave nothing of it in a row that is sure of its target.
                 const int32_t mine = __float_as_int(side[buf][2][sb * 32 + ln]);
-                const bool seldom = __any((mine >= first && mine < first + 32 * NB) || __float_as_int(side[buf][1][sb * 32 + ln]) >= 0);
+                const bool mine_hit = mine >= first && mine < first + 32 * NB;
+                const bool seldom = __any(mine_hit || __float_as_int(side[buf][1][sb * 32 + ln]) >= 0);
                 if (seldom) {
+                    again = __any(mine_hit);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const loss_f4 gt = *(const loss_f4 *)(sd + TM + j * 8), t = *(const loss_f4 *)(sd + 2 * TM + j * 8);
@@ -724,8 +727,10 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
             }
             if (HAS_O) {
                 // Eight streamed rows of a lane are the eight of an operand: rows 16 t + 4 half + {0..3, 8..11}.  P enters O as one number of the types of 16
-                // bits, off by up to half a step of itself: a second one would double O's matrix instructions.  gw of 16 384 x 100 003 x 64 bf16 is 2.4e-3
-                // off its definition in norm (1.65e-3 from its own rounding alone), of 3001 x 40 009 x 100 fp16 2.8e-4 (2.1e-4).
+                // bits, off by up to half a step of itself; a second one for all would double O's matrix instructions.  But what a row leaves to its target
+                // is most of a class's gradient, and a target is in few blocks: these enter the gradient's O once more, with what the rounding has taken.
+                // gw of 16 384 x 100 003 x 64 bf16 is then 1.66e-3 off its definition in norm, as if rounded once (2.4e-3 without), 3001 x 40 009 x 100
+                // fp16 2.1e-4 (2.8e-4), for 1 % of these steps and 1 to 5 % where every block has a target (16 384 x 512 to 16 384 x 64).
                 v8 pb[NB][2][P];
 #pragma unroll
                 for (int b = 0; b < NB; ++b)
@@ -746,25 +751,38 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
                             rounded[b] += loss_add(pb[b][1][0], loss_add(pb[b][0][0], 0.f));
                     }
                 }
+                auto products = [&]() {
 #pragma unroll
-                for (int d = 0; d < DS; ++d) {
+                    for (int d = 0; d < DS; ++d) {
 #pragma unroll
-                    for (int t = 0; t < 2; ++t) {
-                        v8 x[P];
+                        for (int t = 0; t < 2; ++t) {
+                            v8 x[P];
 #pragma unroll
-                        for (int p = 0; p < P; ++p) {
-                            s4 w[2];
+                            for (int p = 0; p < P; ++p) {
+                                s4 w[2];
 #pragma unroll
-                            for (int u = 0; u < 2; ++u)
-                                w[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                    (LOSS_LDS(s4) *)(lds + (o_at[d][u] + buf * TILE) + (p * PLANE + (sb * 32 + t * 16) * DP * 2)));
-                            x[p] = __builtin_shufflevector(__builtin_bit_cast(v4, w[0]), __builtin_bit_cast(v4, w[1]), 0, 1, 2, 3, 4, 5, 6, 7);
+                                for (int u = 0; u < 2; ++u)
+                                    w[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                        (LOSS_LDS(s4) *)(lds + (o_at[d][u] + buf * TILE) + (p * PLANE + (sb * 32 + t * 16) * DP * 2)));
+                                x[p] = __builtin_shufflevector(__builtin_bit_cast(v4, w[0]), __builtin_bit_cast(v4, w[1]), 0, 1, 2, 3, 4, 5, 6, 7);
+                            }
+#pragma unroll
+                            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                                for (int u = 6 - NP; u < 6; ++u)
+                                    o[b][d] = loss_mfma(x[LOSS_PA[u]], pb[b][t][LOSS_PB[u]], o[b][d]);
                         }
+                    }
+                };
+                products();
+                if constexpr (MODE == LOSS_GRAD && P == 1) {
+                    if (again) {
 #pragma unroll
                         for (int b = 0; b < NB; ++b)
 #pragma unroll
-                            for (int u = 6 - NP; u < 6; ++u)
-                                o[b][d] = loss_mfma(x[LOSS_PA[u]], pb[b][t][LOSS_PB[u]], o[b][d]);
+                            for (int i = 0; i < 16; ++i)
+                                pb[b][i / 8][0][i % 8] = (E)(pr[b][i] - (float)pb[b][i / 8][0][i % 8]);
+                        products();
                     }
                 }
             }
