@@ -70,8 +70,8 @@ constexpr int loss_waves(int how, int dp, int mode)
 #define LOSS_WAVES 4
 constexpr int loss_held(int how, int dp, int mode) { return LOSS_WAVES * 32 * loss_blocks(how, dp, mode); }
 
-// few rows, LOSS_FEW_ROWS at most: blocks of 32 that a wave holds, and the workgroups of a launch.  Where a wave holds one block (fp32 padded to 96 and more, 16 bits
-// padded to 256), 33 to 64 rows are two of them, and the classes are read twice.  Spilled: 16 bits of width 129 to 192 in two blocks 163 registers
+// few rows, LOSS_FEW_ROWS at most: blocks of 32 that a wave holds, and the workgroups of a launch.  Where a wave holds one block (fp32
+// padded to 96 and more, 16 bits padded to 256), 33 to 64 rows are two of them, and the classes are read twice.  Spilled: 16 bits of width 129 to 192 in two blocks 163 registers
 // with a bias and 53 without, fp32 of width 193 to 256 65 and 43.
 constexpr int loss_few_blocks(int how, int dp) { return loss_planes_of(how) * dp <= 192 ? 2 : 1; }
 #define LOSS_FEW_ROWS 64
@@ -105,8 +105,9 @@ typedef float loss_f4 __attribute__((ext_vector_type(4)));
 //                  first that brings the largest of a held row, or of all streamed rows, to 2^14 .. 2^15, where values down
 //                  to 2^-18 of it keep all their bits.  Costs a look at all streamed rows before.
 // SHIFT: probabilities are multiplied by 2^SHIFT (fp16 has nothing below 2^-24, and a million classes have probabilities of 2^-20).
-// MOST: the reference (in fp32's gradient, a class's power of two) moves when a lane's sum of 16 of them reaches it.  They are then below fp16's 65504; the other types, with
-// fp32's range, let the reference lag far behind the maximum, which costs no precision and spares them the search for it.
+// MOST: the reference (in fp32's gradient, a class's power of two) moves when a lane's sum of 16 of them reaches it.  They are then below fp16's
+// 65504; the other types, with fp32's range, let the reference lag far behind the maximum, which costs no precision and spares them the
+// search for it.
 template <int HOW> struct loss_type;
 template <> struct loss_type<LOSS_BF16> {
     typedef fae_bf16 T, E;
@@ -834,8 +835,9 @@ __global__ __launch_bounds__(LOSS_WAVES * 64 * loss_shares(HOW, DP, MODE)) __att
     }
 }
 
-// Few rows (serving, small test batches; sums in fp32 alone, so the target may move the reference here): bound by reading w, so that every wave takes a stretch of classes of its own, straight from memory to the
-// matrix instructions' registers with the next 32 on their way, and no wave waits for another before the end.  1 x 200 003 x 64 fp32
+// Few rows (serving, small test batches; sums in fp32 alone, so the target may move the reference here): bound by reading w, so that every wave
+// takes a stretch of classes of its own, straight from memory to the matrix instructions' registers with the next 32 on their way, and
+// no wave waits for another before the end.  1 x 200 003 x 64 fp32
 // 14 to 16 us, 48 x 1 000 003 x 32 47 us, 2.7 TB/s.  When it was built it took 16.8 and 41 (the kernel above: 25 and 106, three of its waves
 // without rows; two steps ahead: 17.4 and 43.6; three waves per SIMD, which spill: 20.5 and 46.6).
 template <int HOW, int DP, int NB, bool BIAS>
